@@ -389,6 +389,105 @@ int pyramid_stitch_add(int32_t D, int32_t H, int32_t W, int32_t K, int32_t z0, i
 int pyramid_stitch_finish(int32_t D, int32_t H, int32_t W, int32_t K, const void *acc,
                           const void *wsum, void *out, void *stream);
 
+/* ---- layer norm, the linear scan and 8-bit checkpoints ------------------- */
+
+/* Slices of larger tensors (the next token's rows) are ordinary arguments here:
+ * tensors of `dtype`, states, lengths, dgamma and dbeta are aligned to their
+ * element, stats to 8 bytes; saved, ws and the codes and scales of 8-bit
+ * checkpoints (and what is packed into them or unpacked) to 16 bytes. */
+
+/* Layer norm over the C channels of each of M rows (voxels, tokens):
+ *   mean = sum_c x / C, var = sum_c (x - mean)^2 / C, rstd = 1/sqrt(var + eps),
+ *   y[m][c] = (x[m][c] - mean) rstd gamma[c] + beta[c].
+ *   x, y [M][C], gamma, beta [C] in `dtype`; statistics in fp32; eps > 0.
+ *   stats       : NULL, or fp32 [M][2], overwritten with (mean, rstd) of each
+ *                 row for the backward.
+ *   xq, xscale  : both NULL, or the 8-bit checkpoint of x (codes [M][C] and
+ *                 pyramid_checkpoint8_scales(M * C) scales), written in the
+ *                 same call with the values of pyramid_checkpoint8_pack.
+ * 1 <= C <= 16384, M >= 1, M * C <= 2^38. */
+int pyramid_layer_norm_forward(int64_t M, int32_t C, int32_t dtype, float eps, const void *x,
+                               const void *gamma, const void *beta, void *y, void *stats,
+                               void *xq, void *xscale, void *stream);
+
+/* Bytes of workspace for pyramid_layer_norm_backward; 0 for a bad shape. */
+size_t pyramid_layer_norm_workspace_size(int64_t M, int32_t C);
+
+/* Gradient of pyramid_layer_norm_forward.  With xh = (x - mean) rstd and
+ * a = dy gamma:
+ *   dx = rstd (a - sum_c a / C - xh sum_c (a xh) / C),
+ *   dgamma = sum_m dy xh, dbeta = sum_m dy   (fixed order of the sums).
+ *   x           : the forward's input in `dtype` (xscale NULL), or its codes,
+ *                 with xscale their scales.
+ *   gamma, dy   : `dtype`; stats: the forward's, of the unrounded x.
+ *   dx          : NULL, or [M][C] in `dtype`, overwritten.
+ *   dgamma, dbeta : fp32 [C], overwritten.
+ *   ws          : at least pyramid_layer_norm_workspace_size(M, C) bytes. */
+int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void *x,
+                                const void *xscale, const void *gamma, const void *stats,
+                                const void *dy, void *dx, void *dgamma, void *dbeta, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/* Gated linear recurrence along the middle axis of [B][T][I] tensors: the
+ * sweep of one direction whose update is linear in the state, so that a long
+ * axis is computed in parallel.  For sequence b of n = lengths[b] steps
+ * (clamped to 0..T; T where lengths is NULL), position s = 0..n-1 is step
+ * t = s, or n - 1 - s with reverse = 1:
+ *   f = sigmoid(g[b][t]),  h_s = f h_{s-1} + (1 - f) u[b][t],  h_{-1} = h0[b],
+ * per channel.  Steps t >= n hold nothing: they are not read, h there is 0.
+ * Any axis of a channels-last volume is such a tensor: z of [N][D][H][W][O]
+ * is [N][D][H W O], y is [N D][H][W O], x is [N D H][W][O].
+ *   g, u, h     : [B][T][I] in `dtype`; h overwritten.
+ *   lengths     : NULL, or int32 [B] on the device.
+ *   h0          : NULL (zeros), or fp32 [B][I].
+ *   hT          : NULL, or fp32 [B][I]: the state after each sequence's last
+ *                 position (h0 where it has none), overwritten; may be h0
+ *                 itself, so single steps (T = 1) update a state in place.
+ *   saved       : NULL, or pyramid_scan_saved_size() bytes for the backward:
+ *                 fp32 [B][ceil(T/16)][I], the state before positions 0, 16, ...
+ *   ws          : at least pyramid_scan_workspace_size() bytes.
+ * States are fp32 whatever the storage type.  B, T, I >= 1, B T I <= 2^38. */
+size_t pyramid_scan_workspace_size(int64_t B, int64_t T, int64_t I);
+size_t pyramid_scan_saved_size(int64_t B, int64_t T, int64_t I);
+int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t reverse,
+                         const void *g, const void *u, const int32_t *lengths, const void *h0,
+                         void *h, void *hT, void *saved, void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of pyramid_scan_forward.  With G_s the gradient of h_s,
+ *   G_s = dh[b][t] + f_{s+1} G_{s+1}   (the last position takes dhT as well),
+ *   du = (1 - f) G_s,  dg = G_s (h_{s-1} - u) f (1 - f),  dh0 = f_0 G_0;
+ * dg and du of steps that a sequence does not have are 0, its dh0 is dhT where
+ * it has none at all.
+ *   g, u        : the forward's, in `dtype` (gscale and uscale NULL), or codes of
+ *                 8-bit checkpoints with their scales (both coded): f, u and
+ *                 the states between kept ones are then those of the codes'
+ *                 values.
+ *   saved       : the forward's.   lengths, reverse: the forward's.
+ *   dh          : [B][T][I] in `dtype`;  dhT: NULL (zeros), or fp32 [B][I].
+ *   dg, du      : [B][T][I] in `dtype`, overwritten.
+ *   dh0         : NULL, or fp32 [B][I], overwritten; may be dhT itself. */
+int pyramid_scan_backward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t reverse,
+                          const void *g, const void *gscale, const void *u, const void *uscale,
+                          const int32_t *lengths, const void *saved, const void *dh,
+                          const void *dhT, void *dg, void *du, void *dh0, void *ws,
+                          size_t ws_bytes, void *stream);
+
+/* Activations held in 8 bits between a forward and its backward.  Blocks of 64
+ * consecutive elements of a flat tensor share a bf16 scale, the smallest bf16
+ * number >= max|x| / 127; code = x / scale to the nearest integer, ties to
+ * even; value = code * scale, off by at most half a scale.  A block whose
+ * largest magnitude is below 2^-119 is held as zeros; one with an infinity or
+ * a NaN is held as NaNs.
+ *   pyramid_checkpoint8_scales  number of scales of n elements (0 for n < 1);
+ *   pyramid_checkpoint8_pack    x [n] (`dtype`) -> q int8 [n], scale bf16;
+ *   pyramid_checkpoint8_unpack  x [n] (`dtype`) = the values.
+ * 1 <= n <= 2^38. */
+int64_t pyramid_checkpoint8_scales(int64_t n);
+int pyramid_checkpoint8_pack(int64_t n, int32_t dtype, const void *x, void *q, void *scale,
+                             void *stream);
+int pyramid_checkpoint8_unpack(int64_t n, int32_t dtype, const void *q, const void *scale,
+                               void *x, void *stream);
+
 /* Forward implementation selection, for testing and tuning (process-wide):
  * 0 = automatic (default): the persistent MFMA sweep where it supports the
  * shape (fp32, O = 16, C <= 4, grid co-resident), else the plane-step MFMA

@@ -32,6 +32,10 @@ __all__ = [
     "pyramid_sample_cubes", "draw_cubes", "pyramid_lstm_device_status",
     "pyramid_lstm_set_wait_test", "PLSTM_DEVICE_WAIT_GAVE_UP", "pyramid_lstm_forward_noalloc",
     "PLSTM_NOALLOC_SCRATCH_BYTES", "PLSTM_ESCRATCH",
+    "pyramid_layer_norm_workspace_size", "pyramid_layer_norm_forward",
+    "pyramid_layer_norm_backward", "pyramid_scan_workspace_size", "pyramid_scan_saved_size",
+    "pyramid_scan_forward", "pyramid_scan_backward", "pyramid_checkpoint8_scales",
+    "pyramid_checkpoint8_pack", "pyramid_checkpoint8_unpack", "checkpoint8_empty",
 ]
 
 PLSTM_F32 = 0
@@ -147,6 +151,26 @@ def load():
     lib.pyramid_stitch_add.restype = ctypes.c_int
     lib.pyramid_stitch_finish.argtypes = [i32] * 4 + [vp, vp, vp, vp]
     lib.pyramid_stitch_finish.restype = ctypes.c_int
+    lib.pyramid_layer_norm_workspace_size.argtypes = [i64, i32]
+    lib.pyramid_layer_norm_workspace_size.restype = sz
+    lib.pyramid_layer_norm_forward.argtypes = [i64, i32, i32, f32] + [vp] * 8
+    lib.pyramid_layer_norm_forward.restype = ctypes.c_int
+    lib.pyramid_layer_norm_backward.argtypes = [i64, i32, i32] + [vp] * 9 + [sz, vp]
+    lib.pyramid_layer_norm_backward.restype = ctypes.c_int
+    lib.pyramid_scan_workspace_size.argtypes = [i64] * 3
+    lib.pyramid_scan_workspace_size.restype = sz
+    lib.pyramid_scan_saved_size.argtypes = [i64] * 3
+    lib.pyramid_scan_saved_size.restype = sz
+    lib.pyramid_scan_forward.argtypes = [i64] * 3 + [i32] * 2 + [vp] * 8 + [sz, vp]
+    lib.pyramid_scan_forward.restype = ctypes.c_int
+    lib.pyramid_scan_backward.argtypes = [i64] * 3 + [i32] * 2 + [vp] * 12 + [sz, vp]
+    lib.pyramid_scan_backward.restype = ctypes.c_int
+    lib.pyramid_checkpoint8_scales.argtypes = [i64]
+    lib.pyramid_checkpoint8_scales.restype = i64
+    lib.pyramid_checkpoint8_pack.argtypes = [i64, i32] + [vp] * 4
+    lib.pyramid_checkpoint8_pack.restype = ctypes.c_int
+    lib.pyramid_checkpoint8_unpack.argtypes = [i64, i32] + [vp] * 4
+    lib.pyramid_checkpoint8_unpack.restype = ctypes.c_int
     lib.pyramid_lstm_timing_enable.argtypes = [ctypes.c_int]
     lib.pyramid_lstm_timing_enable.restype = ctypes.c_int
     lib.pyramid_lstm_timing_read.argtypes = [ctypes.c_int, ctypes.c_char_p,
@@ -479,6 +503,175 @@ def pyramid_stitch_finish(acc, wsum, out, stream=None):
     D, H, W, K = acc.shape
     _check("pyramid_stitch_finish", load().pyramid_stitch_finish(
         D, H, W, K, _ptr(acc), _ptr(wsum), _ptr(out), _stream(stream)))
+
+
+def _tensor(name, t, shape, dtype, device):
+    """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
+    if t is None:
+        return None
+    p = _ptr(t)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s %s on %s, got %s %s on %s" % (
+            name, dtype, list(shape), device, t.dtype, list(t.shape), t.device))
+    return p
+
+
+def _storage(name, t, dims):
+    """Storage type code of an operator's main tensor of `dims` dimensions (None: any)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch.Tensor, got %r" % type(t))
+    if t.dtype not in _DT or dims not in (None, t.dim()):
+        raise ValueError("%s must be float32 or bfloat16%s" % (
+            name, "" if dims is None else " with %d dimensions" % dims))
+    return _DT[t.dtype]
+
+
+def _bytes(ws, device):
+    if ws.device != device:
+        raise ValueError("ws must be on %s" % device)
+    return _ptr(ws), ws.numel() * ws.element_size()
+
+
+def _codes(name, q, scale, shape, device):
+    """Pointers of an 8-bit checkpoint of a tensor of `shape`."""
+    n = 1
+    for e in shape:
+        n *= e
+    return (_tensor(name, q, shape, torch.int8, device),
+            _tensor(name + "'s scale", scale, (-(-n // 64),), torch.bfloat16, device))
+
+
+def _run(name, x, stream, *args):
+    """Calls entry point `name` with x's device current, on `stream` or that
+    device's current stream."""
+    with torch.cuda.device(x.device):
+        _check(name, getattr(load(), name)(*args, _stream(stream)))
+
+
+def pyramid_layer_norm_workspace_size(M: int, C: int) -> int:
+    return int(load().pyramid_layer_norm_workspace_size(M, C))
+
+
+def pyramid_layer_norm_forward(x, gamma, beta, y, stats=None, xq=None, xscale=None, eps=1e-5,
+                               stream=None):
+    """Layer norm of the rows of x [M][C] (gamma, beta [C], y [M][C], one
+    dtype).  stats [M][2] fp32 takes each row's (mean, rstd) for the backward;
+    xq, xscale (see checkpoint8_empty) take x's 8-bit checkpoint."""
+    dt, dev = _storage("x", x, 2), x.device
+    M, C = x.shape
+    if (xq is None) != (xscale is None):
+        raise ValueError("xq and xscale go together")
+    q, qs = _codes("xq", xq, xscale, x.shape, dev)
+    _run("pyramid_layer_norm_forward", x, stream, M, C, dt, float(eps), _ptr(x),
+         _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
+         _tensor("y", y, x.shape, x.dtype, dev), _tensor("stats", stats, (M, 2), torch.float32, dev),
+         q, qs)
+
+
+def pyramid_layer_norm_backward(x, gamma, stats, dy, dx, dgamma, dbeta, xscale=None, ws=None,
+                                stream=None):
+    """Gradients of pyramid_layer_norm_forward: dx [M][C] (or None), dgamma and
+    dbeta [C] fp32, from dy [M][C] and the forward's input x, or its codes x
+    with their scales xscale."""
+    dt, dev = _storage("dy", dy, 2), dy.device
+    M, C = dy.shape
+    if xscale is None:
+        px, ps = _tensor("x", x, dy.shape, dy.dtype, dev), None
+    else:
+        px, ps = _codes("x", x, xscale, dy.shape, dev)
+    if ws is None:
+        ws = _workspace(pyramid_layer_norm_workspace_size(M, C), dev)
+    _run("pyramid_layer_norm_backward", dy, stream, M, C, dt, px, ps,
+         _tensor("gamma", gamma, (C,), dy.dtype, dev),
+         _tensor("stats", stats, (M, 2), torch.float32, dev), _ptr(dy),
+         _tensor("dx", dx, dy.shape, dy.dtype, dev),
+         _tensor("dgamma", dgamma, (C,), torch.float32, dev),
+         _tensor("dbeta", dbeta, (C,), torch.float32, dev), *_bytes(ws, dev))
+
+
+def pyramid_scan_workspace_size(B: int, T: int, I: int) -> int:
+    return int(load().pyramid_scan_workspace_size(B, T, I))
+
+
+def pyramid_scan_saved_size(B: int, T: int, I: int) -> int:
+    return int(load().pyramid_scan_saved_size(B, T, I))
+
+
+def _check_saved(saved, B, T, I, device):
+    if saved is None:
+        return None
+    if saved.numel() * saved.element_size() < pyramid_scan_saved_size(B, T, I) or \
+            saved.device != device:
+        raise ValueError("saved must hold pyramid_scan_saved_size bytes on %s" % device)
+    return _ptr(saved)
+
+
+def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None, saved=None,
+                         ws=None, stream=None):
+    """Gated linear recurrence along axis 1 of g, u [B][T][I] into h (same
+    shape and dtype): f = sigmoid(g_t), h_t = f h_{t-1} + (1 - f) u_t, from the
+    last step with `reverse`.  lengths [B] int32 gives each sequence its own
+    number of steps; h0, hT [B][I] fp32 are the state before and after (hT may
+    be h0); saved (pyramid_scan_saved_size bytes) keeps what the backward
+    needs.  ws=None allocates the workspace with torch."""
+    dt, dev = _storage("g", g, 3), g.device
+    B, T, I = g.shape
+    if ws is None:
+        ws = _workspace(pyramid_scan_workspace_size(B, T, I), dev)
+    _run("pyramid_scan_forward", g, stream, B, T, I, dt, int(bool(reverse)), _ptr(g),
+         _tensor("u", u, g.shape, g.dtype, dev), _tensor("lengths", lengths, (B,), torch.int32, dev),
+         _tensor("h0", h0, (B, I), torch.float32, dev), _tensor("h", h, g.shape, g.dtype, dev),
+         _tensor("hT", hT, (B, I), torch.float32, dev), _check_saved(saved, B, T, I, dev),
+         *_bytes(ws, dev))
+
+
+def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, dhT=None, dh0=None,
+                          gscale=None, uscale=None, ws=None, stream=None):
+    """Gradients of pyramid_scan_forward: dg, du [B][T][I] and dh0 [B][I] fp32
+    (or None) from dh, dhT (or None) and the forward's inputs and saved
+    buffer; g and u may be codes with their scales gscale and uscale."""
+    dt, dev = _storage("dh", dh, 3), dh.device
+    B, T, I = dh.shape
+    if (gscale is None) != (uscale is None):
+        raise ValueError("g and u are both coded or neither")
+    if gscale is None:
+        pg, pgs = _tensor("g", g, dh.shape, dh.dtype, dev), None
+        pu, pus = _tensor("u", u, dh.shape, dh.dtype, dev), None
+    else:
+        pg, pgs = _codes("g", g, gscale, dh.shape, dev)
+        pu, pus = _codes("u", u, uscale, dh.shape, dev)
+    if ws is None:
+        ws = _workspace(pyramid_scan_workspace_size(B, T, I), dev)
+    _run("pyramid_scan_backward", dh, stream, B, T, I, dt, int(bool(reverse)), pg, pgs, pu, pus,
+         _tensor("lengths", lengths, (B,), torch.int32, dev), _check_saved(saved, B, T, I, dev),
+         _ptr(dh), _tensor("dhT", dhT, (B, I), torch.float32, dev),
+         _tensor("dg", dg, dh.shape, dh.dtype, dev), _tensor("du", du, dh.shape, dh.dtype, dev),
+         _tensor("dh0", dh0, (B, I), torch.float32, dev), *_bytes(ws, dev))
+
+
+def pyramid_checkpoint8_scales(n: int) -> int:
+    return int(load().pyramid_checkpoint8_scales(n))
+
+
+def checkpoint8_empty(x):
+    """Uninitialised 8-bit checkpoint of a tensor like x: (codes of x's shape
+    int8, scales bf16, one per 64 elements)."""
+    return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
+            torch.empty(-(-x.numel() // 64), dtype=torch.bfloat16, device=x.device))
+
+
+def pyramid_checkpoint8_pack(x, q, scale, stream=None):
+    """Codes q (x's shape, int8) and scales of x (float32 or bfloat16, any shape)."""
+    dt, px = _storage("x", x, None), _ptr(x)
+    pq, ps = _codes("q", q, scale, x.shape, x.device)
+    _run("pyramid_checkpoint8_pack", x, stream, x.numel(), dt, px, pq, ps)
+
+
+def pyramid_checkpoint8_unpack(q, scale, x, stream=None):
+    """x (float32 or bfloat16, q's shape) = the values of a checkpoint."""
+    dt, px = _storage("x", x, None), _ptr(x)
+    pq, ps = _codes("q", q, scale, x.shape, x.device)
+    _run("pyramid_checkpoint8_unpack", x, stream, x.numel(), dt, pq, ps, px)
 
 
 def pyramid_lstm_timing_enable(on: bool) -> None:

@@ -1,0 +1,75 @@
+// Activations held in 8 bits (device side).  A flat tensor is cut into blocks
+// of 64 consecutive elements; a block has one bf16 scale and an int8 code per
+// element:
+//   top   = max |x| over the block
+//   scale = the smallest bf16 number >= top / 127
+//   code  = x / scale to the nearest integer, ties to even    (|code| <= 127)
+//   value = code * scale                                       (15 bits: exact)
+// An error of half a scale, so at most top / 252 (bf16 has 8 bits: scale <=
+// top / 127 (1 + 2^-7)).  A block whose top is below 2^-119 (where the scale
+// would leave bf16's normal range) has scale 0 and codes 0.  A block with an
+// infinity or a NaN has scale NaN: its values are NaN, so that a checkpoint
+// never hides a divergence.
+#pragma once
+
+#include "common.h"
+
+namespace plstm {
+
+constexpr int kCodeBlock = 64;
+constexpr uint32_t kCodeSmallBits = 0x04000000u;   // 2^-119
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+inline long long code_blocks(long long n) { return (n + kCodeBlock - 1) / kCodeBlock; }
+
+__device__ inline uint32_t float_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
+__device__ inline float bits_float(uint32_t u) { return __builtin_bit_cast(float, u); }
+
+// Scale (bf16 bits) of a block from the bits of its largest magnitude, taken
+// as integers so that a NaN is the largest of all.
+__device__ inline uint16_t code_scale(uint32_t top_bits)
+{
+    if (top_bits >= kInfBits) return 0x7fc0u;
+    if (top_bits < kCodeSmallBits) return 0;
+    const float top = bits_float(top_bits);
+    // IEEE quotient: it never rounds below a bf16 number that the true one exceeds
+    const uint32_t low = float_bits(top / 127.0f) & 0xffff0000u;
+    // 8-bit by 7-bit product: exact
+    return (uint16_t)((low >> 16) + (bits_float(low) * 127.0f < top ? 1u : 0u));
+}
+
+// Codes of a block with scale s: r is 1 / s within an ulp, 0 where codes are 0.
+struct Coder {
+    float s, half_s, r;
+    __device__ explicit Coder(uint16_t scale)
+    {
+        s = bf16_to_f32(scale);
+        const bool zero = scale == 0 || scale == 0x7fc0u;
+        if (zero) s = 0.0f;
+        half_s = 0.5f * s;
+        r = zero ? 0.0f : __builtin_amdgcn_rcpf(s);
+    }
+    // fp32 input: x r is within 1e-5 of x / s, so its nearest integer q is the
+    // right one or, next to a tie, the one beside it.  The remainder x - q s
+    // is exact in one fma (both operands are multiples of a bit that is at
+    // most 2^-17 of s); past half a scale, or at half with q odd, the
+    // neighbour on its side is taken.
+    __device__ int code(float x) const
+    {
+        if (r == 0.0f) return 0;
+        const float q = rintf(x * r);
+        const float rem = fmaf(-q, s, x);
+        int c = (int)q;
+        const uint32_t a = float_bits(rem) & 0x7fffffffu;
+        if (a + (uint32_t)(c & 1) > float_bits(half_s)) c += rem > 0.0f ? 1 : -1;
+        return c;
+    }
+};
+
+// A tensor held in 8 bits, read element by element.
+struct Coded {
+    const int8_t *q;
+    const uint16_t *scale;
+};
+
+}  // namespace plstm

@@ -106,6 +106,8 @@ template <> struct Store<uint16_t> {
 
 __device__ inline float sigmoidf_(float a) { return 1.0f / (1.0f + __expf(-a)); }
 
+inline bool aligned_to(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+inline size_t dtype_size(int dtype) { return dtype == PLSTM_F32 ? 4 : 2; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Bump allocator over a caller-provided workspace.
@@ -169,6 +171,10 @@ int generic_dx(const Geom &g, const float *wx, const float *dA, float *dx, hipSt
 
 // dst[i] = src[i] for n bf16 values widened to fp32.
 int bf16_to_f32(const void *src, float *dst, long long n, hipStream_t st);
+
+// 8-bit checkpoint of n values (code8.h): codes q, a bf16 scale per 64.
+int checkpoint8_pack(long long n, int dtype, const void *x, int8_t *q, uint16_t *scale,
+                     hipStream_t st);
 
 // Fully connected glue.
 int fc_tanh_forward(long long M, int Cin, int Cout, int dtype, const void *x, const void *w,
