@@ -1,26 +1,42 @@
 // 8-bit activation checkpoints: pack and unpack (format in code8.h).
-#include "code8.h"
+#include "rows.h"
 #include "timing.h"
 
 namespace plstm {
 namespace {
 
 constexpr int kPackThreads = 256;
+constexpr int kPackUnroll = 4;      // pieces of 16 bytes that a lane has in flight
+constexpr int kPackBlocks = 4096;
 
-// A wave per block of 64 elements, a lane per element.
+// A lane per 16 bytes of x; a block of 64 elements is 16 lanes (fp32) or 8
+// (bf16).  A workgroup takes kPackUnroll consecutive stretches of a piece a lane,
+// all loaded before the first is coded.
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
 k_pack8(const T *__restrict__ x, int8_t *__restrict__ q, uint16_t *__restrict__ scale, long long n)
 {
-    const long long i = (long long)blockIdx.x * kPackThreads + threadIdx.x;
-    const float v = i < n ? Store<T>::load(x, i) : 0.0f;
-    uint32_t top = float_bits(v) & 0x7fffffffu;
-    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    const uint16_t s = code_scale(top);
-    if (i >= n) return;
-    const Coder c(s);
-    q[i] = (int8_t)c.code(v);
-    if ((i & 63) == 0) scale[i >> 6] = s;
+    constexpr int N = Piece<T>::N;
+    constexpr long long stretch = (long long)kPackThreads * N;
+    for (long long at0 = blockIdx.x * stretch * kPackUnroll + threadIdx.x * N; at0 - threadIdx.x * N < n;
+         at0 += gridDim.x * stretch * kPackUnroll) {
+        float v[kPackUnroll][N];
+#pragma unroll
+        for (int t = 0; t < kPackUnroll; ++t) {
+            const long long at = at0 + t * stretch, left = n - at;
+            load_piece(x + at, left > N ? N : (int)left, v[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < kPackUnroll; ++t) {
+            const long long at = at0 + t * stretch, left = n - at;
+            const uint16_t s = code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[t])));
+            const Coder c(s);
+            int code[N];
+            code_piece<T>(c, v[t], code);
+            store_codes<N>(q + at, left > N ? N : (int)left, code);
+            if ((at & (kCodeBlock - 1)) == 0 && left > 0) scale[at >> 6] = s;
+        }
+    }
 }
 
 template <typename T>
@@ -28,9 +44,29 @@ __global__ void __launch_bounds__(kPackThreads)
 k_unpack8(const int8_t *__restrict__ q, const uint16_t *__restrict__ scale, T *__restrict__ x,
           long long n)
 {
-    const long long i = (long long)blockIdx.x * kPackThreads + threadIdx.x;
-    if (i >= n) return;
-    Store<T>::store(x, i, (float)q[i] * bf16_to_f32(scale[i >> 6]));
+    constexpr int N = Piece<T>::N;
+    constexpr long long stretch = (long long)kPackThreads * N;
+    for (long long at0 = blockIdx.x * stretch * kPackUnroll + threadIdx.x * N; at0 < n;
+         at0 += gridDim.x * stretch * kPackUnroll) {
+        float v[kPackUnroll][N];
+#pragma unroll
+        for (int t = 0; t < kPackUnroll; ++t) {
+            const long long at = at0 + t * stretch, left = n - at;
+            load_coded<N>(q, scale, at, left > N ? N : (int)left, v[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < kPackUnroll; ++t) {
+            const long long at = at0 + t * stretch, left = n - at;
+            store_piece(x + at, left > N ? N : (int)left, v[t]);
+        }
+    }
+}
+
+unsigned pack_grid(long long n, int dtype)
+{
+    const long long each = (long long)kPackThreads * kPackUnroll * (dtype == PLSTM_F32 ? 4 : 8);
+    const long long blocks = (n + each - 1) / each;
+    return (unsigned)(blocks < kPackBlocks ? blocks : kPackBlocks);
 }
 
 }  // namespace
@@ -38,7 +74,7 @@ k_unpack8(const int8_t *__restrict__ q, const uint16_t *__restrict__ scale, T *_
 int checkpoint8_pack(long long n, int dtype, const void *x, int8_t *q, uint16_t *scale,
                      hipStream_t st)
 {
-    const unsigned grid = (unsigned)((n + kPackThreads - 1) / kPackThreads);
+    const unsigned grid = pack_grid(n, dtype);
     if (dtype == PLSTM_F32)
         k_pack8<<<grid, kPackThreads, 0, st>>>((const float *)x, q, scale, n);
     else
@@ -77,7 +113,7 @@ int pyramid_checkpoint8_unpack(int64_t n, int32_t dtype, const void *q, const vo
         return PLSTM_EINVAL;
     if (n > (1LL << 38)) return PLSTM_EUNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
-    const unsigned grid = (unsigned)((n + kPackThreads - 1) / kPackThreads);
+    const unsigned grid = pack_grid(n, dtype);
     timing_begin("unpack8", st);
     if (dtype == PLSTM_F32)
         k_unpack8<<<grid, kPackThreads, 0, st>>>((const int8_t *)q, (const uint16_t *)scale,

@@ -64,12 +64,14 @@ struct Coder {
         if (a + (uint32_t)(c & 1) > float_bits(half_s)) c += rem > 0.0f ? 1 : -1;
         return c;
     }
-};
-
-// A tensor held in 8 bits, read element by element.
-struct Coded {
-    const int8_t *q;
-    const uint16_t *scale;
+    // bf16 input: x / s is a tie or at least 2^-9 from one (both have 8 bits),
+    // and x r is within 2^-14 of it.  Added to 3 2^12 and taken away again it is
+    // rounded to a multiple of 2^-10: ties come out as ties, nothing else does.
+    __device__ int code_bf16(float x) const
+    {
+        const float k = 12288.0f;
+        return r == 0.0f ? 0 : (int)rintf(fmaf(x, r, k) - k);
+    }
 };
 
 }  // namespace plstm

@@ -6,114 +6,333 @@
 //   dgamma = sum_m dy xh, dbeta = sum_m dy
 // Rows are read in the storage type or, in the backward, from an 8-bit
 // checkpoint (code8.h); sums and statistics are fp32.
-#include "code8.h"
+#include "rows.h"
 #include "timing.h"
 
 namespace plstm {
 namespace {
 
-constexpr int kNormThreads = 256;
-constexpr int kNormParts = 256;     // row ranges of the weights' gradients
 constexpr int kNormMaxC = 16384;
+constexpr int kNormMaxParts = 512;  // workgroups, each with a part of the weights' gradients
+constexpr int kNormFwdBlocks = 8192;
 
-__device__ inline float wave_sum(float v)
-{
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
+// A row is held in registers by G lanes, K pieces of 16 bytes (N elements)
+// each: lane j has elements (j + G k) N .., k < K.  Short rows share a wave,
+// long ones take four or sixteen waves.  U rows of a lane group are loaded before
+// the first is used, so that short rows keep enough bytes in flight.
+template <typename T, int G, int K>
+struct Rows {
+    static constexpr int N = Piece<T>::N;
+    static constexpr int U = G > 64 ? 1 : K == 1 ? 4 : K == 2 ? 2 : 1;
+};
 
-template <typename T>
-__device__ inline float load_row(const T *x, const uint16_t *, long long i)
+// Sum of a value over the G lanes of a group, in every lane.  Groups of several
+// waves exchange through `lds` (one slot a wave; not the slots of the exchange
+// before it).
+template <int G>
+__device__ inline float group_sum(float v, float *lds)
 {
-    return Store<T>::load(x, i);
-}
-__device__ inline float load_row(const int8_t *x, const uint16_t *scale, long long i)
-{
-    return (float)x[i] * bf16_to_f32(scale[i >> 6]);
-}
-
-// A wave per row.
-template <typename T>
-__global__ void __launch_bounds__(kNormThreads)
-k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__restrict__ beta,
-           T *__restrict__ y, float2 *__restrict__ stats, long long M, int C, float eps)
-{
-    const long long m = (long long)blockIdx.x * (kNormThreads / 64) + threadIdx.x / 64;
-    if (m >= M) return;
-    const int lane = threadIdx.x & 63;
-    const long long at = m * C;
+    v = lanes_sum<(G < 64 ? G : 64)>(v);
+    if (G <= 64) return v;
+    const int wave = threadIdx.x / 64, first = wave / (G / 64) * (G / 64);
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
+    __syncthreads();
     float s = 0.0f;
-    for (int c = lane; c < C; c += 64) s += Store<T>::load(x, at + c);
-    const float mean = wave_sum(s) / (float)C;
-    float v = 0.0f;
-    for (int c = lane; c < C; c += 64) {
-        const float d = Store<T>::load(x, at + c) - mean;
-        v += d * d;
-    }
-    const float rstd = 1.0f / sqrtf(wave_sum(v) / (float)C + eps);
-    for (int c = lane; c < C; c += 64)
-        Store<T>::store(y, at + c,
-                        (Store<T>::load(x, at + c) - mean) * rstd * Store<T>::load(gamma, c) +
-                            Store<T>::load(beta, c));
-    if (stats && lane == 0) stats[m] = make_float2(mean, rstd);
+#pragma unroll
+    for (int w = 0; w < G / 64; ++w) s += lds[first + w];
+    return s;
 }
 
-template <typename T, typename X>
-__global__ void __launch_bounds__(kNormThreads)
-k_norm_dx(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
-          const T *__restrict__ gamma, const float2 *__restrict__ stats,
-          const T *__restrict__ dy, T *__restrict__ dx, long long M, int C)
+// CODE: also the 8-bit checkpoint of x, where its blocks of 64 elements are
+// aligned lanes of a wave (fused_codes).
+template <typename T, int G, int K, bool CODE>
+__global__ void __launch_bounds__(G > 256 ? G : 256)
+k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__restrict__ beta,
+           T *__restrict__ y, float2 *__restrict__ stats, int8_t *__restrict__ xq,
+           uint16_t *__restrict__ xscale, long long M, int C, float eps)
 {
-    const long long m = (long long)blockIdx.x * (kNormThreads / 64) + threadIdx.x / 64;
-    if (m >= M) return;
-    const int lane = threadIdx.x & 63;
-    const long long at = m * C;
-    const float2 st = stats[m];
-    float sa = 0.0f, sb = 0.0f;
-    for (int c = lane; c < C; c += 64) {
-        const float a = Store<T>::load(dy, at + c) * Store<T>::load(gamma, c);
-        sa += a;
-        sb += a * ((load_row(x, xscale, at + c) - st.x) * st.y);
+    constexpr int N = Rows<T, G, K>::N, U = Rows<T, G, K>::U;
+    constexpr int threads = G > 256 ? G : 256, rows = threads / G;
+    __shared__ float lds[2][2][threads / 64];
+    const int j = threadIdx.x % G, group = threadIdx.x / G;
+    const float inv = 1.0f / (float)C;
+    float ga[K][N], be[K][N];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (j + G * k) * N;
+        load_piece(gamma + c, C - c, ga[k]);
+        load_piece(beta + c, C - c, be[k]);
     }
-    sa = wave_sum(sa) / (float)C;
-    sb = wave_sum(sb) / (float)C;
-    for (int c = lane; c < C; c += 64) {
-        const float a = Store<T>::load(dy, at + c) * Store<T>::load(gamma, c);
-        const float xh = (load_row(x, xscale, at + c) - st.x) * st.y;
-        Store<T>::store(dx, at + c, st.y * (a - sa - xh * sb));
+    int turn = 0;
+    for (long long m0 = (long long)blockIdx.x * rows * U; m0 < M;
+         m0 += (long long)gridDim.x * rows * U) {
+        float v[U][K][N];
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const long long m = m0 + t * rows + group;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = (j + G * k) * N;
+                load_piece(x + m * C + c, m < M ? C - c : 0, v[t][k]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const long long m = m0 + t * rows + group;
+            if (CODE) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const int c = (j + G * k) * N;
+                    const long long at = m * C + c;
+                    const uint16_t s =
+                        code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[t][k])));
+                    const Coder cd(s);
+                    int code[N];
+                    code_piece<T>(cd, v[t][k], code);
+                    if (m < M && c < C) {
+                        store_codes<N>(xq + at, N, code);
+                        if ((at & (kCodeBlock - 1)) == 0) xscale[at >> 6] = s;
+                    }
+                }
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum += v[t][k][i];
+            sum = group_sum<G>(sum, lds[turn][0]);
+            // the quotient sum / C, one step better than the product with 1 / C: a row of
+            // one value has to have that value as its mean, or rstd = eps^-1/2 shows it
+            float mean = sum * inv;
+            mean = fmaf(fmaf(-mean, (float)C, sum), inv, mean);
+            float var = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = (j + G * k) * N;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    v[t][k][i] -= mean;
+                    if (c + i < C) var = fmaf(v[t][k][i], v[t][k][i], var);
+                }
+            }
+            const float rstd = rsqrtf(fmaf(group_sum<G>(var, lds[turn][1]), inv, eps));
+            turn ^= 1;
+            if (m < M) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const int c = (j + G * k) * N;
+                    float o[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        o[i] = fmaf(v[t][k][i] * rstd, ga[k][i], be[k][i]);
+                    store_piece(y + m * C + c, C - c, o);
+                }
+                if (stats && j == 0) stats[m] = make_float2(mean, rstd);
+            }
+        }
     }
 }
 
-// Partial sums of dgamma and dbeta over the rows m = part, part + kNormParts, ...
-// part [kNormParts][2][C].
-template <typename T, typename X>
-__global__ void __launch_bounds__(kNormThreads)
-k_norm_dw(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
-          const float2 *__restrict__ stats, const T *__restrict__ dy, float *__restrict__ part,
-          long long M, int C)
+template <typename T, int N>
+__device__ inline void load_x(const T *x, const uint16_t *, long long at, int have, float *v)
 {
-    const int c = blockIdx.x * kNormThreads + threadIdx.x;
-    if (c >= C) return;
-    float g = 0.0f, b = 0.0f;
-    for (long long m = blockIdx.y; m < M; m += kNormParts) {
-        const float2 st = stats[m];
-        const float d = Store<T>::load(dy, m * C + c);
-        g += d * ((load_row(x, xscale, m * C + c) - st.x) * st.y);
-        b += d;
-    }
-    part[(long long)blockIdx.y * 2 * C + c] = g;
-    part[(long long)blockIdx.y * 2 * C + C + c] = b;
+    load_piece(x + at, have, v);
+}
+template <typename T, int N>
+__device__ inline void load_x(const int8_t *x, const uint16_t *scale, long long at, int have,
+                              float *v)
+{
+    load_coded<N>(x, scale, at, have, v);
 }
 
-__global__ void __launch_bounds__(kNormThreads)
-k_norm_dw_sum(const float *__restrict__ part, float *__restrict__ dgamma,
+// A workgroup walks every gridDim-th stretch of rows with its columns' sums of
+// dy xh and dy in registers; at the end its lane groups' sums are added in
+// order and written as its part [2][C] of `part` (dgamma and dbeta themselves
+// where it is alone).
+template <typename T, typename X, int G, int K>
+__global__ void __launch_bounds__(G > 512 ? G : 512)
+k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
+           const T *__restrict__ gamma, const float2 *__restrict__ stats,
+           const T *__restrict__ dy, T *__restrict__ dx, float *__restrict__ dgamma,
+           float *__restrict__ dbeta, float *__restrict__ part, long long M, int C)
+{
+    constexpr int N = Rows<T, G, K>::N, U = Rows<T, G, K>::U;
+    constexpr int threads = G > 512 ? G : 512, rows = threads / G;
+    constexpr int wide = G > 64 ? G : 64, parts = threads / wide;   // sums a column has in the end
+    __shared__ float lds[2][2][threads / 64];
+    __shared__ float cols[parts > 1 ? parts : 1][parts > 1 ? G * K * N : 1];
+    const int j = threadIdx.x % G, group = threadIdx.x / G;
+    const float inv = 1.0f / (float)C;
+    float ga[K][N], sg[K][N], sb[K][N];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (j + G * k) * N;
+        load_piece(gamma + c, C - c, ga[k]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sg[k][i] = sb[k][i] = 0.0f;
+    }
+    int turn = 0;
+    for (long long m0 = (long long)blockIdx.x * rows * U; m0 < M;
+         m0 += (long long)gridDim.x * rows * U) {
+        float v[U][K][N], d[U][K][N];
+        float2 st[U];
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const long long m = m0 + t * rows + group;
+            st[t] = m < M ? stats[m] : make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = (j + G * k) * N, have = m < M ? C - c : 0;
+                load_x<T, N>(x, xscale, m * C + c, have, v[t][k]);
+                load_piece(dy + m * C + c, have, d[t][k]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            const long long m = m0 + t * rows + group;
+            float ta = 0.0f, tb = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float xh = (v[t][k][i] - st[t].x) * st[t].y, a = d[t][k][i] * ga[k][i];
+                    v[t][k][i] = xh;
+                    ta += a;
+                    tb = fmaf(a, xh, tb);
+                    sg[k][i] = fmaf(d[t][k][i], xh, sg[k][i]);
+                    sb[k][i] += d[t][k][i];
+                }
+            if (!dx) continue;
+            ta = group_sum<G>(ta, lds[turn][0]) * inv;
+            tb = group_sum<G>(tb, lds[turn][1]) * inv;
+            turn ^= 1;
+            if (m < M) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const int c = (j + G * k) * N;
+                    float o[N];
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        o[i] = st[t].y * (fmaf(d[t][k][i], ga[k][i], -ta) - v[t][k][i] * tb);
+                    store_piece(dx + m * C + c, C - c, o);
+                }
+            }
+        }
+    }
+    float *og = gridDim.x == 1 ? dgamma : part + (long long)blockIdx.x * 2 * C;
+    float *ob = gridDim.x == 1 ? dbeta : og + C;
+    // lanes of a wave with the same columns, then the waves (or wider groups)
+    for (int pass = 0; pass < 2; ++pass) {
+        float (*s)[N] = pass ? sb : sg;
+        float *out = pass ? ob : og;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int w = G; w < 64; w *= 2) s[k][i] += __shfl_xor(s[k][i], w);
+        if (parts == 1) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = (j + G * k) * N;
+#pragma unroll
+                for (int i = 0; i < N; i += 4) store_piece(out + c + i, C - c - i, s[k] + i);
+            }
+            continue;
+        }
+        if (pass) __syncthreads();
+        if (G >= 64 || (threadIdx.x & 63) < G) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    cols[threadIdx.x / wide][(j + G * k) * N + i] = s[k][i];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < C; c += threads) {
+            float v = 0.0f;
+#pragma unroll
+            for (int p = 0; p < parts; ++p) v += cols[p][c];
+            out[c] = v;
+        }
+    }
+}
+
+// dgamma and dbeta from `count` parts, in order: 64 columns and 16 stretches of parts a workgroup.
+__global__ void __launch_bounds__(1024)
+k_norm_dw_sum(const float *__restrict__ part, int count, float *__restrict__ dgamma,
               float *__restrict__ dbeta, int C)
 {
-    const int c = blockIdx.x * kNormThreads + threadIdx.x;
-    if (c >= 2 * C) return;
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const int c = blockIdx.x * 64 + lane;
     float s = 0.0f;
-    for (int k = 0; k < kNormParts; ++k) s += part[(long long)k * 2 * C + c];
+    if (c < 2 * C)
+        for (int k = w; k < count; k += 16) s += part[(long long)k * 2 * C + c];
+    lds[w][lane] = s;
+    __syncthreads();
+    if (w != 0 || c >= 2 * C) return;
+    s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += lds[k][lane];
     (c < C ? dgamma[c] : dbeta[c - C]) = s;
+}
+
+// Workgroups of the backward: what rows there are for, at most kNormMaxParts
+// (two for each CU), and fewer for long rows, whose parts cost as much as rows do.
+long long norm_parts(long long M, int C, int rows)
+{
+    const long long need = (M + rows - 1) / rows, most = C > 2048 ? kNormMaxParts / 2 : kNormMaxParts;
+    return need < most ? need : most;
+}
+
+// fn(G, K) as compile-time constants for rows of C elements of type T.
+template <int V> struct Const { static constexpr int value = V; };
+template <typename T, typename F>
+int with_rows(int C, F fn)
+{
+    constexpr int N = Piece<T>::N;
+    const int pieces = (C + N - 1) / N;
+    if (pieces <= 1) return fn(Const<1>(), Const<1>());
+    if (pieces <= 2) return fn(Const<2>(), Const<1>());
+    if (pieces <= 4) return fn(Const<4>(), Const<1>());
+    if (pieces <= 8) return fn(Const<8>(), Const<1>());
+    if (pieces <= 16) return fn(Const<16>(), Const<1>());
+    if (pieces <= 32) return fn(Const<32>(), Const<1>());
+    if (pieces <= 64) return fn(Const<64>(), Const<1>());
+    if (pieces <= 128) return fn(Const<64>(), Const<2>());
+    if (pieces <= 256) return fn(Const<256>(), Const<1>());
+    if (pieces <= 512) return fn(Const<256>(), Const<2>());
+    if (pieces <= 1024) return fn(Const<1024>(), Const<1>());
+    if (pieces <= 2048) return fn(Const<1024>(), Const<2>());
+    if constexpr (N == 4) return fn(Const<1024>(), Const<4>());
+    return PLSTM_EUNSUPPORTED;
+}
+
+// Blocks of 64 elements lie in whole rows, or whole rows of pieces in a block.
+template <typename T> bool fused_codes(int C)
+{
+    return C % kCodeBlock == 0 || (kCodeBlock % C == 0 && C >= Piece<T>::N);
+}
+
+template <typename T>
+int norm_forward(long long M, int C, float eps, const T *x, const T *gamma, const T *beta, T *y,
+                 float2 *stats, int8_t *xq, uint16_t *xscale, hipStream_t st)
+{
+    return with_rows<T>(C, [&](auto g, auto k) -> int {
+        constexpr int G = decltype(g)::value, K = decltype(k)::value;
+        constexpr int threads = G > 256 ? G : 256, rows = threads / G * Rows<T, G, K>::U;
+        const long long need = (M + rows - 1) / rows;
+        const unsigned grid = (unsigned)(need < kNormFwdBlocks ? need : kNormFwdBlocks);
+        if (xq)
+            k_norm_fwd<T, G, K, true><<<grid, threads, 0, st>>>(x, gamma, beta, y, stats, xq,
+                                                               xscale, M, C, eps);
+        else
+            k_norm_fwd<T, G, K, false><<<grid, threads, 0, st>>>(x, gamma, beta, y, stats,
+                                                                nullptr, nullptr, M, C, eps);
+        PLSTM_LAUNCH_CHECK();
+        return PLSTM_OK;
+    });
 }
 
 int check_rows(int64_t M, int32_t C, int32_t dtype)
@@ -124,38 +343,43 @@ int check_rows(int64_t M, int32_t C, int32_t dtype)
     return PLSTM_OK;
 }
 
+// `launches` counts the kernels.
 template <typename T, typename X>
 int norm_backward(long long M, int C, const X *x, const uint16_t *xscale, const T *gamma,
                   const float2 *stats, const T *dy, T *dx, float *dgamma, float *dbeta,
-                  float *part, hipStream_t st)
+                  float *part, int *launches, hipStream_t st)
 {
-    if (dx) {
-        k_norm_dx<T, X><<<(unsigned)((M + 3) / 4), kNormThreads, 0, st>>>(x, xscale, gamma, stats,
-                                                                         dy, dx, M, C);
+    return with_rows<T>(C, [&](auto g, auto k) -> int {
+        constexpr int G = decltype(g)::value, K = decltype(k)::value;
+        constexpr int threads = G > 512 ? G : 512, rows = threads / G * Rows<T, G, K>::U;
+        const int count = (int)norm_parts(M, C, rows);
+        k_norm_bwd<T, X, G, K><<<(unsigned)count, threads, 0, st>>>(
+            x, xscale, gamma, stats, dy, dx, dgamma, dbeta, part, M, C);
         PLSTM_LAUNCH_CHECK();
-    }
-    const unsigned cols = (unsigned)((C + kNormThreads - 1) / kNormThreads);
-    k_norm_dw<T, X><<<dim3(cols, kNormParts), kNormThreads, 0, st>>>(x, xscale, stats, dy, part,
-                                                                    M, C);
-    PLSTM_LAUNCH_CHECK();
-    k_norm_dw_sum<<<(unsigned)((2 * C + kNormThreads - 1) / kNormThreads), kNormThreads, 0, st>>>(
-        part, dgamma, dbeta, C);
-    PLSTM_LAUNCH_CHECK();
-    return PLSTM_OK;
+        *launches = 1;
+        if (count > 1) {
+            k_norm_dw_sum<<<(unsigned)((2 * C + 63) / 64), 1024, 0, st>>>(part, count, dgamma,
+                                                                         dbeta, C);
+            PLSTM_LAUNCH_CHECK();
+            *launches = 2;
+        }
+        return PLSTM_OK;
+    });
 }
 
 template <typename T>
 int norm_backward_from(long long M, int C, const void *x, const void *xscale, const void *gamma,
                        const void *stats, const void *dy, void *dx, void *dgamma, void *dbeta,
-                       void *ws, hipStream_t st)
+                       void *ws, int *launches, hipStream_t st)
 {
     if (xscale)
         return norm_backward<T, int8_t>(M, C, (const int8_t *)x, (const uint16_t *)xscale,
                                         (const T *)gamma, (const float2 *)stats, (const T *)dy,
-                                        (T *)dx, (float *)dgamma, (float *)dbeta, (float *)ws, st);
+                                        (T *)dx, (float *)dgamma, (float *)dbeta, (float *)ws,
+                                        launches, st);
     return norm_backward<T, T>(M, C, (const T *)x, nullptr, (const T *)gamma,
                                (const float2 *)stats, (const T *)dy, (T *)dx, (float *)dgamma,
-                               (float *)dbeta, (float *)ws, st);
+                               (float *)dbeta, (float *)ws, launches, st);
 }
 
 }  // namespace
@@ -168,14 +392,14 @@ extern "C" {
 size_t pyramid_layer_norm_workspace_size(int64_t M, int32_t C)
 {
     if (check_rows(M, C, PLSTM_F32) != PLSTM_OK) return 0;
-    return align_up((size_t)kNormParts * 2 * C * sizeof(float), 256);
+    return align_up((size_t)norm_parts(M, C, 1) * 2 * C * sizeof(float), 256);
 }
 
 int pyramid_layer_norm_forward(int64_t M, int32_t C, int32_t dtype, float eps, const void *x,
                                const void *gamma, const void *beta, void *y, void *stats,
                                void *xq, void *xscale, void *stream)
 {
-    const int rc = check_rows(M, C, dtype);
+    int rc = check_rows(M, C, dtype);
     if (rc != PLSTM_OK) return rc;
     if (!(eps > 0.0f) || !x || !gamma || !beta || !y || !xq != !xscale) return PLSTM_EINVAL;
     const size_t e = dtype_size(dtype);
@@ -184,23 +408,21 @@ int pyramid_layer_norm_forward(int64_t M, int32_t C, int32_t dtype, float eps, c
         return PLSTM_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     timing_begin("norm_fwd", st);
-    if (xq) {
-        const int prc = checkpoint8_pack((long long)M * C, dtype, x, (int8_t *)xq,
-                                         (uint16_t *)xscale, st);
-        if (prc != PLSTM_OK) return prc;
+    const bool fused = dtype == PLSTM_F32 ? fused_codes<float>(C) : fused_codes<uint16_t>(C);
+    if (xq && !fused) {
+        rc = checkpoint8_pack((long long)M * C, dtype, x, (int8_t *)xq, (uint16_t *)xscale, st);
+        if (rc != PLSTM_OK) return rc;
     }
-    const unsigned grid = (unsigned)((M + 3) / 4);
-    if (dtype == PLSTM_F32)
-        k_norm_fwd<<<grid, kNormThreads, 0, st>>>((const float *)x, (const float *)gamma,
-                                                  (const float *)beta, (float *)y,
-                                                  (float2 *)stats, M, C, eps);
-    else
-        k_norm_fwd<<<grid, kNormThreads, 0, st>>>((const uint16_t *)x, (const uint16_t *)gamma,
-                                                  (const uint16_t *)beta, (uint16_t *)y,
-                                                  (float2 *)stats, M, C, eps);
-    PLSTM_LAUNCH_CHECK();
-    timing_end(xq ? 2 : 1, st);
-    return PLSTM_OK;
+    int8_t *q = fused ? (int8_t *)xq : nullptr;
+    rc = dtype == PLSTM_F32
+             ? norm_forward(M, C, eps, (const float *)x, (const float *)gamma,
+                            (const float *)beta, (float *)y, (float2 *)stats, q,
+                            (uint16_t *)xscale, st)
+             : norm_forward(M, C, eps, (const uint16_t *)x, (const uint16_t *)gamma,
+                            (const uint16_t *)beta, (uint16_t *)y, (float2 *)stats, q,
+                            (uint16_t *)xscale, st);
+    if (rc == PLSTM_OK) timing_end(xq && !fused ? 2 : 1, st);
+    return rc;
 }
 
 int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void *x,
@@ -219,12 +441,13 @@ int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void 
     if (ws_bytes < pyramid_layer_norm_workspace_size(M, C)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     timing_begin("norm_bwd", st);
+    int launches = 0;
     rc = dtype == PLSTM_F32
              ? norm_backward_from<float>(M, C, x, xscale, gamma, stats, dy, dx, dgamma, dbeta, ws,
-                                         st)
+                                         &launches, st)
              : norm_backward_from<uint16_t>(M, C, x, xscale, gamma, stats, dy, dx, dgamma, dbeta,
-                                            ws, st);
-    if (rc == PLSTM_OK) timing_end(dx ? 3 : 2, st);
+                                            ws, &launches, st);
+    if (rc == PLSTM_OK) timing_end(launches, st);
     return rc;
 }
 

@@ -1,0 +1,187 @@
+// 16-byte pieces of rows in the storage types, and sums over groups of lanes
+// (device side).  Pieces start at any element: global memory takes 16-byte
+// accesses at any address, so rows of odd lengths need no other path than a
+// last piece that is read and written element by element.
+#pragma once
+
+#include "code8.h"
+
+namespace plstm {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Two fp32 values rounded to bf16 (nearest, ties to even; NaN kept quiet) in
+// one conversion, the first in the low half.
+__device__ inline uint32_t pack_bf16(float a, float b)
+{
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+template <typename T> struct Piece;
+
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+    __device__ static void load(const float *p, float *v)
+    {
+        const V w = *(const V *)p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = w[j];
+    }
+    __device__ static void store(float *p, const float *v)
+    {
+        V w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = v[j];
+        *(V *)p = w;
+    }
+};
+
+template <> struct Piece<uint16_t> {
+    static constexpr int N = 8;
+    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+    __device__ static void load(const uint16_t *p, float *v)
+    {
+        const V w = *(const V *)p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bits_float(w[j] << 16);
+            v[2 * j + 1] = bits_float(w[j] & 0xffff0000u);
+        }
+    }
+    __device__ static void store(uint16_t *p, const float *v)
+    {
+        V w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        *(V *)p = w;
+    }
+};
+
+// Elements [0, have) of a piece; the others read as 0 and are not written.
+template <typename T>
+__device__ inline void load_piece(const T *p, int have, float *v)
+{
+    constexpr int N = Piece<T>::N;
+    if (have >= N) {
+        Piece<T>::load(p, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < have ? Store<T>::load(p, j) : 0.0f;
+    }
+}
+template <typename T>
+__device__ inline void store_piece(T *p, int have, const float *v)
+{
+    constexpr int N = Piece<T>::N;
+    if (have >= N) {
+        Piece<T>::store(p, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < have) Store<T>::store(p, j, v[j]);
+    }
+}
+
+// N = 4 or 8 codes as bytes, and back.
+template <int N>
+__device__ inline void store_codes(int8_t *q, int have, const int *c)
+{
+    typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
+    if (have >= N) {
+        V w;
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j)
+            w[j] = (uint32_t)(c[4 * j] & 255) | (uint32_t)(c[4 * j + 1] & 255) << 8 |
+                   (uint32_t)(c[4 * j + 2] & 255) << 16 | (uint32_t)c[4 * j + 3] << 24;
+        *(V *)q = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < have) q[j] = (int8_t)c[j];
+    }
+}
+template <int N>
+__device__ inline void load_codes(const int8_t *q, int have, float *v)
+{
+    typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
+    if (have >= N) {
+        const V w = *(const V *)q;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = (float)(int)(int8_t)(w[j / 4] >> (8 * (j % 4)));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < have ? (float)q[j] : 0.0f;
+    }
+}
+
+// The values of codes at flat elements at .. at + N - 1 of a checkpoint (two
+// blocks at most).
+template <int N>
+__device__ inline void load_coded(const int8_t *q, const uint16_t *scale, long long at, int have,
+                                  float *v)
+{
+    if (have > N) have = N;
+    if (have <= 0) have = 0;
+    load_codes<N>(q + at, have, v);
+    if (have == 0) return;
+    const float s0 = bf16_to_f32(scale[at >> 6]), s1 = bf16_to_f32(scale[(at + have - 1) >> 6]);
+    const int turn = kCodeBlock - (int)(at & (kCodeBlock - 1));
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] *= j < turn ? s0 : s1;
+}
+
+// Largest / sum over aligned groups of G lanes (a power of two <= 64), in every
+// lane.  Up to 16 lanes by data-parallel moves: once lanes that differ in the
+// lower bits agree, a mirrored half row or row stands for the lane across.
+template <int CTRL>
+__device__ inline uint32_t moved(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+}
+template <int G, typename F>
+__device__ inline uint32_t over_lanes(uint32_t v, F f)
+{
+    if (G >= 2) v = f(v, moved<0xb1>(v));       // quad_perm 1 0 3 2
+    if (G >= 4) v = f(v, moved<0x4e>(v));       // quad_perm 2 3 0 1
+    if (G >= 8) v = f(v, moved<0x141>(v));      // row_half_mirror
+    if (G >= 16) v = f(v, moved<0x140>(v));     // row_mirror
+    if (G >= 32) v = f(v, (uint32_t)__shfl_xor((int)v, 16));
+    if (G >= 64) v = f(v, (uint32_t)__shfl_xor((int)v, 32));
+    return v;
+}
+template <int G>
+__device__ inline float lanes_sum(float v)
+{
+    return bits_float(over_lanes<G>(float_bits(v), [](uint32_t a, uint32_t b) {
+        return float_bits(bits_float(a) + bits_float(b));
+    }));
+}
+template <int G>
+__device__ inline uint32_t lanes_max(uint32_t v)
+{
+    return over_lanes<G>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
+// Bits of the largest magnitude of N values, a NaN the largest of all.
+template <int N>
+__device__ inline uint32_t top_bits(const float *v)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = max(top, float_bits(v[j]) & 0x7fffffffu);
+    return top;
+}
+
+// Codes of a piece of a block whose largest magnitude has bits `top`.
+template <typename T>
+__device__ inline void code_piece(const Coder &c, const float *v, int *q)
+{
+#pragma unroll
+    for (int j = 0; j < Piece<T>::N; ++j)
+        q[j] = Piece<T>::N == 8 ? c.code_bf16(v[j]) : c.code(v[j]);
+}
+
+}  // namespace plstm
