@@ -10,6 +10,7 @@ the binding raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -505,47 +506,63 @@ def pyramid_stitch_finish(acc, wsum, out, stream=None):
         D, H, W, K, _ptr(acc), _ptr(wsum), _ptr(out), _stream(stream)))
 
 
-def _tensor(name, t, shape, dtype, device):
-    """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
-    if t is None:
-        return None
-    p = _ptr(t)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s %s on %s, got %s %s on %s" % (
-            name, dtype, list(shape), device, t.dtype, list(t.shape), t.device))
-    return p
-
-
-def _storage(name, t, dims):
-    """Storage type code of an operator's main tensor of `dims` dimensions (None: any)."""
+# The operators below run down to a few microseconds, so their marshalling keeps
+# to plain integers: data_ptr() and the raw stream instead of ctypes and torch
+# objects, and no device switch where the tensors' device is current.
+def _main(name, t, dims):
+    """Storage type code and pointer of an operator's main tensor of `dims` dimensions (None: any)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("expected a torch.Tensor, got %r" % type(t))
     if t.dtype not in _DT or dims not in (None, t.dim()):
         raise ValueError("%s must be float32 or bfloat16%s" % (
             name, "" if dims is None else " with %d dimensions" % dims))
-    return _DT[t.dtype]
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return _DT[t.dtype], t.data_ptr()
+
+
+def _tensor(name, t, shape, dtype, device):
+    """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch.Tensor, got %r" % type(t))
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be %s %s on %s and contiguous, got %s %s on %s%s" % (
+            name, dtype, list(shape), device, t.dtype, list(t.shape), t.device,
+            "" if t.is_contiguous() else ", not contiguous"))
+    return t.data_ptr()
 
 
 def _bytes(ws, device):
-    if ws.device != device:
-        raise ValueError("ws must be on %s" % device)
-    return _ptr(ws), ws.numel() * ws.element_size()
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous and on %s" % device)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _codes(name, q, scale, shape, device):
-    """Pointers of an 8-bit checkpoint of a tensor of `shape`."""
-    n = 1
-    for e in shape:
-        n *= e
-    return (_tensor(name, q, shape, torch.int8, device),
-            _tensor(name + "'s scale", scale, (-(-n // 64),), torch.bfloat16, device))
+def _codes(name, q, scale, x, device):
+    """Pointers of an 8-bit checkpoint of a tensor of x's shape."""
+    return (_tensor(name, q, x.shape, torch.int8, device),
+            _tensor(name + "'s scale", scale, (-(-x.numel() // 64),), torch.bfloat16, device))
 
 
 def _run(name, x, stream, *args):
     """Calls entry point `name` with x's device current, on `stream` or that
     device's current stream."""
-    with torch.cuda.device(x.device):
-        _check(name, getattr(load(), name)(*args, _stream(stream)))
+    dev = x.get_device()
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    else:
+        stream = _stream(stream)
+    if dev == torch.cuda.current_device():
+        rc = getattr(load(), name)(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = getattr(load(), name)(*args, stream)
+    if rc != 0:
+        raise PyramidLSTMError(name, rc)
 
 
 def pyramid_layer_norm_workspace_size(M: int, C: int) -> int:
@@ -557,12 +574,12 @@ def pyramid_layer_norm_forward(x, gamma, beta, y, stats=None, xq=None, xscale=No
     """Layer norm of the rows of x [M][C] (gamma, beta [C], y [M][C], one
     dtype).  stats [M][2] fp32 takes each row's (mean, rstd) for the backward;
     xq, xscale (see checkpoint8_empty) take x's 8-bit checkpoint."""
-    dt, dev = _storage("x", x, 2), x.device
+    (dt, px), dev = _main("x", x, 2), x.device
     M, C = x.shape
     if (xq is None) != (xscale is None):
         raise ValueError("xq and xscale go together")
-    q, qs = _codes("xq", xq, xscale, x.shape, dev)
-    _run("pyramid_layer_norm_forward", x, stream, M, C, dt, float(eps), _ptr(x),
+    q, qs = _codes("xq", xq, xscale, x, dev) if xq is not None else (None, None)
+    _run("pyramid_layer_norm_forward", x, stream, M, C, dt, eps, px,
          _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
          _tensor("y", y, x.shape, x.dtype, dev), _tensor("stats", stats, (M, 2), torch.float32, dev),
          q, qs)
@@ -573,37 +590,57 @@ def pyramid_layer_norm_backward(x, gamma, stats, dy, dx, dgamma, dbeta, xscale=N
     """Gradients of pyramid_layer_norm_forward: dx [M][C] (or None), dgamma and
     dbeta [C] fp32, from dy [M][C] and the forward's input x, or its codes x
     with their scales xscale."""
-    dt, dev = _storage("dy", dy, 2), dy.device
+    (dt, pdy), dev = _main("dy", dy, 2), dy.device
     M, C = dy.shape
     if xscale is None:
         px, ps = _tensor("x", x, dy.shape, dy.dtype, dev), None
     else:
-        px, ps = _codes("x", x, xscale, dy.shape, dev)
+        px, ps = _codes("x", x, xscale, dy, dev)
     if ws is None:
         ws = _workspace(pyramid_layer_norm_workspace_size(M, C), dev)
     _run("pyramid_layer_norm_backward", dy, stream, M, C, dt, px, ps,
          _tensor("gamma", gamma, (C,), dy.dtype, dev),
-         _tensor("stats", stats, (M, 2), torch.float32, dev), _ptr(dy),
+         _tensor("stats", stats, (M, 2), torch.float32, dev), pdy,
          _tensor("dx", dx, dy.shape, dy.dtype, dev),
          _tensor("dgamma", dgamma, (C,), torch.float32, dev),
          _tensor("dbeta", dbeta, (C,), torch.float32, dev), *_bytes(ws, dev))
 
 
+@functools.lru_cache(maxsize=256)
 def pyramid_scan_workspace_size(B: int, T: int, I: int) -> int:
     return int(load().pyramid_scan_workspace_size(B, T, I))
 
 
+@functools.lru_cache(maxsize=256)
 def pyramid_scan_saved_size(B: int, T: int, I: int) -> int:
     return int(load().pyramid_scan_saved_size(B, T, I))
 
 
-def _check_saved(saved, B, T, I, device):
+def _saved(saved, B, T, I, device):
     if saved is None:
         return None
-    if saved.numel() * saved.element_size() < pyramid_scan_saved_size(B, T, I) or \
-            saved.device != device:
+    if saved.device != device or not saved.is_contiguous() or \
+            saved.numel() * saved.element_size() < pyramid_scan_saved_size(B, T, I):
         raise ValueError("saved must hold pyramid_scan_saved_size bytes on %s" % device)
-    return _ptr(saved)
+    return saved.data_ptr()
+
+
+_scan_ws = {}
+
+
+def _scan_workspace(ws, B, T, I, device):
+    """Pointer and bytes of `ws`, or of one made with torch.  A call that needs
+    none takes 256 bytes as every call does, and shares them: it does not touch
+    them."""
+    if ws is None:
+        need = pyramid_scan_workspace_size(B, T, I)
+        if need > 256:
+            ws = _workspace(need, device)
+        else:
+            ws = _scan_ws.get(device)
+            if ws is None:
+                ws = _scan_ws[device] = _workspace(256, device)
+    return ws, _bytes(ws, device)
 
 
 def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None, saved=None,
@@ -614,15 +651,13 @@ def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None,
     number of steps; h0, hT [B][I] fp32 are the state before and after (hT may
     be h0); saved (pyramid_scan_saved_size bytes) keeps what the backward
     needs.  ws=None allocates the workspace with torch."""
-    dt, dev = _storage("g", g, 3), g.device
+    (dt, pg), dev = _main("g", g, 3), g.device
     B, T, I = g.shape
-    if ws is None:
-        ws = _workspace(pyramid_scan_workspace_size(B, T, I), dev)
-    _run("pyramid_scan_forward", g, stream, B, T, I, dt, int(bool(reverse)), _ptr(g),
+    ws, pws = _scan_workspace(ws, B, T, I, dev)
+    _run("pyramid_scan_forward", g, stream, B, T, I, dt, int(bool(reverse)), pg,
          _tensor("u", u, g.shape, g.dtype, dev), _tensor("lengths", lengths, (B,), torch.int32, dev),
          _tensor("h0", h0, (B, I), torch.float32, dev), _tensor("h", h, g.shape, g.dtype, dev),
-         _tensor("hT", hT, (B, I), torch.float32, dev), _check_saved(saved, B, T, I, dev),
-         *_bytes(ws, dev))
+         _tensor("hT", hT, (B, I), torch.float32, dev), _saved(saved, B, T, I, dev), *pws)
 
 
 def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, dhT=None, dh0=None,
@@ -630,7 +665,7 @@ def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, 
     """Gradients of pyramid_scan_forward: dg, du [B][T][I] and dh0 [B][I] fp32
     (or None) from dh, dhT (or None) and the forward's inputs and saved
     buffer; g and u may be codes with their scales gscale and uscale."""
-    dt, dev = _storage("dh", dh, 3), dh.device
+    (dt, pdh), dev = _main("dh", dh, 3), dh.device
     B, T, I = dh.shape
     if (gscale is None) != (uscale is None):
         raise ValueError("g and u are both coded or neither")
@@ -638,15 +673,14 @@ def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, 
         pg, pgs = _tensor("g", g, dh.shape, dh.dtype, dev), None
         pu, pus = _tensor("u", u, dh.shape, dh.dtype, dev), None
     else:
-        pg, pgs = _codes("g", g, gscale, dh.shape, dev)
-        pu, pus = _codes("u", u, uscale, dh.shape, dev)
-    if ws is None:
-        ws = _workspace(pyramid_scan_workspace_size(B, T, I), dev)
+        pg, pgs = _codes("g", g, gscale, dh, dev)
+        pu, pus = _codes("u", u, uscale, dh, dev)
+    ws, pws = _scan_workspace(ws, B, T, I, dev)
     _run("pyramid_scan_backward", dh, stream, B, T, I, dt, int(bool(reverse)), pg, pgs, pu, pus,
-         _tensor("lengths", lengths, (B,), torch.int32, dev), _check_saved(saved, B, T, I, dev),
-         _ptr(dh), _tensor("dhT", dhT, (B, I), torch.float32, dev),
+         _tensor("lengths", lengths, (B,), torch.int32, dev), _saved(saved, B, T, I, dev),
+         pdh, _tensor("dhT", dhT, (B, I), torch.float32, dev),
          _tensor("dg", dg, dh.shape, dh.dtype, dev), _tensor("du", du, dh.shape, dh.dtype, dev),
-         _tensor("dh0", dh0, (B, I), torch.float32, dev), *_bytes(ws, dev))
+         _tensor("dh0", dh0, (B, I), torch.float32, dev), *pws)
 
 
 def pyramid_checkpoint8_scales(n: int) -> int:
@@ -662,15 +696,15 @@ def checkpoint8_empty(x):
 
 def pyramid_checkpoint8_pack(x, q, scale, stream=None):
     """Codes q (x's shape, int8) and scales of x (float32 or bfloat16, any shape)."""
-    dt, px = _storage("x", x, None), _ptr(x)
-    pq, ps = _codes("q", q, scale, x.shape, x.device)
+    dt, px = _main("x", x, None)
+    pq, ps = _codes("q", q, scale, x, x.device)
     _run("pyramid_checkpoint8_pack", x, stream, x.numel(), dt, px, pq, ps)
 
 
 def pyramid_checkpoint8_unpack(q, scale, x, stream=None):
     """x (float32 or bfloat16, q's shape) = the values of a checkpoint."""
-    dt, px = _storage("x", x, None), _ptr(x)
-    pq, ps = _codes("q", q, scale, x.shape, x.device)
+    dt, px = _main("x", x, None)
+    pq, ps = _codes("q", q, scale, x, x.device)
     _run("pyramid_checkpoint8_unpack", x, stream, x.numel(), dt, pq, ps, px)
 
 

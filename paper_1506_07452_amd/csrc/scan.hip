@@ -11,7 +11,7 @@
 // computes the others again from g and u (in the storage type or from 8-bit
 // checkpoints), which costs 1/4 byte an element where reading h would cost 2
 // or 4.
-#include "code8.h"
+#include "rows.h"
 #include "sweep.h"
 #include "timing.h"
 
@@ -28,6 +28,8 @@ struct ScanArgs {
     int reverse;
     const int32_t *lengths;
     long long runs;                 // ceil(T / kRun)
+    long long across;               // workgroups across a sequence's channels; 0: 64 columns
+                                    // each, whatever sequences they belong to
 };
 
 // Chunks of a sequence (kRun positions for each wave of a workgroup) run at the
@@ -63,128 +65,159 @@ k_scan_chain_init(Chain ch, long long cols, const float *start)
     if (i0 == 0) *ch.ticket = 0;
 }
 
-// f and 1 - f of sigmoid's argument.
+// f and 1 - f of sigmoid's argument.  exp(-|g|) <= 1: nothing overflows, and
+// neither is a difference.
 __device__ inline void gate(float g, float &keep, float &take)
 {
-    const float e = __expf(-fabsf(g));
+    const float e = __builtin_amdgcn_exp2f(fabsf(g) * -1.44269504f);
     const float r = __builtin_amdgcn_rcpf(1.0f + e);
     const float small = e * r;
     keep = g < 0.0f ? small : r;
     take = g < 0.0f ? r : small;
 }
 
-template <typename T>
-__device__ inline float load_at(const T *x, const uint16_t *, long long i)
-{
-    return Store<T>::load(x, i);
-}
-__device__ inline float load_at(const int8_t *x, const uint16_t *scale, long long i)
-{
-    return (float)x[i] * bf16_to_f32(scale[i >> 6]);
-}
-
-// A lane's column: a channel i of sequence b.
+// A workgroup's 64 columns (channels of sequences) and a lane's among them.
+// Element (b, t, i) of the lane is element `base` + off + t I: base is the same
+// for the workgroup, so that addresses are a scalar pointer and a lane's 32-bit
+// offset (the host keeps offsets below 2^32 bytes, scan_plan).
 struct Column {
     bool has;                       // false past the last column (then a copy of it)
-    long long col, base, saved;     // base: element (b, 0, i); saved: state (b, 0, i)
+    long long base, saved, first;   // of the first column: element (b, 0, i), state (b, 0, i), column
+    uint32_t off, soff, coff;       // the lane's, from those
     long long n;                    // the sequence's length
 };
-__device__ inline Column column_of(const ScanArgs &a, long long col)
+__device__ inline Column column_of(const ScanArgs &a, int block, int lane)
 {
     Column c;
-    c.has = col < a.cols;
-    c.col = c.has ? col : a.cols - 1;
-    const long long b = c.col / a.I, i = c.col - b * a.I;
+    long long b;
+    uint32_t i, last;
+    if (a.across) {
+        b = block / a.across;
+        i = (uint32_t)(block - b * a.across) * 64;
+        last = (uint32_t)a.I - 1 - i;
+        c.first = b * a.I + i;
+    } else {
+        c.first = (long long)block * 64;
+        b = c.first / a.I;
+        i = (uint32_t)(c.first - b * a.I);
+        last = (uint32_t)min(a.cols - 1 - c.first, 63LL);
+    }
+    c.has = lane <= (int)min(last, 63u);
+    c.coff = min((uint32_t)lane, last);
+    const uint32_t at = i + c.coff, I = (uint32_t)a.I;
+    const uint32_t db = a.across ? 0 : at / I, di = at - db * I - i;
     c.base = b * a.T * a.I + i;
     c.saved = b * a.runs * a.I + i;
+    c.off = db * (uint32_t)(a.T * a.I) + di;
+    c.soff = db * (uint32_t)(a.runs * a.I) + di;
     c.n = a.T;
     if (a.lengths) {
-        const long long n = a.lengths[b];
+        const long long n = a.lengths[b + db];
         c.n = n < 0 ? 0 : n > a.T ? a.T : n;
     }
     return c;
 }
 
-// Elements of a run of positions s0 .. s0 + count - 1 (count <= kRun) of a column.
-// Positions past the sequence's length stand for the steps of the same number.
+// Element offset of a lane from a uniform one: 32 bits where all sequences have
+// the same length, else 64 (positions count from each sequence's end).
+template <bool RAGGED> struct Offset { typedef uint32_t type; };
+template <> struct Offset<true> { typedef long long type; };
+
+template <typename O>
+__device__ inline float get(const float *p, const uint16_t *, long long base, O off)
+{
+    return *(const float *)((const char *)(p + base) + (O)(off * 4));
+}
+template <typename O>
+__device__ inline float get(const uint16_t *p, const uint16_t *, long long base, O off)
+{
+    return bf16_to_f32(*(const uint16_t *)((const char *)(p + base) + (O)(off * 2)));
+}
+template <typename O>
+__device__ inline float get(const int8_t *q, const uint16_t *scale, long long base, O off)
+{
+    const O block = ((O)(base & (kCodeBlock - 1)) + off) >> 6;
+    return (float)*(const int8_t *)((const char *)(q + base) + off) *
+           bf16_to_f32(*(const uint16_t *)((const char *)(scale + (base >> 6)) + (O)(block * 2)));
+}
+template <typename O>
+__device__ inline void put(float *p, long long base, O off, float v)
+{
+    *(float *)((char *)(p + base) + (O)(off * 4)) = v;
+}
+template <typename O>
+__device__ inline void put(uint16_t *p, long long base, O off, float v)
+{
+    *(uint16_t *)((char *)(p + base) + (O)(off * 2)) = (uint16_t)pack_bf16(v, v);
+}
+
+// The elements of a run of positions s0 .. s0 + count - 1 of a column.  Positions
+// past a sequence's length stand for the steps of the same number.
 template <bool RAGGED>
 struct RunAt {
-    long long first, step, pad, I;
+    typedef typename Offset<RAGGED>::type O;
+    long long base, step;           // position k: base + k step, from the lane's `off`
+    O off;
+    long long pbase, pstep;         // the same for positions past the length
+    O poff;
     int live;                       // positions of the run that the sequence has
     __device__ RunAt(const ScanArgs &a, const Column &c, long long s0)
     {
-        I = a.I;
-        first = c.base + (a.reverse ? c.n - 1 - s0 : s0) * I;
-        step = a.reverse ? -I : I;
-        pad = c.base + s0 * I;
+        const long long end = RAGGED ? 0 : a.T - 1;
+        base = c.base + (a.reverse ? end - s0 : s0) * a.I;
+        step = a.reverse ? -a.I : a.I;
+        off = RAGGED && a.reverse ? (O)(c.off + (c.n - 1) * a.I) : (O)c.off;
+        pbase = c.base + s0 * a.I;
+        pstep = a.I;
+        poff = (O)c.off;
         const long long left = c.n - s0;
         live = left < 0 ? 0 : left > kRun ? kRun : (int)left;
     }
-    __device__ long long at(int k) const
+    // Position k where every lane has all of the run's 16.
+    template <typename X>
+    __device__ float load(const X *x, const uint16_t *scale, int k) const
     {
-        if (RAGGED) return k < live ? first + k * step : pad + k * I;
-        return first + k * step;
+        return get(x, scale, base + k * step, off);
+    }
+    template <typename T> __device__ void store(T *x, int k, float v) const
+    {
+        put(x, base + k * step, off, v);
+    }
+    // Position k of `count` > 0 that the tensor has, of which a sequence has `live`:
+    // `other` where it has not, read from some place that there is (a load under
+    // a condition would wait for the one before it), and 0 is stored.
+    template <typename X>
+    __device__ float load(const X *x, const uint16_t *scale, int k, int count, float other) const
+    {
+        const int j = k < count ? k : count - 1;
+        float v;
+        if (RAGGED) v = get(x, scale, 0, (O)(j < live ? base + j * step + off : pbase + j * pstep + poff));
+        else v = get(x, scale, base + j * step, off);
+        return k < count && k < live ? v : other;
+    }
+    template <typename T> __device__ void store(T *x, int k, int count, float v) const
+    {
+        if (k >= count) return;
+        if (RAGGED) put(x, 0, (O)(k < live ? base + k * step + off : pbase + k * pstep + poff), k < live ? v : 0.0f);
+        else put(x, base + k * step, off, v);
     }
 };
 
-// Folds (A, H) pairs lds[0 .. count - 1] over v in order.
-__device__ inline float fold(const float2 (*lds)[64], int count, int lane, float v)
+// Waits for a word of the chain to be written; false when it gave up.
+template <typename V>
+__device__ inline bool wait_word(const Chain &ch, const V *p, V empty, V &v)
 {
-    for (int w = 0; w < count; ++w) {
-        const float2 p = lds[w][lane];
-        v = fmaf(p.x, v, p.y);
-    }
-    return v;
-}
-
-// The state before chunk k of the lane's column, and the end state to the next
-// group where chunk k is a group's last.  (A, H): the chunk's aggregate.
-__device__ inline float chained(const Chain &ch, long long cols, long long col, bool has, int k,
-                                float A, float H)
-{
-    if (has) {
-        const uint64_t word = (uint64_t)float_bits(H) << 32 |
-                              (A != A ? 0x7fc00000u : float_bits(A));
-        __hip_atomic_store(&ch.agg[k * cols + col], word, __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-    }
-    const int g = k / kGroup, first = g * kGroup;
-    uint64_t w[kGroup];
-    uint32_t s = kEmptyState;
     for (int polls = 0;; ++polls) {
-        s = __hip_atomic_load(&ch.state[g * cols + col], __ATOMIC_RELAXED,
-                              __HIP_MEMORY_SCOPE_AGENT);
-        bool all = s != kEmptyState;
-#pragma unroll
-        for (int j = 0; j < kGroup - 1; ++j)
-            if (first + j < k) {
-                w[j] = __hip_atomic_load(&ch.agg[(first + j) * cols + col], __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_AGENT);
-                all = all && w[j] != kEmpty;
-            }
-        if (__all(all && ch.bias == 0)) break;
+        v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (__all(v != empty && ch.bias == 0)) return true;
         if (polls >= ch.spin) {
-            // gave up: NaN from here on
-            if (threadIdx.x == 0)
+            if ((threadIdx.x & 63) == 0)
                 __hip_atomic_fetch_or(ch.status, PLSTM_DEVICE_WAIT_GAVE_UP, __ATOMIC_RELAXED,
                                       __HIP_MEMORY_SCOPE_AGENT);
-            s = 0x7fc00000u;
-            break;
+            return false;
         }
         __builtin_amdgcn_s_sleep(1);
     }
-    float v = bits_float(s);
-#pragma unroll
-    for (int j = 0; j < kGroup - 1; ++j)
-        if (first + j < k) v = fmaf(bits_float((uint32_t)w[j]), v, bits_float((uint32_t)(w[j] >> 32)));
-    if (k - first == kGroup - 1 && has) {
-        const float e = fmaf(A, v, H);
-        if (k + 1 < ch.chunks)
-            __hip_atomic_store(&ch.state[(g + 1) * cols + col],
-                               e != e ? 0x7fc00000u : float_bits(e), __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-    }
-    return v;
 }
 
 // The next chunk of the chain: its number, and the workgroup's place across the columns.
@@ -194,89 +227,164 @@ __device__ inline void take_chunk(const Chain &ch, int &chunk, int &block)
     if (threadIdx.x == 0)
         ticket = __hip_atomic_fetch_add(ch.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    chunk = (int)(ticket / (uint32_t)ch.blocks);
-    block = (int)(ticket - (uint32_t)chunk * (uint32_t)ch.blocks);
+    const uint32_t t = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
+    chunk = (int)(t / (uint32_t)ch.blocks);
+    block = (int)(t - (uint32_t)chunk * (uint32_t)ch.blocks);
+}
+
+// What the waves of a workgroup give each other: (A, H) of their runs, and
+// (CHAIN) of the chunks before it in its group and the group's state.
+template <int W, bool CHAIN>
+struct Shared {
+    float2 part[CHAIN ? 1 : 2][W][64];      // two turns: one barrier a turn
+    float2 prev[CHAIN ? W : 1][64];
+    float start[64];
+};
+
+// The state before the wave's run, `carry` being the one before the workgroup's
+// first (CHAIN: taken from the chain); carry becomes the one after its last.
+// Every wave of the workgroup is here at once.
+template <int W, bool CHAIN>
+__device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &ch, long long cols,
+                                   const Column &c, int chunk, int wave, int lane, float A, float H,
+                                   float &carry)
+{
+    const float2 (*part)[64] = sh.part[CHAIN ? 0 : turn];
+    sh.part[CHAIN ? 0 : turn][wave][lane] = make_float2(A, H);
+    __syncthreads();
+    if (CHAIN) {
+        const int g = chunk / kGroup, first = g * kGroup;
+        if (wave == 0 && chunk + 1 < ch.chunks) {
+            float a = 1.0f, h = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float2 p = part[w][lane];
+                a *= p.x;
+                h = fmaf(p.x, h, p.y);
+            }
+            const uint64_t word = (uint64_t)float_bits(h) << 32 |
+                                  (a != a ? 0x7fc00000u : float_bits(a));
+            if (c.has)
+                __hip_atomic_store(ch.agg + (chunk * cols + c.first) + c.coff, word,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        // each wave takes its share of the chunks before
+        float a = 1.0f, h = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kGroup / W; ++j) {
+            const int k = first + wave * (kGroup / W) + j;
+            if (k >= chunk) break;
+            uint64_t w;
+            const bool ok = wait_word(ch, ch.agg + (k * cols + c.first) + c.coff, kEmpty, w);
+            const float wa = ok ? bits_float((uint32_t)w) : __builtin_nanf("");
+            a *= wa;
+            h = fmaf(wa, h, bits_float((uint32_t)(w >> 32)));
+        }
+        sh.prev[wave][lane] = make_float2(a, h);
+        if (wave == W - 1) {
+            uint32_t s;
+            const bool ok = wait_word(ch, ch.state + (g * cols + c.first) + c.coff, kEmptyState, s);
+            sh.start[lane] = ok ? bits_float(s) : __builtin_nanf("");
+        }
+        __syncthreads();
+        carry = sh.start[lane];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float2 p = sh.prev[w][lane];
+            carry = fmaf(p.x, carry, p.y);
+        }
+    }
+    float v = carry, at = carry;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const float2 p = part[w][lane];
+        at = w == wave ? v : at;
+        v = fmaf(p.x, v, p.y);
+    }
+    carry = v;
+    if (CHAIN && wave == 0 && (chunk + 1) % kGroup == 0 && chunk + 1 < ch.chunks && c.has)
+        __hip_atomic_store(ch.state + ((chunk + 1) / kGroup * cols + c.first) + c.coff,
+                           v != v ? 0x7fc00000u : float_bits(v), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    return at;
 }
 
 // A workgroup of W waves advances 64 columns by W runs of 16 positions at a
 // time, wave w holding run w in registers.  W = 1 walks its runs one after
 // another; with more, each wave folds its run to (A, H), and starts it again from
 // the state that the waves before it leave.  CHAIN: the workgroup has one chunk
-// of W runs and takes the state from the chain.
+// of W runs and takes the state from the chain.  Runs that every lane has in full
+// are loaded and stored without a condition.
 template <typename T, int W, bool RAGGED, bool CHAIN>
 __global__ void __launch_bounds__(64 * W)
 k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ u,
            const float *h0, T *__restrict__ h, float *hT, float *__restrict__ saved)
 {
-    __shared__ float2 lds[CHAIN ? 1 : 2][W > 1 ? W : 1][64];
-    __shared__ float start[64];
-    const int lane = threadIdx.x & 63, wave = W > 1 ? threadIdx.x / 64 : 0;
-    int chunk = 0, block = blockIdx.x;
+    __shared__ Shared<W, CHAIN> sh;
+    const int lane = threadIdx.x & 63;
+    const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    int chunk = 0, block = blockIdx.x, turn = 0;
     if (CHAIN) take_chunk(ch, chunk, block);
-    const Column c = column_of(a, (long long)block * 64 + lane);
-    float carry = !CHAIN && h0 ? h0[c.col] : 0.0f;
-    int turn = 0;
+    const Column c = column_of(a, block, lane);
+    float carry = !CHAIN && h0 ? h0[c.first + c.coff] : 0.0f;
     for (long long r0 = (long long)chunk * W; r0 < a.runs; r0 += W, turn ^= 1) {
         const long long run = r0 + wave, s0 = run * kRun;
         const int count = run < a.runs ? (int)min((long long)kRun, a.T - s0) : 0;
         const RunAt<RAGGED> at(a, c, s0);
+        const bool full = count == kRun && (!RAGGED || __all(at.live == kRun));
         float f[kRun], v[kRun];
-        if (count > 0) {
+        if (full) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
-                const long long e = at.at(k < count ? k : count - 1);
-                f[k] = Store<T>::load(g, e);
-                v[k] = Store<T>::load(u, e);
+                f[k] = at.load(g, nullptr, k);
+                v[k] = at.load(u, nullptr, k);
+            }
+        } else if (count > 0) {
+            // a position that is not there keeps the state: f = 1, nothing taken
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                f[k] = at.load(g, nullptr, k, count, __builtin_inff());
+                v[k] = at.load(u, nullptr, k, count, 0.0f);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                f[k] = __builtin_inff();
+                v[k] = 0.0f;
             }
         }
         float A = 1.0f, H = 0.0f;
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            float keep, take;
-            gate(f[k], keep, take);
-            const bool in = RAGGED ? k < at.live && k < count : k < count;
-            f[k] = in ? keep : 1.0f;
-            v[k] = in ? take * v[k] : 0.0f;
+            float take;
+            gate(f[k], f[k], take);
+            v[k] *= take;
             if (W > 1) {
                 A *= f[k];
                 H = fmaf(f[k], H, v[k]);
             }
         }
         float st = carry;
-        if (W > 1) {
-            lds[CHAIN ? 0 : turn][wave][lane] = make_float2(A, H);
-            __syncthreads();
-            const float2 (*parts)[64] = lds[CHAIN ? 0 : turn];
-            if (CHAIN) {
-                if (wave == 0) {
-                    float ca = 1.0f, cb = 0.0f;
-                    for (int w = 0; w < W; ++w) {
-                        const float2 p = parts[w][lane];
-                        ca *= p.x;
-                        cb = fmaf(p.x, cb, p.y);
-                    }
-                    start[lane] = chained(ch, a.cols, c.col, c.has, chunk, ca, cb);
-                }
-                __syncthreads();
-                carry = start[lane];
-            }
-            st = fold(parts, wave, lane, carry);
-        }
-        if (count > 0) {
-            if (saved && c.has) saved[c.saved + run * a.I] = st;
+        if constexpr (W > 1)
+            st = before_run(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
+        if (saved && count > 0 && c.has) put(saved, c.saved + run * a.I, c.soff, st);
+        if (full && c.has) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 st = fmaf(f[k], st, v[k]);
-                const bool in = !RAGGED || k < at.live;
-                if (k < count && c.has) Store<T>::store(h, at.at(k), in ? st : 0.0f);
+                at.store(h, k, st);
+            }
+        } else if (c.has) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                st = fmaf(f[k], st, v[k]);
+                at.store(h, k, count, st);
             }
         }
         if (W == 1) carry = st;
-        else if (!CHAIN) carry = fold(lds[turn] + wave, W - wave, lane, fold(lds[turn], wave, lane, carry));
-        else if (hT && c.has && run == a.runs - 1) hT[c.col] = st;
-        if (CHAIN) return;
+        if (CHAIN) break;
     }
-    if (hT && c.has && wave == 0) hT[c.col] = carry;
+    if (hT && c.has && wave == 0 && (!CHAIN || chunk == ch.chunks - 1)) hT[c.first + c.coff] = carry;
 }
 
 // As k_scan_fwd from the last run to the first: c, what later positions give a
@@ -289,86 +397,82 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
            const float *__restrict__ saved, const T *__restrict__ dh, const float *dhT,
            T *__restrict__ dg, T *__restrict__ du, float *dh0)
 {
-    __shared__ float2 lds[CHAIN ? 1 : 2][W > 1 ? W : 1][64];
-    __shared__ float start[64];
-    const int lane = threadIdx.x & 63, wave = W > 1 ? threadIdx.x / 64 : 0;
-    int chunk = 0, block = blockIdx.x;
+    __shared__ Shared<W, CHAIN> sh;
+    const int lane = threadIdx.x & 63;
+    const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    int chunk = 0, block = blockIdx.x, turn = 0;
     if (CHAIN) take_chunk(ch, chunk, block);
-    const Column c = column_of(a, (long long)block * 64 + lane);
-    float carry = !CHAIN && dhT ? dhT[c.col] : 0.0f;
-    int turn = 0;
+    const Column c = column_of(a, block, lane);
+    float carry = !CHAIN && dhT ? dhT[c.first + c.coff] : 0.0f;
     // wave 0 has the last run of a chunk; a chunk's runs may end before the first
     for (long long r0 = a.runs - 1 - (long long)chunk * W; r0 >= 0; r0 -= W, turn ^= 1) {
         const long long run = r0 - wave, s0 = run * kRun;
         const int count = run >= 0 ? (int)min((long long)kRun, a.T - s0) : 0;
         const RunAt<RAGGED> at(a, c, s0);
+        const bool full = count == kRun && (!RAGGED || __all(at.live == kRun));
         float f[kRun], k1[kRun], d[kRun], v[kRun];      // f, 1 - f, dh, h before - u
         float st = 0.0f;
-        if (count > 0) {
-            st = saved[c.saved + run * a.I];
+        if (count > 0) st = get(saved, nullptr, c.saved + run * a.I, c.soff);
+        if (full) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
-                const long long e = at.at(k < count ? k : count - 1);
-                f[k] = load_at(g, gscale, e);
-                v[k] = load_at(u, uscale, e);
-                d[k] = Store<T>::load(dh, e);
+                f[k] = at.load(g, gscale, k);
+                v[k] = at.load(u, uscale, k);
+                d[k] = at.load(dh, nullptr, k);
+            }
+        } else if (count > 0) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                f[k] = at.load(g, gscale, k, count, __builtin_inff());
+                v[k] = at.load(u, uscale, k, count, 0.0f);
+                d[k] = at.load(dh, nullptr, k, count, 0.0f);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                f[k] = __builtin_inff();
+                v[k] = d[k] = 0.0f;
             }
         }
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            const bool in = RAGGED ? k < at.live && k < count : k < count;
             gate(f[k], f[k], k1[k]);
             const float uk = v[k];
             v[k] = st - uk;
-            st = in ? fmaf(f[k], st, k1[k] * uk) : st;
-            f[k] = in ? f[k] : 1.0f;
-            d[k] = in ? d[k] : 0.0f;
+            st = fmaf(f[k], st, k1[k] * uk);
         }
         float cin = carry;
-        if (W > 1) {
+        if constexpr (W > 1) {
             float A = 1.0f, H = 0.0f;
 #pragma unroll
             for (int k = kRun - 1; k >= 0; --k) {
                 A *= f[k];
                 H = f[k] * (d[k] + H);
             }
-            lds[CHAIN ? 0 : turn][wave][lane] = make_float2(A, H);
-            __syncthreads();
-            const float2 (*parts)[64] = lds[CHAIN ? 0 : turn];
-            if (CHAIN) {
-                if (wave == 0) {
-                    float ca = 1.0f, cb = 0.0f;
-                    for (int w = 0; w < W; ++w) {
-                        const float2 p = parts[w][lane];
-                        ca *= p.x;
-                        cb = fmaf(p.x, cb, p.y);
-                    }
-                    start[lane] = chained(ch, a.cols, c.col, c.has, chunk, ca, cb);
-                }
-                __syncthreads();
-                carry = start[lane];
-            }
-            cin = fold(parts, wave, lane, carry);
+            cin = before_run(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
         }
-        if (count > 0) {
+        if (full && c.has) {
 #pragma unroll
             for (int k = kRun - 1; k >= 0; --k) {
-                const bool in = !RAGGED || k < at.live;
-                const float G = d[k] + cin;
-                const float vu = G * k1[k];
-                if (k < count && c.has) {
-                    Store<T>::store(dg, at.at(k), in ? vu * f[k] * v[k] : 0.0f);
-                    Store<T>::store(du, at.at(k), in ? vu : 0.0f);
-                }
+                const float G = d[k] + cin, vu = G * k1[k];
                 cin = f[k] * G;
+                at.store(dg, k, vu * f[k] * v[k]);
+                at.store(du, k, vu);
+            }
+        } else if (c.has) {
+#pragma unroll
+            for (int k = kRun - 1; k >= 0; --k) {
+                const float G = d[k] + cin, vu = G * k1[k];
+                cin = f[k] * G;
+                at.store(dg, k, count, vu * f[k] * v[k]);
+                at.store(du, k, count, vu);
             }
         }
         if (W == 1) carry = cin;
-        else if (!CHAIN) carry = fold(lds[turn] + wave, W - wave, lane, fold(lds[turn], wave, lane, carry));
-        else if (dh0 && c.has && run == 0) dh0[c.col] = cin;
-        if (CHAIN) return;
+        if (CHAIN) break;
     }
-    if (dh0 && c.has && wave == 0) dh0[c.col] = carry;
+    if (dh0 && c.has && wave == 0 && (!CHAIN || chunk == ch.chunks - 1))
+        dh0[c.first + c.coff] = carry;
 }
 
 int check_scan(int64_t B, int64_t T, int64_t I, int32_t dtype)
@@ -385,6 +489,7 @@ constexpr int kWaves = 8;           // of a workgroup with more than one
 // How a call is spread: waves of a workgroup, and whether chunks are chained.
 struct Plan {
     ScanArgs a;
+    long long blocks;               // workgroups across the columns
     int waves;
     Chain ch;                       // chunks 0: none
     size_t ws;
@@ -393,8 +498,16 @@ struct Plan {
 Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *lengths, void *ws)
 {
     Plan p{};
-    p.a = ScanArgs{T, I, B * I, reverse, lengths, (T + kRun - 1) / kRun};
-    const long long blocks = (p.a.cols + 63) / 64;
+    p.a = ScanArgs{T, I, B * I, reverse, lengths, (T + kRun - 1) / kRun, 0};
+    long long blocks = (p.a.cols + 63) / 64;
+    // a lane's offset from its workgroup's first column, in bytes of fp32: the
+    // sequences that 64 columns touch.  Past 32 bits columns do not share workgroups
+    // across sequences.
+    if (B > 1 && (double)(63 / I + 1) * T * I >= (double)(1 << 30)) {
+        p.a.across = (I + 63) / 64;
+        blocks = B * p.a.across;
+    }
+    p.blocks = blocks;
     const long long chunks = (p.a.runs + kWaves - 1) / kWaves;
     p.waves = blocks >= 1024 || p.a.runs <= 2 ? 1 : kWaves;
     Carve cv(ws);
@@ -427,8 +540,7 @@ template <typename T, int W, bool RAGGED, bool CHAIN>
 void launch_fwd(const Plan &p, const void *g, const void *u, const void *h0, void *h, void *hT,
                 void *saved, hipStream_t st)
 {
-    const long long blocks = (p.a.cols + 63) / 64;
-    k_scan_fwd<T, W, RAGGED, CHAIN><<<(unsigned)(CHAIN ? blocks * p.ch.chunks : blocks), 64 * W, 0, st>>>(
+    k_scan_fwd<T, W, RAGGED, CHAIN><<<(unsigned)(CHAIN ? p.blocks * p.ch.chunks : p.blocks), 64 * W, 0, st>>>(
         p.a, p.ch, (const T *)g, (const T *)u, (const float *)h0, (T *)h, (float *)hT,
         (float *)saved);
 }
@@ -455,8 +567,7 @@ void launch_bwd(const Plan &p, const void *g, const void *gscale, const void *u,
                 const void *uscale, const void *saved, const void *dh, const void *dhT, void *dg,
                 void *du, void *dh0, hipStream_t st)
 {
-    const long long blocks = (p.a.cols + 63) / 64;
-    k_scan_bwd<T, X, W, RAGGED, CHAIN><<<(unsigned)(CHAIN ? blocks * p.ch.chunks : blocks), 64 * W, 0, st>>>(
+    k_scan_bwd<T, X, W, RAGGED, CHAIN><<<(unsigned)(CHAIN ? p.blocks * p.ch.chunks : p.blocks), 64 * W, 0, st>>>(
         p.a, p.ch, (const X *)g, (const uint16_t *)gscale, (const X *)u, (const uint16_t *)uscale,
         (const float *)saved, (const T *)dh, (const float *)dhT, (T *)dg, (T *)du, (float *)dh0);
 }

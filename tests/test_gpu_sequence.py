@@ -586,3 +586,34 @@ def test_refusals_of_the_binding():
     with pytest.raises(ValueError):
         P.pyramid_checkpoint8_pack(x, torch.zeros((4, 8), dtype=torch.int8, device=DEV),
                                    torch.zeros(2, dtype=BF16, device=DEV))
+
+
+def test_scan_sequences_far_apart():
+    """Sequences too long for 32-bit offsets between them: columns of two of
+    them in one wave (odd I), the last steps of each."""
+    B, T, I = 3, (1 << 20) + 33, 517
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    g, u = (torch.empty((B, T, I), dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
+    lengths = [T, T - 5000, T - 77]
+    ln = torch.tensor(lengths, dtype=torch.int32).to(DEV)
+    say("scan far apart")
+    for reverse in (False, True):
+        for n in (None, ln):
+            h, dg, du = (torch.empty_like(g) for _ in range(3))
+            saved = torch.empty(P.pyramid_scan_saved_size(B, T, I), dtype=torch.uint8, device=DEV)
+            P.pyramid_scan_forward(g, u, h, reverse, n, saved=saved)
+            P.pyramid_scan_backward(g, u, saved, u, dg, du, reverse, n)
+            cols = [0, 1, I - 1]
+            for b in range(B):
+                end = T if n is None else lengths[b]
+                # the sweep's last 200 positions; 100 steps before them are forgotten to 2^-64
+                at = slice(0, 200) if reverse else slice(end - 200, end)
+                gl, ul = (v[b:b + 1, at][:, :, cols].cpu() for v in (g, u))
+                rh, e, _, _, before, eb = R.scan_forward(gl, ul, reverse, None, None)
+                (rg, eg), (ru, eu), _ = R.scan_backward(gl, ul, before, eb, ul, reverse, None, None)
+                keep = slice(0, 100) if reverse else slice(100, 200)
+                for name, got, ref, err in (("h", h, rh, e), ("dg", dg, rg, eg), ("du", du, ru, eu)):
+                    near(name, got[b:b + 1, at][:, :, cols].cpu()[:, keep], ref[:, keep],
+                         R.rounded(ref, err, BF16)[:, keep])
+                if end < T:
+                    assert not h[b, end:].any() and not dg[b, end:].any() and not du[b, end:].any()
