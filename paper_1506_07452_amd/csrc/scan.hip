@@ -82,6 +82,7 @@ __device__ inline void gate(float g, float &keep, float &take)
 // offset (the host keeps offsets below 2^32 bytes, scan_plan).
 struct Column {
     bool has;                       // false past the last column (then a copy of it)
+    bool one;                       // all columns of the workgroup are of one sequence
     long long base, saved, first;   // of the first column: element (b, 0, i), state (b, 0, i), column
     uint32_t off, soff, coff;       // the lane's, from those
     long long n;                    // the sequence's length
@@ -92,17 +93,18 @@ __device__ inline Column column_of(const ScanArgs &a, int block, int lane)
     long long b;
     uint32_t i, last;
     if (a.across) {
-        b = block / a.across;
+        b = (uint32_t)block / (uint32_t)a.across;
         i = (uint32_t)(block - b * a.across) * 64;
         last = (uint32_t)a.I - 1 - i;
         c.first = b * a.I + i;
     } else {
         c.first = (long long)block * 64;
-        b = c.first / a.I;
+        b = (uint32_t)c.first / (uint32_t)a.I;
         i = (uint32_t)(c.first - b * a.I);
         last = (uint32_t)min(a.cols - 1 - c.first, 63LL);
     }
     c.has = lane <= (int)min(last, 63u);
+    c.one = i + min(last, 63u) < (uint32_t)a.I;
     c.coff = min((uint32_t)lane, last);
     const uint32_t at = i + c.coff, I = (uint32_t)a.I;
     const uint32_t db = a.across ? 0 : at / I, di = at - db * I - i;
@@ -123,23 +125,61 @@ __device__ inline Column column_of(const ScanArgs &a, int block, int lane)
 template <bool RAGGED> struct Offset { typedef uint32_t type; };
 template <> struct Offset<true> { typedef long long type; };
 
+// Loads give raw bits.
 template <typename O>
-__device__ inline float get(const float *p, const uint16_t *, long long base, O off)
+__device__ inline uint32_t get(const float *p, long long base, O off)
 {
-    return *(const float *)((const char *)(p + base) + (O)(off * 4));
+    return *(const uint32_t *)((const char *)(p + base) + (O)(off * 4));
 }
 template <typename O>
-__device__ inline float get(const uint16_t *p, const uint16_t *, long long base, O off)
+__device__ inline uint32_t get(const uint16_t *p, long long base, O off)
 {
-    return bf16_to_f32(*(const uint16_t *)((const char *)(p + base) + (O)(off * 2)));
+    return *(const uint16_t *)((const char *)(p + base) + (O)(off * 2));
 }
 template <typename O>
-__device__ inline float get(const int8_t *q, const uint16_t *scale, long long base, O off)
+__device__ inline uint32_t get(const int8_t *p, long long base, O off)
+{
+    return (uint32_t)(int)*(const int8_t *)((const char *)(p + base) + off);
+}
+template <typename X> __device__ inline float value(uint32_t raw);
+template <> __device__ inline float value<float>(uint32_t raw) { return bits_float(raw); }
+template <> __device__ inline float value<uint16_t>(uint32_t raw) { return bits_float(raw << 16); }
+template <> __device__ inline float value<int8_t>(uint32_t raw) { return (float)(int)raw; }
+// All loads so far are issued before anything that follows: left to itself the
+// scheduler converts codes as they come, and a run waits sixteen times.
+__device__ inline void loads_issued() { __builtin_amdgcn_sched_barrier(0); }
+
+// Raw scale of a code.
+template <typename O>
+__device__ inline uint32_t get_scale(const uint16_t *scale, long long base, O off)
 {
     const O block = ((O)(base & (kCodeBlock - 1)) + off) >> 6;
-    return (float)*(const int8_t *)((const char *)(q + base) + off) *
-           bf16_to_f32(*(const uint16_t *)((const char *)(scale + (base >> 6)) + (O)(block * 2)));
+    return *(const uint16_t *)((const char *)(scale + (base >> 6)) + (O)(block * 2));
 }
+
+// Scales of a run of a coded tensor where a workgroup's columns are of one
+// sequence: a position's 64 elements, consecutive from `first` + k step, lie in two blocks
+// at most.  Lane k has the scale of the first one of position k, lane 16 + k of
+// the second: one load instead of one a position.
+struct RunScales {
+    uint32_t s;
+    long long first, step;
+    __device__ RunScales(const uint16_t *scale, long long blocks, long long first_, long long step_,
+                         int lane)
+        : first(first_), step(step_)
+    {
+        const long long b = ((first + (lane & 15) * step) >> 6) + (lane >> 4 & 1);
+        s = scale[b < blocks ? b : blocks - 1];
+    }
+    __device__ float of(int k, int lane) const
+    {
+        const uint32_t s0 = (uint32_t)__builtin_amdgcn_readlane((int)s, k);
+        const uint32_t s1 = (uint32_t)__builtin_amdgcn_readlane((int)s, 16 + k);
+        const int turn = kCodeBlock - (int)((first + k * step) & (kCodeBlock - 1));
+        return bits_float((lane < turn ? s0 : s1) << 16);
+    }
+};
+
 template <typename O>
 __device__ inline void put(float *p, long long base, O off, float v)
 {
@@ -173,33 +213,34 @@ struct RunAt {
         const long long left = c.n - s0;
         live = left < 0 ? 0 : left > kRun ? kRun : (int)left;
     }
-    // Position k where every lane has all of the run's 16.
-    template <typename X>
-    __device__ float load(const X *x, const uint16_t *scale, int k) const
+    // Where position k is, and how far the lane from there: of a run that every lane
+    // has in full, and of any (`count` > 0 positions are the tensor's, `live` of
+    // them the sequence's; others stand for some place that there is).
+    __device__ long long from(int k) const { return base + k * step; }
+    __device__ void any(int k, int count, long long &b, O &o) const
     {
-        return get(x, scale, base + k * step, off);
+        const int j = k < count ? k : count - 1;
+        if (RAGGED) {
+            b = 0;
+            o = (O)(j < live ? base + j * step + off : pbase + j * pstep + poff);
+        } else {
+            b = base + j * step;
+            o = off;
+        }
     }
+    __device__ bool has(int k, int count) const { return k < count && k < live; }
     template <typename T> __device__ void store(T *x, int k, float v) const
     {
         put(x, base + k * step, off, v);
     }
-    // Position k of `count` > 0 that the tensor has, of which a sequence has `live`:
-    // `other` where it has not, read from some place that there is (a load under
-    // a condition would wait for the one before it), and 0 is stored.
-    template <typename X>
-    __device__ float load(const X *x, const uint16_t *scale, int k, int count, float other) const
-    {
-        const int j = k < count ? k : count - 1;
-        float v;
-        if (RAGGED) v = get(x, scale, 0, (O)(j < live ? base + j * step + off : pbase + j * pstep + poff));
-        else v = get(x, scale, base + j * step, off);
-        return k < count && k < live ? v : other;
-    }
+    // 0 where the sequence has no position k
     template <typename T> __device__ void store(T *x, int k, int count, float v) const
     {
         if (k >= count) return;
-        if (RAGGED) put(x, 0, (O)(k < live ? base + k * step + off : pbase + k * pstep + poff), k < live ? v : 0.0f);
-        else put(x, base + k * step, off, v);
+        long long b;
+        O o;
+        any(k, count, b, o);
+        put(x, b, o, k < live ? v : 0.0f);
     }
 };
 
@@ -336,21 +377,26 @@ k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ 
         if (full) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
-                f[k] = at.load(g, nullptr, k);
-                v[k] = at.load(u, nullptr, k);
-            }
-        } else if (count > 0) {
-            // a position that is not there keeps the state: f = 1, nothing taken
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                f[k] = at.load(g, nullptr, k, count, __builtin_inff());
-                v[k] = at.load(u, nullptr, k, count, 0.0f);
+                f[k] = value<T>(get(g, at.from(k), at.off));
+                v[k] = value<T>(get(u, at.from(k), at.off));
             }
         } else {
+            // a position that is not there keeps the state: f = 1, nothing taken
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 f[k] = __builtin_inff();
                 v[k] = 0.0f;
+            }
+            if (count > 0) {
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) {
+                    long long b;
+                    typename RunAt<RAGGED>::O o;
+                    at.any(k, count, b, o);
+                    const float fk = value<T>(get(g, b, o)), vk = value<T>(get(u, b, o));
+                    f[k] = at.has(k, count) ? fk : __builtin_inff();
+                    v[k] = at.has(k, count) ? vk : 0.0f;
+                }
             }
         }
         float A = 1.0f, H = 0.0f;
@@ -387,6 +433,51 @@ k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ 
     if (hT && c.has && wave == 0 && (!CHAIN || chunk == ch.chunks - 1)) hT[c.first + c.coff] = carry;
 }
 
+// g and u of a full run from their codes.
+template <bool RAGGED>
+__device__ inline void coded_run(const ScanArgs &a, const RunAt<RAGGED> &at, const Column &c,
+                                 int lane, const int8_t *g, const uint16_t *gscale,
+                                 const int8_t *u, const uint16_t *uscale, float *f, float *v)
+{
+    uint32_t rg[kRun], ru[kRun];
+    if (c.one) {
+        // the lanes of a sequence are as far from its end
+        const long long first =
+            at.base + (RAGGED ? (long long)__builtin_amdgcn_readfirstlane((int)((long long)at.off >> 32)) << 32 |
+                                    (uint32_t)__builtin_amdgcn_readfirstlane((int)at.off)
+                              : 0);
+        const long long blocks = (a.cols * a.T + kCodeBlock - 1) / kCodeBlock;
+        const RunScales sg(gscale, blocks, first, at.step, lane);
+        const RunScales su(uscale, blocks, first, at.step, lane);
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            rg[k] = get(g, at.from(k), at.off);
+            ru[k] = get(u, at.from(k), at.off);
+        }
+        loads_issued();
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            f[k] = value<int8_t>(rg[k]) * sg.of(k, lane);
+            v[k] = value<int8_t>(ru[k]) * su.of(k, lane);
+        }
+    } else {
+        uint32_t sg[kRun], su[kRun];
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            rg[k] = get(g, at.from(k), at.off);
+            ru[k] = get(u, at.from(k), at.off);
+            sg[k] = get_scale(gscale, at.from(k), at.off);
+            su[k] = get_scale(uscale, at.from(k), at.off);
+        }
+        loads_issued();
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            f[k] = value<int8_t>(rg[k]) * value<uint16_t>(sg[k]);
+            v[k] = value<int8_t>(ru[k]) * value<uint16_t>(su[k]);
+        }
+    }
+}
+
 // As k_scan_fwd from the last run to the first: c, what later positions give a
 // position's G, goes through a run as c -> A c + H.  The states inside the run
 // come from the one kept before it.
@@ -397,6 +488,7 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
            const float *__restrict__ saved, const T *__restrict__ dh, const float *dhT,
            T *__restrict__ dg, T *__restrict__ du, float *dh0)
 {
+    constexpr bool coded = sizeof(X) == 1;
     __shared__ Shared<W, CHAIN> sh;
     const int lane = threadIdx.x & 63;
     const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
@@ -412,26 +504,41 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
         const bool full = count == kRun && (!RAGGED || __all(at.live == kRun));
         float f[kRun], k1[kRun], d[kRun], v[kRun];      // f, 1 - f, dh, h before - u
         float st = 0.0f;
-        if (count > 0) st = get(saved, nullptr, c.saved + run * a.I, c.soff);
+        if (count > 0) st = value<float>(get(saved, c.saved + run * a.I, c.soff));
         if (full) {
+            if constexpr (coded) {
+                coded_run(a, at, c, lane, g, gscale, u, uscale, f, v);
+            } else {
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                f[k] = at.load(g, gscale, k);
-                v[k] = at.load(u, uscale, k);
-                d[k] = at.load(dh, nullptr, k);
+                for (int k = 0; k < kRun; ++k) {
+                    f[k] = value<X>(get(g, at.from(k), at.off));
+                    v[k] = value<X>(get(u, at.from(k), at.off));
+                }
             }
-        } else if (count > 0) {
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                f[k] = at.load(g, gscale, k, count, __builtin_inff());
-                v[k] = at.load(u, uscale, k, count, 0.0f);
-                d[k] = at.load(dh, nullptr, k, count, 0.0f);
-            }
+            for (int k = 0; k < kRun; ++k) d[k] = value<T>(get(dh, at.from(k), at.off));
         } else {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 f[k] = __builtin_inff();
                 v[k] = d[k] = 0.0f;
+            }
+            if (count > 0) {
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) {
+                    long long b;
+                    typename RunAt<RAGGED>::O o;
+                    at.any(k, count, b, o);
+                    float fk = value<X>(get(g, b, o)), vk = value<X>(get(u, b, o));
+                    const float dk = value<T>(get(dh, b, o));
+                    if constexpr (coded) {
+                        fk *= value<uint16_t>(get_scale(gscale, b, o));
+                        vk *= value<uint16_t>(get_scale(uscale, b, o));
+                    }
+                    f[k] = at.has(k, count) ? fk : __builtin_inff();
+                    v[k] = at.has(k, count) ? vk : 0.0f;
+                    d[k] = at.has(k, count) ? dk : 0.0f;
+                }
             }
         }
 #pragma unroll
@@ -484,7 +591,7 @@ int check_scan(int64_t B, int64_t T, int64_t I, int32_t dtype)
     return PLSTM_OK;
 }
 
-constexpr int kWaves = 8;           // of a workgroup with more than one
+constexpr int kWaves = 8, kFewWaves = 4;    // of a workgroup that shares a column's runs
 
 // How a call is spread: waves of a workgroup, and whether chunks are chained.
 struct Plan {
@@ -509,9 +616,9 @@ Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *
     }
     p.blocks = blocks;
     const long long chunks = (p.a.runs + kWaves - 1) / kWaves;
-    p.waves = blocks >= 1024 || p.a.runs <= 2 ? 1 : kWaves;
+    p.waves = p.a.runs == 1 ? 1 : p.a.runs <= kFewWaves ? kFewWaves : kWaves;
     Carve cv(ws);
-    if (p.waves > 1 && chunks > 1 && blocks < 256 && chunks * blocks <= (1 << 21)) {
+    if (chunks > 1 && blocks < 256 && chunks * blocks <= (1 << 21)) {
         p.ch.agg = cv.take<uint64_t>(chunks * p.a.cols);
         p.ch.state = cv.take<uint32_t>((chunks + kGroup - 1) / kGroup * p.a.cols);
         p.ch.ticket = cv.take<uint32_t>(1);
@@ -553,8 +660,10 @@ int scan_forward(Plan &p, const void *g, const void *u, const void *h0, void *h,
         const int rc = start_chain(p, (const float *)h0, st);
         if (rc != PLSTM_OK) return rc;
         launch_fwd<T, kWaves, RAGGED, true>(p, g, u, h0, h, hT, saved, st);
-    } else if (p.waves > 1) {
+    } else if (p.waves == kWaves) {
         launch_fwd<T, kWaves, RAGGED, false>(p, g, u, h0, h, hT, saved, st);
+    } else if (p.waves == kFewWaves) {
+        launch_fwd<T, kFewWaves, RAGGED, false>(p, g, u, h0, h, hT, saved, st);
     } else {
         launch_fwd<T, 1, RAGGED, false>(p, g, u, h0, h, hT, saved, st);
     }
@@ -581,8 +690,10 @@ int scan_backward(Plan &p, const void *g, const void *gscale, const void *u, con
         const int rc = start_chain(p, (const float *)dhT, st);
         if (rc != PLSTM_OK) return rc;
         launch_bwd<T, X, kWaves, RAGGED, true>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
-    } else if (p.waves > 1) {
+    } else if (p.waves == kWaves) {
         launch_bwd<T, X, kWaves, RAGGED, false>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
+    } else if (p.waves == kFewWaves) {
+        launch_bwd<T, X, kFewWaves, RAGGED, false>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
     } else {
         launch_bwd<T, X, 1, RAGGED, false>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
     }
