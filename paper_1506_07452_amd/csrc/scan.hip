@@ -19,7 +19,7 @@ namespace plstm {
 namespace {
 
 constexpr int kRun = 16;            // positions between kept states, and of a wave's run
-constexpr int kGroup = 16;          // chunks between chained states
+constexpr int kGroup = 16;          // chunks between chained states, at least
 constexpr uint64_t kEmpty = ~0ull;  // a word that its chunk has not written
 constexpr uint32_t kEmptyState = ~0u;
 
@@ -35,19 +35,20 @@ struct ScanArgs {
 // Chunks of a sequence (kRun positions for each wave of a workgroup) run at the
 // same time and hand the state on through memory:
 //   agg [chunk][cols]   (A, H) of a chunk: its last state is A (state before) + H
-//   state [group][cols] the state before every kGroup-th chunk
+//   state [group][cols] the state before every group of chunks
 // A word is written whole, so whoever finds it other than empty has it all: no
 // flag, no fence.  A chunk publishes its aggregate as soon as it has its inputs;
 // it then needs its group's state and the aggregates of the chunks before it in
 // the group, always folded in the same order, so results do not depend on which
-// chunk was faster.  Only the last chunk of a group waits on a chain, one link
-// per kGroup chunks.
+// chunk was faster.  Only the last chunk of a group waits on a chain, whose links
+// take about 2 us each.
 struct Chain {
     uint64_t *agg;
     uint32_t *state;
     uint32_t *ticket;               // chunks are taken in order: whoever waits, waits on started ones
     int *status;                    // device status word
     int chunks, blocks;             // chunks of a sequence, workgroups across the columns
+    int group;                      // chunks of a group
     int spin, bias;                 // polls before a wait gives up; test mode
 };
 
@@ -56,7 +57,7 @@ k_scan_chain_init(Chain ch, long long cols, const float *start)
 {
     const long long i0 = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long stride = (long long)gridDim.x * 256;
-    const long long na = ch.chunks * cols, ns = (ch.chunks + kGroup - 1) / kGroup * cols;
+    const long long na = ch.chunks * cols, ns = (ch.chunks + ch.group - 1) / ch.group * cols;
     for (long long i = i0; i < na; i += stride) ch.agg[i] = kEmpty;
     for (long long i = i0; i < ns; i += stride) {
         const float v = i < cols && start ? start[i] : 0.0f;
@@ -294,7 +295,7 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
     sh.part[CHAIN ? 0 : turn][wave][lane] = make_float2(A, H);
     __syncthreads();
     if (CHAIN) {
-        const int g = chunk / kGroup, first = g * kGroup;
+        const int g = chunk / ch.group, first = g * ch.group, share = ch.group / W;
         if (wave == 0 && chunk + 1 < ch.chunks) {
             float a = 1.0f, h = 0.0f;
 #pragma unroll
@@ -311,10 +312,7 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
         }
         // each wave takes its share of the chunks before
         float a = 1.0f, h = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kGroup / W; ++j) {
-            const int k = first + wave * (kGroup / W) + j;
-            if (k >= chunk) break;
+        for (int k = first + wave * share; k < min(first + (wave + 1) * share, chunk); ++k) {
             uint64_t w;
             const bool ok = wait_word(ch, ch.agg + (k * cols + c.first) + c.coff, kEmpty, w);
             const float wa = ok ? bits_float((uint32_t)w) : __builtin_nanf("");
@@ -343,8 +341,8 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
         v = fmaf(p.x, v, p.y);
     }
     carry = v;
-    if (CHAIN && wave == 0 && (chunk + 1) % kGroup == 0 && chunk + 1 < ch.chunks && c.has)
-        __hip_atomic_store(ch.state + ((chunk + 1) / kGroup * cols + c.first) + c.coff,
+    if (CHAIN && wave == 0 && (chunk + 1) % ch.group == 0 && chunk + 1 < ch.chunks && c.has)
+        __hip_atomic_store(ch.state + ((chunk + 1) / ch.group * cols + c.first) + c.coff,
                            v != v ? 0x7fc00000u : float_bits(v), __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);
     return at;
@@ -591,7 +589,17 @@ int check_scan(int64_t B, int64_t T, int64_t I, int32_t dtype)
     return PLSTM_OK;
 }
 
-constexpr int kWaves = 8, kFewWaves = 4;    // of a workgroup that shares a column's runs
+// Waves of a workgroup by the runs of a sequence: one for a single run, four up to
+// four, else eight (training along x of a 48 x 240 x 240 volume, fp32, 15 runs: 305 us with
+// one, 286 with eight; 256 sequences of 4 runs of 2048 channels 257 with one, 212 with four).
+constexpr int kWaves = 8, kFewWaves = 4;
+// Waves of a chained chunk of the forward: sixteen, so half the links, and one
+// workgroup a CU (bf16, 16384 steps of 1024 channels: 31 us; with eight, four
+// workgroups a CU, 39).  The backward's registers do not leave room for them.
+constexpr int kChainWaves = 16;
+// Columns from which a card is filled without chains: at 16384 (fp32, eight sequences of
+// 2048 steps of 2048 channels) 88 us, 97 chained; at 4096 189 and 93.
+constexpr long long kChainCols = 16384;
 
 // How a call is spread: waves of a workgroup, and whether chunks are chained.
 struct Plan {
@@ -602,28 +610,31 @@ struct Plan {
     size_t ws;
 };
 
-Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *lengths, void *ws)
+Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *lengths, void *ws,
+               int chain_waves = kWaves)
 {
     Plan p{};
     p.a = ScanArgs{T, I, B * I, reverse, lengths, (T + kRun - 1) / kRun, 0};
-    long long blocks = (p.a.cols + 63) / 64;
+    p.blocks = (p.a.cols + 63) / 64;
     // a lane's offset from its workgroup's first column, in bytes of fp32: the
     // sequences that 64 columns touch.  Past 32 bits columns do not share workgroups
     // across sequences.
     if (B > 1 && (double)(63 / I + 1) * T * I >= (double)(1 << 30)) {
         p.a.across = (I + 63) / 64;
-        blocks = B * p.a.across;
+        p.blocks = B * p.a.across;
     }
-    p.blocks = blocks;
-    const long long chunks = (p.a.runs + kWaves - 1) / kWaves;
+    const long long chunks = (p.a.runs + chain_waves - 1) / chain_waves;
     p.waves = p.a.runs == 1 ? 1 : p.a.runs <= kFewWaves ? kFewWaves : kWaves;
     Carve cv(ws);
-    if (chunks > 1 && blocks < 256 && chunks * blocks <= (1 << 21)) {
+    if (chunks > 1 && p.a.cols < kChainCols && chunks * p.blocks <= (1 << 21)) {
         p.ch.agg = cv.take<uint64_t>(chunks * p.a.cols);
         p.ch.state = cv.take<uint32_t>((chunks + kGroup - 1) / kGroup * p.a.cols);
         p.ch.ticket = cv.take<uint32_t>(1);
         p.ch.chunks = (int)chunks;
-        p.ch.blocks = (int)blocks;
+        p.ch.blocks = (int)p.blocks;
+        // where links would take longer than the data, twice as many chunks a link
+        // (bf16, 65536 steps of 256 channels, eight waves: 72 -> 50 us)
+        p.ch.group = p.a.cols <= 512 ? 2 * kGroup : kGroup;
         p.ch.spin = g_wait_spin_limit;
         p.ch.bias = g_wait_bias;
     }
@@ -659,7 +670,7 @@ int scan_forward(Plan &p, const void *g, const void *u, const void *h0, void *h,
     if (p.ch.chunks) {
         const int rc = start_chain(p, (const float *)h0, st);
         if (rc != PLSTM_OK) return rc;
-        launch_fwd<T, kWaves, RAGGED, true>(p, g, u, h0, h, hT, saved, st);
+        launch_fwd<T, kChainWaves, RAGGED, true>(p, g, u, h0, h, hT, saved, st);
     } else if (p.waves == kWaves) {
         launch_fwd<T, kWaves, RAGGED, false>(p, g, u, h0, h, hT, saved, st);
     } else if (p.waves == kFewWaves) {
@@ -733,7 +744,7 @@ int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t
         return PLSTM_EINVAL;
     if (ws_bytes < pyramid_scan_workspace_size(B, T, I)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    Plan p = scan_plan(B, T, I, reverse, lengths, ws);
+    Plan p = scan_plan(B, T, I, reverse, lengths, ws, kChainWaves);
     timing_begin("scan_fwd", st);
     rc = dtype == PLSTM_F32
              ? (lengths ? scan_forward<float, true> : scan_forward<float, false>)(p, g, u, h0, h, hT,

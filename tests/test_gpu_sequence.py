@@ -588,10 +588,11 @@ def test_refusals_of_the_binding():
                                    torch.zeros(2, dtype=BF16, device=DEV))
 
 
-def test_scan_sequences_far_apart():
-    """Sequences too long for 32-bit offsets between them: columns of two of
-    them in one wave (odd I), the last steps of each."""
-    B, T, I = 3, (1 << 20) + 33, 517
+@pytest.mark.parametrize("I", [517, 514])
+def test_scan_sequences_far_apart(I):
+    """Sequences too long for 32-bit offsets between them, whose columns would
+    share a wave: the last steps of each."""
+    B, T = 3, (1 << 20) + 33
     gen = torch.Generator(device=DEV).manual_seed(5)
     g, u = (torch.empty((B, T, I), dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
     lengths = [T, T - 5000, T - 77]
@@ -599,7 +600,7 @@ def test_scan_sequences_far_apart():
     say("scan far apart")
     for reverse in (False, True):
         for n in (None, ln):
-            h, dg, du = (torch.empty_like(g) for _ in range(3))
+            h, dg, du = (torch.full_like(g, FILL) for _ in range(3))
             saved = torch.empty(P.pyramid_scan_saved_size(B, T, I), dtype=torch.uint8, device=DEV)
             P.pyramid_scan_forward(g, u, h, reverse, n, saved=saved)
             P.pyramid_scan_backward(g, u, saved, u, dg, du, reverse, n)
