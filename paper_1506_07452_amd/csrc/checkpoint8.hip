@@ -20,19 +20,22 @@ k_pack8(const T *__restrict__ x, int8_t *__restrict__ q, uint16_t *__restrict__ 
     constexpr long long stretch = (long long)kPackThreads * N;
     for (long long at0 = blockIdx.x * stretch * kPackUnroll + threadIdx.x * N; at0 - threadIdx.x * N < n;
          at0 += gridDim.x * stretch * kPackUnroll) {
-        float v[kPackUnroll][N];
+        u32x4 raw[kPackUnroll];
 #pragma unroll
         for (int t = 0; t < kPackUnroll; ++t) {
             const long long at = at0 + t * stretch, left = n - at;
-            load_piece(x + at, left > N ? N : (int)left, v[t]);
+            raw[t] = load_piece(x + at, left > N ? N : (int)left);
         }
+        loads_issued();
 #pragma unroll
         for (int t = 0; t < kPackUnroll; ++t) {
             const long long at = at0 + t * stretch, left = n - at;
-            const uint16_t s = code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[t])));
+            float v[N];
+            Piece<T>::unpack(raw[t], v);
+            const uint16_t s = code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v)));
             const Coder c(s);
             int code[N];
-            code_piece<T>(c, v[t], code);
+            code_piece<T>(c, v, code);
             store_codes<N>(q + at, left > N ? N : (int)left, code);
             if ((at & (kCodeBlock - 1)) == 0 && left > 0) scale[at >> 6] = s;
         }
@@ -48,16 +51,19 @@ k_unpack8(const int8_t *__restrict__ q, const uint16_t *__restrict__ scale, T *_
     constexpr long long stretch = (long long)kPackThreads * N;
     for (long long at0 = blockIdx.x * stretch * kPackUnroll + threadIdx.x * N; at0 < n;
          at0 += gridDim.x * stretch * kPackUnroll) {
-        float v[kPackUnroll][N];
+        RawCodes<N> raw[kPackUnroll];
 #pragma unroll
         for (int t = 0; t < kPackUnroll; ++t) {
             const long long at = at0 + t * stretch, left = n - at;
-            load_coded<N>(q, scale, at, left > N ? N : (int)left, v[t]);
+            raw[t] = load_coded<N>(q, scale, at, left > N ? N : (int)left);
         }
+        loads_issued();
 #pragma unroll
         for (int t = 0; t < kPackUnroll; ++t) {
             const long long at = at0 + t * stretch, left = n - at;
-            store_piece(x + at, left > N ? N : (int)left, v[t]);
+            float v[N];
+            unpack_coded<N>(raw[t], at, v);
+            store_piece(x + at, left > N ? N : (int)left, v);
         }
     }
 }

@@ -60,35 +60,39 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int c = (j + G * k) * N;
-        load_piece(gamma + c, C - c, ga[k]);
-        load_piece(beta + c, C - c, be[k]);
+        Piece<T>::unpack(load_piece(gamma + c, C - c), ga[k]);
+        Piece<T>::unpack(load_piece(beta + c, C - c), be[k]);
     }
     int turn = 0;
     for (long long m0 = (long long)blockIdx.x * rows * U; m0 < M;
          m0 += (long long)gridDim.x * rows * U) {
-        float v[U][K][N];
+        u32x4 raw[U][K];
 #pragma unroll
         for (int t = 0; t < U; ++t) {
             const long long m = m0 + t * rows + group;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int c = (j + G * k) * N;
-                load_piece(x + m * C + c, m < M ? C - c : 0, v[t][k]);
+                raw[t][k] = load_piece(x + m * C + c, m < M ? C - c : 0);
             }
         }
+        loads_issued();
 #pragma unroll
         for (int t = 0; t < U; ++t) {
             const long long m = m0 + t * rows + group;
+            float v[K][N];
+#pragma unroll
+            for (int k = 0; k < K; ++k) Piece<T>::unpack(raw[t][k], v[k]);
             if (CODE) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     const int c = (j + G * k) * N;
                     const long long at = m * C + c;
                     const uint16_t s =
-                        code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[t][k])));
+                        code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[k])));
                     const Coder cd(s);
                     int code[N];
-                    code_piece<T>(cd, v[t][k], code);
+                    code_piece<T>(cd, v[k], code);
                     if (m < M && c < C) {
                         store_codes<N>(xq + at, N, code);
                         if ((at & (kCodeBlock - 1)) == 0) xscale[at >> 6] = s;
@@ -99,7 +103,7 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum += v[t][k][i];
+                for (int i = 0; i < N; ++i) sum += v[k][i];
             sum = group_sum<G>(sum, lds[turn][0]);
             // the quotient sum / C, one step better than the product with 1 / C: a row of
             // one value has to have that value as its mean, or rstd = eps^-1/2 shows it
@@ -111,8 +115,8 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
                 const int c = (j + G * k) * N;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    v[t][k][i] -= mean;
-                    if (c + i < C) var = fmaf(v[t][k][i], v[t][k][i], var);
+                    v[k][i] -= mean;
+                    if (c + i < C) var = fmaf(v[k][i], v[k][i], var);
                 }
             }
             const float rstd = rsqrtf(fmaf(group_sum<G>(var, lds[turn][1]), inv, eps));
@@ -124,7 +128,7 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
                     float o[N];
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        o[i] = fmaf(v[t][k][i] * rstd, ga[k][i], be[k][i]);
+                        o[i] = fmaf(v[k][i] * rstd, ga[k][i], be[k][i]);
                     store_piece(y + m * C + c, C - c, o);
                 }
                 if (stats && j == 0) stats[m] = make_float2(mean, rstd);
@@ -133,17 +137,23 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
     }
 }
 
-template <typename T, int N>
-__device__ inline void load_x(const T *x, const uint16_t *, long long at, int have, float *v)
-{
-    load_piece(x + at, have, v);
-}
-template <typename T, int N>
-__device__ inline void load_x(const int8_t *x, const uint16_t *scale, long long at, int have,
-                              float *v)
-{
-    load_coded<N>(x, scale, at, have, v);
-}
+// A piece of x in raw bits and its values: from the storage type, or from codes.
+template <typename T, typename X> struct RawX {
+    u32x4 w;
+    __device__ void load(const T *x, const uint16_t *, long long at, int have)
+    {
+        w = load_piece(x + at, have);
+    }
+    __device__ void unpack(long long, float *v) const { Piece<T>::unpack(w, v); }
+};
+template <typename T> struct RawX<T, int8_t> {
+    RawCodes<Piece<T>::N> w;
+    __device__ void load(const int8_t *x, const uint16_t *scale, long long at, int have)
+    {
+        w = load_coded<Piece<T>::N>(x, scale, at, have);
+    }
+    __device__ void unpack(long long at, float *v) const { unpack_coded(w, at, v); }
+};
 
 // A workgroup walks every gridDim-th stretch of rows with its columns' sums of
 // dy xh and dy in registers; at the end its lane groups' sums are added in
@@ -167,14 +177,15 @@ k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int c = (j + G * k) * N;
-        load_piece(gamma + c, C - c, ga[k]);
+        Piece<T>::unpack(load_piece(gamma + c, C - c), ga[k]);
 #pragma unroll
         for (int i = 0; i < N; ++i) sg[k][i] = sb[k][i] = 0.0f;
     }
     int turn = 0;
     for (long long m0 = (long long)blockIdx.x * rows * U; m0 < M;
          m0 += (long long)gridDim.x * rows * U) {
-        float v[U][K][N], d[U][K][N];
+        RawX<T, X> rx[U][K];
+        u32x4 rd[U][K];
         float2 st[U];
 #pragma unroll
         for (int t = 0; t < U; ++t) {
@@ -183,24 +194,31 @@ k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int c = (j + G * k) * N, have = m < M ? C - c : 0;
-                load_x<T, N>(x, xscale, m * C + c, have, v[t][k]);
-                load_piece(dy + m * C + c, have, d[t][k]);
+                rx[t][k].load(x, xscale, m * C + c, have);
+                rd[t][k] = load_piece(dy + m * C + c, have);
             }
         }
+        loads_issued();
 #pragma unroll
         for (int t = 0; t < U; ++t) {
             const long long m = m0 + t * rows + group;
+            float v[K][N], d[K][N];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                rx[t][k].unpack(m * C + (j + G * k) * N, v[k]);
+                Piece<T>::unpack(rd[t][k], d[k]);
+            }
             float ta = 0.0f, tb = 0.0f;
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float xh = (v[t][k][i] - st[t].x) * st[t].y, a = d[t][k][i] * ga[k][i];
-                    v[t][k][i] = xh;
+                    const float xh = (v[k][i] - st[t].x) * st[t].y, a = d[k][i] * ga[k][i];
+                    v[k][i] = xh;
                     ta += a;
                     tb = fmaf(a, xh, tb);
-                    sg[k][i] = fmaf(d[t][k][i], xh, sg[k][i]);
-                    sb[k][i] += d[t][k][i];
+                    sg[k][i] = fmaf(d[k][i], xh, sg[k][i]);
+                    sb[k][i] += d[k][i];
                 }
             if (!dx) continue;
             ta = group_sum<G>(ta, lds[turn][0]) * inv;
@@ -213,7 +231,7 @@ k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
                     float o[N];
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        o[i] = st[t].y * (fmaf(d[t][k][i], ga[k][i], -ta) - v[t][k][i] * tb);
+                        o[i] = st[t].y * (fmaf(d[k][i], ga[k][i], -ta) - v[k][i] * tb);
                     store_piece(dx + m * C + c, C - c, o);
                 }
             }
@@ -258,23 +276,31 @@ k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
     }
 }
 
-// dgamma and dbeta from `count` parts, in order: 64 columns and 16 stretches of parts a workgroup.
+// dgamma and dbeta from `count` parts: 16 columns a workgroup, 64 lanes each with every
+// 64th part; then the lanes of a wave, then the waves, in order.
 __global__ void __launch_bounds__(1024)
 k_norm_dw_sum(const float *__restrict__ part, int count, float *__restrict__ dgamma,
               float *__restrict__ dbeta, int C)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
-    const int c = blockIdx.x * 64 + lane;
+    __shared__ float lds[16][16];
+    const int col = threadIdx.x & 15, w = threadIdx.x / 64;
+    const int c = blockIdx.x * 16 + col;
     float s = 0.0f;
-    if (c < 2 * C)
-        for (int k = w; k < count; k += 16) s += part[(long long)k * 2 * C + c];
-    lds[w][lane] = s;
+    if (c < 2 * C) {
+#pragma unroll
+        for (int i = 0; i < kNormMaxParts / 64; ++i) {
+            const int k = (int)(threadIdx.x / 16) + 64 * i;
+            s += k < count ? part[(long long)k * 2 * C + c] : 0.0f;
+        }
+    }
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 63) < 16) lds[w][col] = s;
     __syncthreads();
-    if (w != 0 || c >= 2 * C) return;
+    if (threadIdx.x >= 16 || c >= 2 * C) return;
     s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += lds[k][lane];
+    for (int k = 0; k < 16; ++k) s += lds[k][col];
     (c < C ? dgamma[c] : dbeta[c - C]) = s;
 }
 
@@ -358,7 +384,7 @@ int norm_backward(long long M, int C, const X *x, const uint16_t *xscale, const 
         PLSTM_LAUNCH_CHECK();
         *launches = 1;
         if (count > 1) {
-            k_norm_dw_sum<<<(unsigned)((2 * C + 63) / 64), 1024, 0, st>>>(part, count, dgamma,
+            k_norm_dw_sum<<<(unsigned)((2 * C + 15) / 16), 1024, 0, st>>>(part, count, dgamma,
                                                                          dbeta, C);
             PLSTM_LAUNCH_CHECK();
             *launches = 2;

@@ -19,65 +19,68 @@ __device__ inline uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// All loads so far are issued before anything that follows.  Loads give raw bits for
+// this: left to itself the scheduler converts values as they come, and waits for
+// each of a lane's loads in turn.
+__device__ inline void loads_issued() { __builtin_amdgcn_sched_barrier(0); }
+
 template <typename T> struct Piece;
 
 template <> struct Piece<float> {
     static constexpr int N = 4;
-    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
-    __device__ static void load(const float *p, float *v)
+    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(4)));
+    __device__ static void unpack(u32x4 w, float *v)
     {
-        const V w = *(const V *)p;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = w[j];
+        for (int j = 0; j < 4; ++j) v[j] = bits_float(w[j]);
     }
-    __device__ static void store(float *p, const float *v)
+    __device__ static u32x4 packed(const float *v)
     {
-        V w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[j];
-        *(V *)p = w;
+        return u32x4{float_bits(v[0]), float_bits(v[1]), float_bits(v[2]), float_bits(v[3])};
     }
 };
 
 template <> struct Piece<uint16_t> {
     static constexpr int N = 8;
     typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
-    __device__ static void load(const uint16_t *p, float *v)
+    __device__ static void unpack(u32x4 w, float *v)
     {
-        const V w = *(const V *)p;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v[2 * j] = bits_float(w[j] << 16);
             v[2 * j + 1] = bits_float(w[j] & 0xffff0000u);
         }
     }
-    __device__ static void store(uint16_t *p, const float *v)
+    __device__ static u32x4 packed(const float *v)
     {
-        V w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-        *(V *)p = w;
+        return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+                     pack_bf16(v[6], v[7])};
     }
 };
 
 // Elements [0, have) of a piece; the others read as 0 and are not written.
 template <typename T>
-__device__ inline void load_piece(const T *p, int have, float *v)
+__device__ inline u32x4 load_piece(const T *p, int have)
 {
-    constexpr int N = Piece<T>::N;
-    if (have >= N) {
-        Piece<T>::load(p, v);
-    } else {
+    constexpr int N = Piece<T>::N, per = N / 4;
+    if (have >= N) return *(const typename Piece<T>::V *)p;
+    u32x4 w = {0, 0, 0, 0};
+    if (have > 0) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = j < have ? Store<T>::load(p, j) : 0.0f;
+        for (int j = 0; j < N - 1; ++j)
+            if (j < have) w[j / per] |= per == 1 ? float_bits(Store<T>::load(p, j))
+                                                 : float_bits(Store<T>::load(p, j)) >> 16 << (16 * (j % per));
     }
+    return w;
 }
 template <typename T>
 __device__ inline void store_piece(T *p, int have, const float *v)
 {
     constexpr int N = Piece<T>::N;
     if (have >= N) {
-        Piece<T>::store(p, v);
+        *(typename Piece<T>::V *)p = Piece<T>::packed(v);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -85,7 +88,7 @@ __device__ inline void store_piece(T *p, int have, const float *v)
     }
 }
 
-// N = 4 or 8 codes as bytes, and back.
+// N = 4 or 8 codes as bytes.
 template <int N>
 __device__ inline void store_codes(int8_t *q, int have, const int *c)
 {
@@ -103,34 +106,45 @@ __device__ inline void store_codes(int8_t *q, int have, const int *c)
             if (j < have) q[j] = (int8_t)c[j];
     }
 }
+
+// N codes at flat elements at .. at + have - 1 of a checkpoint, with the scales of
+// the blocks that they are in (two at most), in raw bits.
+template <int N> struct RawCodes {
+    uint32_t w[N / 4];
+    uint32_t s0, s1;
+};
 template <int N>
-__device__ inline void load_codes(const int8_t *q, int have, float *v)
+__device__ inline RawCodes<N> load_coded(const int8_t *q, const uint16_t *scale, long long at,
+                                         int have)
 {
     typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
-    if (have >= N) {
-        const V w = *(const V *)q;
+    RawCodes<N> r;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = (float)(int)(int8_t)(w[j / 4] >> (8 * (j % 4)));
+    for (int j = 0; j < N / 4; ++j) r.w[j] = 0;
+    r.s0 = r.s1 = 0;
+    if (have <= 0) return r;
+    if (have >= N) {
+        have = N;
+        const V w = *(const V *)(q + at);
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) r.w[j] = w[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = j < have ? (float)q[j] : 0.0f;
+        for (int j = 0; j < N - 1; ++j)
+            if (j < have) r.w[j / 4] |= (uint32_t)(uint8_t)q[at + j] << (8 * (j % 4));
     }
+    r.s0 = scale[at >> 6];
+    r.s1 = scale[(at + have - 1) >> 6];
+    return r;
 }
-
-// The values of codes at flat elements at .. at + N - 1 of a checkpoint (two
-// blocks at most).
 template <int N>
-__device__ inline void load_coded(const int8_t *q, const uint16_t *scale, long long at, int have,
-                                  float *v)
+__device__ inline void unpack_coded(const RawCodes<N> &r, long long at, float *v)
 {
-    if (have > N) have = N;
-    if (have <= 0) have = 0;
-    load_codes<N>(q + at, have, v);
-    if (have == 0) return;
-    const float s0 = bf16_to_f32(scale[at >> 6]), s1 = bf16_to_f32(scale[(at + have - 1) >> 6]);
     const int turn = kCodeBlock - (int)(at & (kCodeBlock - 1));
+    const float s0 = bits_float(r.s0 << 16), s1 = bits_float(r.s1 << 16);
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] *= j < turn ? s0 : s1;
+    for (int j = 0; j < N; ++j)
+        v[j] = (float)(int)(int8_t)(r.w[j / 4] >> (8 * (j % 4))) * (j < turn ? s0 : s1);
 }
 
 // Largest / sum over aligned groups of G lanes (a power of two <= 64), in every

@@ -146,10 +146,6 @@ template <typename X> __device__ inline float value(uint32_t raw);
 template <> __device__ inline float value<float>(uint32_t raw) { return bits_float(raw); }
 template <> __device__ inline float value<uint16_t>(uint32_t raw) { return bits_float(raw << 16); }
 template <> __device__ inline float value<int8_t>(uint32_t raw) { return (float)(int)raw; }
-// All loads so far are issued before anything that follows: left to itself the
-// scheduler converts codes as they come, and a run waits sixteen times.
-__device__ inline void loads_issued() { __builtin_amdgcn_sched_barrier(0); }
-
 // Raw scale of a code.
 template <typename O>
 __device__ inline uint32_t get_scale(const uint16_t *scale, long long base, O off)
