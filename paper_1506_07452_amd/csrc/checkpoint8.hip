@@ -34,9 +34,9 @@ k_pack8(const T *__restrict__ x, int8_t *__restrict__ q, uint16_t *__restrict__ 
             Piece<T>::unpack(raw[t], v);
             const uint16_t s = code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v)));
             const Coder c(s);
-            int code[N];
+            uint32_t code[N];
             code_piece<T>(c, v, code);
-            store_codes<N>(q + at, left > N ? N : (int)left, code);
+            store_codes<N>(q + at, left > N ? N : (int)left, code, c.keep);
             if ((at & (kCodeBlock - 1)) == 0 && left > 0) scale[at >> 6] = s;
         }
     }

@@ -91,10 +91,10 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
                     const uint16_t s =
                         code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v[k])));
                     const Coder cd(s);
-                    int code[N];
+                    uint32_t code[N];
                     code_piece<T>(cd, v[k], code);
                     if (m < M && c < C) {
-                        store_codes<N>(xq + at, N, code);
+                        store_codes<N>(xq + at, N, code, cd.keep);
                         if ((at & (kCodeBlock - 1)) == 0) xscale[at >> 6] = s;
                     }
                 }

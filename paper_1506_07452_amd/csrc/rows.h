@@ -88,22 +88,24 @@ __device__ inline void store_piece(T *p, int have, const float *v)
     }
 }
 
-// N = 4 or 8 codes as bytes.
+// N = 4 or 8 codes, each in the low byte of its word, as bytes.
 template <int N>
-__device__ inline void store_codes(int8_t *q, int have, const int *c)
+__device__ inline void store_codes(int8_t *q, int have, const uint32_t *c, uint32_t keep)
 {
     typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
-    if (have >= N) {
-        V w;
+    V w;
 #pragma unroll
-        for (int j = 0; j < N / 4; ++j)
-            w[j] = (uint32_t)(c[4 * j] & 255) | (uint32_t)(c[4 * j + 1] & 255) << 8 |
-                   (uint32_t)(c[4 * j + 2] & 255) << 16 | (uint32_t)c[4 * j + 3] << 24;
+    for (int j = 0; j < N / 4; ++j) {
+        const uint32_t lo = __builtin_amdgcn_perm(c[4 * j + 1], c[4 * j], 0x0c0c0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(c[4 * j + 3], c[4 * j + 2], 0x04000c0cu);
+        w[j] = (lo | hi) & keep;
+    }
+    if (have >= N) {
         *(V *)q = w;
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            if (j < have) q[j] = (int8_t)c[j];
+            if (j < have) q[j] = (int8_t)(w[j / 4] >> (8 * (j % 4)));
     }
 }
 
@@ -191,7 +193,7 @@ __device__ inline uint32_t top_bits(const float *v)
 
 // Codes of a piece of a block whose largest magnitude has bits `top`.
 template <typename T>
-__device__ inline void code_piece(const Coder &c, const float *v, int *q)
+__device__ inline void code_piece(const Coder &c, const float *v, uint32_t *q)
 {
 #pragma unroll
     for (int j = 0; j < Piece<T>::N; ++j)
