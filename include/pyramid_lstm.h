@@ -405,7 +405,7 @@ int pyramid_stitch_finish(int32_t D, int32_t H, int32_t W, int32_t K, const void
  *   xq, xscale  : both NULL, or the 8-bit checkpoint of x (codes [M][C] and
  *                 pyramid_checkpoint8_scales(M * C) scales), written in the
  *                 same call with the values of pyramid_checkpoint8_pack.
- * 1 <= C <= 16384, M >= 1, M * C <= 2^38. */
+ * 1 <= C <= 16384, 1 <= M <= 2^32, M * C <= 2^38. */
 int pyramid_layer_norm_forward(int64_t M, int32_t C, int32_t dtype, float eps, const void *x,
                                const void *gamma, const void *beta, void *y, void *stats,
                                void *xq, void *xscale, void *stream);
@@ -446,7 +446,10 @@ int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void 
  *   saved       : NULL, or pyramid_scan_saved_size() bytes for the backward:
  *                 fp32 [B][ceil(T/16)][I], the state before positions 0, 16, ...
  *   ws          : at least pyramid_scan_workspace_size() bytes.
- * States are fp32 whatever the storage type.  B, T, I >= 1, B T I <= 2^38. */
+ * States are fp32 whatever the storage type.  B, T, I >= 1, B I <= 2^30,
+ * T <= 2^31, B T I <= 2^38.  Long sequences are cut into chunks that wait for
+ * each other on the device, every wait bounded: one that gives up makes the
+ * states behind it NaN and raises PLSTM_DEVICE_WAIT_GAVE_UP. */
 size_t pyramid_scan_workspace_size(int64_t B, int64_t T, int64_t I);
 size_t pyramid_scan_saved_size(int64_t B, int64_t T, int64_t I);
 int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t reverse,

@@ -4,6 +4,9 @@ Fig. 3 / Section 2.3: PyraMiD-LSTM layer -> per-voxel FC + tanh, repeated;
 the last FC layer feeds a per-voxel softmax.  This module only allocates
 tensors with torch and calls the library (every arithmetic step runs in the
 HIP kernels); gradients flow through the same entry points in reverse.
+Beyond Fig. 3 a layer's output may be normed over its channels before its FC
+(`norms`), and a training step may hold what the layers keep for their
+backward in 8 bits (`checkpoint8`).
 """
 from __future__ import annotations
 
@@ -12,11 +15,14 @@ from typing import List, Optional, Tuple
 
 import torch
 
-from . import (plstm_shape, pyramid_fc_tanh_backward, pyramid_fc_tanh_forward,
+from . import (checkpoint8_empty, plstm_shape, pyramid_checkpoint8_pack,
+               pyramid_checkpoint8_unpack, pyramid_fc_tanh_backward, pyramid_fc_tanh_forward,
                pyramid_head_forward, pyramid_head_forward_supported,
-               pyramid_head_train, pyramid_head_workspace_size, pyramid_lstm_backward,
+               pyramid_head_train, pyramid_head_workspace_size, pyramid_layer_norm_backward,
+               pyramid_layer_norm_forward, pyramid_lstm_backward,
                pyramid_lstm_forward, pyramid_lstm_saved_size, pyramid_lstm_workspace_size,
                pyramid_lstm2d_backward, pyramid_lstm2d_forward, pyramid_lstm2d_saved_size,
+               pyramid_scan_backward, pyramid_scan_forward, pyramid_scan_saved_size,
                pyramid_softmax_ce, shape2d_for, shape_for)
 
 
@@ -74,6 +80,99 @@ def layer2d_backward(x, L: LayerW, saved, dh, want_dx=True, ws=None, stream=None
     return dx, dwx, dwh, db
 
 
+def norm_forward(h: torch.Tensor, gamma, beta, eps: float = 1e-5, training: bool = False,
+                 checkpoint8: bool = False, stream=None):
+    """Layer norm over the last axis of h; returns (y, kept): kept is None for
+    inference, else what norm_backward needs, with h itself or (checkpoint8)
+    its 8-bit checkpoint."""
+    C = h.shape[-1]
+    rows = h.view(-1, C)
+    y = torch.empty_like(h)
+    if not training:
+        pyramid_layer_norm_forward(rows, gamma, beta, y.view(-1, C), eps=eps, stream=stream)
+        return y, None
+    stats = torch.empty((rows.shape[0], 2), dtype=torch.float32, device=h.device)
+    q, scale = checkpoint8_empty(rows) if checkpoint8 else (None, None)
+    pyramid_layer_norm_forward(rows, gamma, beta, y.view(-1, C), stats, q, scale, eps=eps,
+                               stream=stream)
+    return y, (rows if q is None else q, scale, stats)
+
+
+def norm_backward(kept, gamma, dy, want_dx=True, ws=None, stream=None):
+    """(dx or None, dgamma, dbeta) of norm_forward for dy of its output's shape."""
+    x, scale, stats = kept
+    rows = dy.view(x.shape)
+    dx = torch.empty_like(rows) if want_dx else None
+    dgamma, dbeta = (torch.empty(x.shape[1], dtype=torch.float32, device=dy.device)
+                     for _ in range(2))
+    pyramid_layer_norm_backward(x, gamma, stats, rows, dx, dgamma, dbeta, xscale=scale, ws=ws,
+                                stream=stream)
+    return None if dx is None else dx.view(dy.shape), dgamma, dbeta
+
+
+def _sequences(x, axis):
+    """The [B][T][I] view of a volume [N][D][H][W][C] whose middle axis is `axis`."""
+    if x.dim() != 5 or axis not in ("z", "y", "x"):
+        raise ValueError("x must be [N][D][H][W][C] and axis one of z, y, x")
+    N, D, H, W, C = x.shape
+    return x.view({"z": (N, D, H * W * C), "y": (N * D, H, W * C), "x": (N * D * H, W, C)}[axis])
+
+
+def scan_forward(g: torch.Tensor, u: torch.Tensor, axis: str, reverse: bool = False,
+                 training: bool = False, ws=None, stream=None):
+    """Linear sweep of a volume along `axis` ("z", "y" or "x"; from the far side
+    with `reverse`), gates g and inputs u [N][D][H][W][C]; returns (h, saved or
+    None)."""
+    gs, us = _sequences(g, axis), _sequences(u, axis)
+    h = torch.empty_like(g)
+    saved = None
+    if training:
+        saved = torch.empty(pyramid_scan_saved_size(*gs.shape), dtype=torch.uint8, device=g.device)
+    pyramid_scan_forward(gs, us, _sequences(h, axis), reverse, saved=saved, ws=ws, stream=stream)
+    return h, saved
+
+
+def scan_backward(g, u, saved, dh, axis: str, reverse: bool = False, ws=None, stream=None):
+    """(dg, du) of scan_forward; g and u are its inputs, or (codes, scale) pairs of
+    their 8-bit checkpoints."""
+    (g, gscale), (u, uscale) = (t if isinstance(t, tuple) else (t, None) for t in (g, u))
+    dg, du = torch.empty_like(dh), torch.empty_like(dh)
+    pyramid_scan_backward(_sequences(g, axis), _sequences(u, axis), saved, _sequences(dh, axis),
+                          _sequences(dg, axis), _sequences(du, axis), reverse, gscale=gscale,
+                          uscale=uscale, ws=ws, stream=stream)
+    return dg, du
+
+
+def _saved_arrays(saved, s: plstm_shape):
+    """The fp32 arrays (gates, c^d, h^d) of a training forward's saved buffer:
+    each starts at the next 256-byte boundary."""
+    cells = 6 * s.N * s.D * s.H * s.W * s.O
+    out, off = [], 0
+    for n in (4 * cells, cells, cells):
+        off = -(-off // 256) * 256
+        out.append(saved[off:off + 4 * n].view(torch.float32))
+        off += 4 * n
+    return out
+
+
+def saved_pack(saved, s: plstm_shape, stream=None):
+    """8-bit checkpoints of a saved buffer's arrays (about a quarter of its bytes)."""
+    out = []
+    for a in _saved_arrays(saved, s):
+        q, scale = checkpoint8_empty(a)
+        pyramid_checkpoint8_pack(a, q, scale, stream)
+        out.append((q, scale))
+    return out
+
+
+def saved_unpack(packed, s: plstm_shape, stream=None):
+    """A saved buffer with the values of saved_pack's checkpoints."""
+    saved = torch.empty(pyramid_lstm_saved_size(s), dtype=torch.uint8, device=packed[0][0].device)
+    for (q, scale), a in zip(packed, _saved_arrays(saved, s)):
+        pyramid_checkpoint8_unpack(q, scale, a, stream)
+    return saved
+
+
 def workspace_for(x_shape, hidden: List[int], fc: bool, dtype, training: bool, device):
     """One workspace big enough for every layer of a network whose FC layers
     are twice as wide as the layer before (3 x 3 filters)."""
@@ -96,10 +195,14 @@ def workspace_for_layers(x_shape, shapes, dtype, training: bool, device):
 
 def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch.Tensor]],
                     head: Tuple[torch.Tensor, torch.Tensor], labels: Optional[torch.Tensor] = None,
-                    training: bool = False, ws=None, stream=None, loss: str = "ce"):
+                    training: bool = False, ws=None, stream=None, loss: str = "ce", norms=None,
+                    checkpoint8: bool = False):
     """Returns dict: 'p' [M][K] fp32, 'loss' (device scalar, with labels),
     'acts' (per-layer inputs/outputs and saved activations for training).
-    loss: "ce" (mean cross-entropy) or "sq" (squared error, Eq. (14))."""
+    loss: "ce" (mean cross-entropy) or "sq" (squared error, Eq. (14)).
+    norms: per layer None or (gamma, beta) [O], a layer norm of its output over
+    the channels before its FC.  checkpoint8 (training): as in
+    network_train_step."""
     N, D, H, W, _ = x.shape
     M = N * D * H * W
     if len(fcs) not in (len(layers), len(layers) - 1):
@@ -113,9 +216,8 @@ def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch
     a = x
     acts = []
     for li, L in enumerate(layers):
-        h, saved = layer_forward(a, L, training, ws, stream)
-        act = {"in": a, "h": h, "saved": saved}
-        a = h
+        act = _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream)
+        h = a = act["h"]
         if fused and li == len(layers) - 1:
             acts.append(act)
             p = torch.empty((M, K), dtype=torch.float32, device=x.device)
@@ -151,11 +253,48 @@ def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch
     return out
 
 
+def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
+    """Layer li and its norm on input a: 'h' is what the FC reads; for training
+    'saved' and, with a norm, 'kept'.  With checkpoint8 a layer below the last
+    one keeps its saved buffer, and its norm's input, in 8 bits ('packed'): until
+    its backward they lie idle."""
+    L = layers[li]
+    eight = training and checkpoint8 and li < len(layers) - 1
+    h, saved = layer_forward(a, L, training, ws, stream)
+    act = {"in": a, "h": h, "saved": saved}
+    if eight:
+        act["packed"] = saved_pack(saved, shape_for(a, L.O, L.K), stream)
+        act["saved"] = None
+    if norms is not None and norms[li] is not None:
+        act["h"], act["kept"] = norm_forward(h, *norms[li], training=training, checkpoint8=eight,
+                                             stream=stream)
+    return act
+
+
+def _layer_act_backward(act, li, layers, norms, dh, ws, stream):
+    """(dx or None, (dwx, dwh, db), (dgamma, dbeta) or None) from the gradient of
+    act's 'h'."""
+    L, dn = layers[li], None
+    if "kept" in act:
+        dh, dgamma, dbeta = norm_backward(act["kept"], norms[li][0], dh, stream=stream)
+        dn = (dgamma, dbeta)
+    saved = act["saved"]
+    if "packed" in act:
+        saved = saved_unpack(act["packed"], shape_for(act["in"], L.O, L.K), stream)
+    dx, dwx, dwh, db = layer_backward(act["in"], L, saved, dh.view(act["h"].shape),
+                                      want_dx=li > 0, ws=ws, stream=stream)
+    return dx, (dwx, dwh, db), dn
+
+
 def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused_head=True,
-                       loss="ce"):
+                       loss="ce", norms=None, checkpoint8=False):
     """Forward + back-propagation through the whole network (fp32).
     Returns dict with 'loss', 'p', 'head' (dw, db), 'fcs' [(dw, db)],
-    'layers' [(dwx, dwh, db)].  With `fused_head` (default) the last FC + tanh,
+    'layers' [(dwx, dwh, db)] and, with norms (see network_forward), 'norms'
+    [(dgamma, dbeta) or None].  checkpoint8: the layers below the last hold their saved
+    buffers, and the inputs of their norms, in 8 bits until their backward
+    (gradients are then those of activations rounded to a 127th of the largest
+    of 64).  With `fused_head` (default) the last FC + tanh,
     the softmax head, the loss and their backward run as one pass over the
     voxels (pyramid_head_train) where it covers the widths."""
     N, D, H, W, _ = x.shape
@@ -164,12 +303,13 @@ def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused
     O_last, F_last, K = layers[-1].O, fcs[-1][0].shape[0], head[0].shape[0]
     if not (fused_head and loss == "ce" and len(fcs) == nl and
             pyramid_head_workspace_size(M, O_last, F_last, K) > 0):
-        return _train_step_unfused(x, layers, fcs, head, labels, ws, stream, loss)
+        return _train_step_unfused(x, layers, fcs, head, labels, ws, stream, loss, norms,
+                                   checkpoint8)
     a = x
     acts = []
     for li in range(nl):
-        h, saved = layer_forward(a, layers[li], True, ws, stream)
-        act = {"in": a, "h": h, "saved": saved}
+        act = _layer_act(a, li, layers, norms, True, checkpoint8, ws, stream)
+        h = act["h"]
         if li < nl - 1:
             wf, bf = fcs[li]
             y = torch.empty((N, D, H, W, wf.shape[0]), dtype=a.dtype, device=a.device)
@@ -186,7 +326,7 @@ def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused
     pyramid_head_train(acts[-1]["h"].view(M, O_last), wf, bf, head[0], head[1], labels, p, lval,
                        dh, dwf, dbf, dw, db, stream=stream)
     fc_grads = [None] * len(fcs)
-    layer_grads = [None] * nl
+    layer_grads, norm_grads = [None] * nl, [None] * nl
     fc_grads[-1] = (dwf, dbf)
     g = None
     for li in range(nl - 1, -1, -1):
@@ -199,24 +339,25 @@ def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused
             pyramid_fc_tanh_backward(act["h"].view(M, O), wf, act["y"].view(M, -1),
                                      g.view(M, -1), dh, dwf, dbf, stream=stream)
             fc_grads[li] = (dwf, dbf)
-        dx, dwx, dwh, db_l = layer_backward(act["in"], layers[li], act["saved"],
-                                            dh.view(act["h"].shape), want_dx=li > 0, ws=ws,
-                                            stream=stream)
-        layer_grads[li] = (dwx, dwh, db_l)
-        g = dx
-    return {"loss": lval, "p": p, "head": (dw, db), "fcs": fc_grads, "layers": layer_grads}
+        g, layer_grads[li], norm_grads[li] = _layer_act_backward(act, li, layers, norms, dh, ws,
+                                                                 stream)
+    out = {"loss": lval, "p": p, "head": (dw, db), "fcs": fc_grads, "layers": layer_grads}
+    if norms is not None:
+        out["norms"] = norm_grads
+    return out
 
 
-def _train_step_unfused(x, layers, fcs, head, labels, ws=None, stream=None, loss="ce"):
+def _train_step_unfused(x, layers, fcs, head, labels, ws=None, stream=None, loss="ce", norms=None,
+                        checkpoint8=False):
     """network_train_step composed from the separate FC / softmax entry points."""
     out = network_forward(x, layers, fcs, head, labels, training=True, ws=ws, stream=stream,
-                          loss=loss)
+                          loss=loss, norms=norms, checkpoint8=checkpoint8)
     acts = out["acts"]
     g = out["dlast"]
     N, D, H, W, _ = x.shape
     M = N * D * H * W
     fc_grads = [None] * len(fcs)
-    layer_grads = [None] * len(layers)
+    layer_grads, norm_grads = [None] * len(layers), [None] * len(layers)
     for li in range(len(layers) - 1, -1, -1):
         act = acts[li]
         O = act["h"].shape[-1]
@@ -229,25 +370,30 @@ def _train_step_unfused(x, layers, fcs, head, labels, ws=None, stream=None, loss
             fc_grads[li] = (dwf, dbf)
         else:
             dh = g      # the output layer reads h directly
-        dx, dwx, dwh, db = layer_backward(act["in"], layers[li], act["saved"],
-                                          dh.view(act["h"].shape), want_dx=li > 0, ws=ws,
-                                          stream=stream)
-        layer_grads[li] = (dwx, dwh, db)
+        dx, layer_grads[li], norm_grads[li] = _layer_act_backward(act, li, layers, norms, dh, ws,
+                                                                  stream)
         if li > 0:
             g = dx
-    return {"loss": out["loss"], "p": out["p"], "head": out["head_grad"], "fcs": fc_grads,
-            "layers": layer_grads}
+    res = {"loss": out["loss"], "p": out["p"], "head": out["head_grad"], "fcs": fc_grads,
+           "layers": layer_grads}
+    if norms is not None:
+        res["norms"] = norm_grads
+    return res
 
 
-def network_parameters(layers, fcs, head):
+def network_parameters(layers, fcs, head, norms=None):
     """Every parameter tensor of a network, in the order of
-    `network_gradients`: per layer (wx, wh, b), per hidden FC (w, b), head."""
+    `network_gradients`: per layer (wx, wh, b), per hidden FC (w, b), head, per
+    norm (gamma, beta)."""
     out = []
     for L in layers:
         out += [L.wx, L.wh, L.b]
     for w, b in fcs:
         out += [w, b]
-    return out + [head[0], head[1]]
+    out += [head[0], head[1]]
+    for n in norms or []:
+        out += list(n or ())
+    return out
 
 
 def network_gradients(g):
@@ -258,7 +404,10 @@ def network_gradients(g):
         out += list(t)
     for t in g["fcs"]:
         out += list(t)
-    return out + [g["head"][0], g["head"][1]]
+    out += [g["head"][0], g["head"][1]]
+    for n in g.get("norms", []):
+        out += list(n or ())
+    return out
 
 
 def grid_axis(extent, size, stride):
@@ -275,7 +424,7 @@ def grid_axis(extent, size, stride):
 
 
 def network_infer_volume(x, layers, fcs, head, tile, stride=None, sigma_scale=0.25, ws=None,
-                         stream=None, origins=None):
+                         stream=None, origins=None, norms=None):
     """Class probabilities [N][D][H][W][K] of a volume processed as sub-volumes
     (Section 3, "Sub-volumes and Augmentation"): tiles of size `tile` (d, h, w),
     each run through the network on its own and stitched with Gaussian weights
@@ -307,7 +456,8 @@ def network_infer_volume(x, layers, fcs, head, tile, stride=None, sigma_scale=0.
                 for x0 in xs:
                     box = (z0, y0, x0, td, th, tw)
                     pyramid_crop(x, n, box, sub, stream)
-                    p = network_forward(sub, layers, fcs, head, ws=ws, stream=stream)["p"]
+                    p = network_forward(sub, layers, fcs, head, ws=ws, stream=stream,
+                                        norms=norms)["p"]
                     pyramid_stitch_add(p.view(td, th, tw, K), box, acc, wsum, sigma_scale,
                                        stream)
         pyramid_stitch_finish(acc, wsum, out[n], stream)

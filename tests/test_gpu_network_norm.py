@@ -1,0 +1,317 @@
+"""Networks with layer norms and 8-bit checkpoints, linear sweeps of volumes,
+and the operators together as a block, on the GPU against 64-bit compositions."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_1506_07452_amd as P
+import synth
+from paper_1506_07452_amd import network as net
+from tests import seq_ref as R
+from tests.gpu_util import DEV, TOL, dev, host, layer_dev, normwise, say
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+
+
+def norm64(h, gamma, beta):
+    """y and what its backward needs, numpy float64."""
+    rows = torch.from_numpy(np.ascontiguousarray(h.reshape(-1, h.shape[-1])))
+    y, _, mean, rstd = R.norm_forward(rows, torch.from_numpy(gamma), torch.from_numpy(beta), EPS, torch.float32)
+    return y.numpy().reshape(h.shape), (rows, mean, rstd)
+
+
+def norm64_backward(kept, gamma, dy):
+    rows, mean, rstd = kept
+    d = torch.from_numpy(np.ascontiguousarray(dy.reshape(rows.shape)))
+    dx, dg, db = R.norm_backward(rows, mean, rstd, torch.from_numpy(gamma), d, torch.float32)
+    return dx[0].numpy().reshape(dy.shape), dg[0].numpy(), db[0].numpy()
+
+
+def oracle_step(x, layers, norms, fcs, head, labels):
+    """The training step of a normed network on the fp64 oracle."""
+    N, D, H, W, _ = x.shape
+    a, acts = np.asarray(x, np.float64), []
+    for li, (wx, wh, b) in enumerate(layers):
+        act = {"in": a, "raw": oracle.forward(a, wx, wh, b)["h"]}
+        act["h"] = act["raw"]
+        if norms[li] is not None:
+            act["h"], act["kept"] = norm64(act["raw"], *norms[li])
+        a = act["h"]
+        if li < len(fcs):
+            act["y"] = a = oracle.fc_tanh_forward(a.reshape(-1, a.shape[-1]), *fcs[li]).reshape(N, D, H, W, -1)
+        acts.append(act)
+    out = oracle.softmax_ce(a.reshape(-1, a.shape[-1]), head[0], head[1], labels, grad=True)
+    g, gl, gn, gf = out["dx"].reshape(a.shape), [None] * len(layers), [None] * len(layers), [None] * len(fcs)
+    for li in range(len(layers) - 1, -1, -1):
+        act = acts[li]
+        if li < len(fcs):
+            f = oracle.fc_tanh_backward(act["h"].reshape(-1, act["h"].shape[-1]), fcs[li][0],
+                                        act["y"].reshape(-1, act["y"].shape[-1]), g.reshape(-1, g.shape[-1]))
+            gf[li] = (f["dw"], f["db"])
+            g = f["dx"].reshape(act["h"].shape)
+        if "kept" in act:
+            g, dgamma, dbeta = norm64_backward(act["kept"], norms[li][0], g)
+            gn[li] = (dgamma, dbeta)
+        lg = oracle.backward(act["in"], *layers[li], g, want_dx=li > 0)
+        gl[li] = (lg["dwx"], lg["dwh"], lg["db"])
+        g = lg.get("dx")
+    return {"loss": out["loss"], "p": out["p"], "head": (out["dw"], out["db"]), "fcs": gf, "layers": gl, "norms": gn}
+
+
+def case(hidden, last_fc, seed, normed):
+    """A small network: seeded layers, FCs and norms, numpy (fp32 values) and on the device."""
+    wl = synth.Workload("normed", 1, 4, 9, 11, 3, hidden, fc=True, classes=4, labels=True, seed=seed)
+    inst = synth.make(wl)
+    rng = np.random.default_rng(seed)
+    fcs, head = list(inst.fcs), inst.head
+    if not last_fc:
+        fcs = fcs[:-1]
+        head = (rng.uniform(-.1, .1, (4, hidden[-1])).astype(np.float32), head[1])
+    norms = [(rng.uniform(.5, 1.5, o).astype(np.float32), rng.uniform(-.2, .2, o).astype(np.float32)) if n else None
+             for o, n in zip(hidden, normed)]
+    d = {"x": dev(inst.x), "layers": [layer_dev(L) for L in inst.layers], "fcs": [(dev(w), dev(b)) for w, b in fcs],
+         "head": (dev(head[0]), dev(head[1])), "labels": torch.from_numpy(inst.labels).to(DEV),
+         "norms": [None if n is None else (dev(n[0]), dev(n[1])) for n in norms]}
+    ref = (inst.x, [(L.wx, L.wh, L.b) for L in inst.layers],
+           [None if n is None else tuple(v.astype(np.float64) for v in n) for n in norms],
+           [tuple(np.asarray(v, np.float64) for v in f) for f in fcs], tuple(np.asarray(v, np.float64) for v in head),
+           inst.labels)
+    return d, ref
+
+
+def step(d, **kw):
+    return net.network_train_step(d["x"], d["layers"], d["fcs"], d["head"], d["labels"], norms=d["norms"], **kw)
+
+
+def compare(got, ref, tol):
+    assert normwise(host(got["p"]), ref["p"]) <= tol
+    assert abs(float(got["loss"]) - float(ref["loss"])) <= tol * abs(float(ref["loss"]))
+    for key in ("layers", "fcs", "norms"):
+        for a, b in zip(got[key], ref[key]):
+            assert (a is None) == (b is None)
+            for u, v in zip(a or (), b or ()):
+                assert normwise(host(u), np.asarray(v)) <= tol, key
+    for u, v in zip(got["head"], ref["head"]):
+        assert normwise(host(u), np.asarray(v)) <= tol
+
+
+@pytest.mark.parametrize("last_fc,fused,normed", [(True, True, (1, 1)), (True, False, (1, 1)), (False, True, (1, 1)),
+                                                  (True, True, (0, 1)), (True, True, (1, 0))])
+def test_normed_training_step_matches_oracle(last_fc, fused, normed):
+    d, ref = case([16, 32], last_fc, 41, normed)
+    say("normed step", last_fc, fused, normed)
+    got = step(d, fused_head=fused)
+    compare(got, oracle_step(*ref), TOL["f32"])
+    grads, params = net.network_gradients(got), net.network_parameters(d["layers"], d["fcs"], d["head"], d["norms"])
+    assert [g.shape for g in grads] == [p.shape for p in params]
+
+
+def test_network_without_norms_is_as_before():
+    d, _ = case([16, 32], True, 43, (0, 0))
+    a = net.network_train_step(d["x"], d["layers"], d["fcs"], d["head"], d["labels"])
+    b = step(d)
+    assert "norms" not in a
+    assert all(torch.equal(u, v) for u, v in zip(net.network_gradients(a), net.network_gradients(b)))
+    assert torch.equal(a["p"], b["p"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_normed_inference_matches_oracle(dtype):
+    d, ref = case([16, 32], True, 44, (1, 1))
+    t = (lambda v: v) if dtype == "f32" else (lambda v: v.to(torch.bfloat16))
+    say("normed inference", dtype)
+    layers = [net.LayerW(t(L.wx), t(L.wh), t(L.b)) for L in d["layers"]]
+    args = (layers, [tuple(map(t, f)) for f in d["fcs"]], tuple(map(t, d["head"])))
+    norms = [tuple(map(t, n)) for n in d["norms"]]
+    p = net.network_forward(t(d["x"]), *args, norms=norms)["p"]
+    assert normwise(host(p), oracle_step(*ref)["p"]) <= TOL[dtype]
+    v = net.network_infer_volume(t(d["x"]), *args, tile=d["x"].shape[1:4], stride=(4, 4, 4), norms=norms)
+    assert normwise(host(v.reshape(p.shape)), host(p)) <= 1e-6      # one tile: acc / wsum of one product
+
+
+@pytest.mark.parametrize("last_fc", [True, False])
+def test_checkpoint8_step_is_the_step_of_the_held_values(last_fc):
+    """Gradients with checkpoint8 are those of a backward whose lower layers
+    read the values that their 8-bit checkpoints stand for."""
+    d, _ = case([16, 32, 16], last_fc, 45, (1, 0, 1))
+    say("checkpoint8 step", last_fc)
+    got = step(d, checkpoint8=True)
+    plain = step(d)
+    assert torch.equal(got["p"], plain["p"]) and torch.equal(got["loss"], plain["loss"])
+    top = len(d["layers"]) - 1
+    assert all(torch.equal(a, b) for a, b in zip(got["layers"][top], plain["layers"][top]))     # not held in 8 bits
+    # by hand, from the acts of the forward and the oracle of the codes
+    out = net.network_forward(d["x"], d["layers"], d["fcs"], d["head"], d["labels"], training=True, norms=d["norms"])
+    g = out["dlast"]
+    for li in range(top, -1, -1):
+        act, L = out["acts"][li], d["layers"][li]
+        if li < len(d["fcs"]):
+            h2 = act["h"].view(-1, L.O)
+            dh, w = torch.empty_like(h2), d["fcs"][li][0]
+            P.pyramid_fc_tanh_backward(h2, w, act["y"].view(h2.shape[0], -1), g.view(h2.shape[0], -1), dh,
+                                       torch.empty_like(w), torch.empty(w.shape[0], device=DEV))
+        else:
+            dh = g
+        if "kept" in act:
+            x, _, stats = act["kept"]
+            if li < top:
+                x = R.codes(x.cpu())[2].float().to(DEV)
+            dh, dgamma, dbeta = net.norm_backward((x, None, stats), d["norms"][li][0], dh)
+            assert normwise(host(got["norms"][li][0]), host(dgamma)) <= 1e-6
+            assert normwise(host(got["norms"][li][1]), host(dbeta)) <= 1e-6
+        saved = act["saved"]
+        if li < top:
+            s = P.shape_for(act["in"], L.O, L.K)
+            for a in net._saved_arrays(saved, s):
+                a.copy_(R.codes(a.cpu())[2].float())
+        grads = net.layer_backward(act["in"], L, saved, dh.view(act["h"].shape), want_dx=li > 0)
+        for a, b in zip(got["layers"][li], grads[1:]):
+            assert normwise(host(a), host(b)) <= 1e-5       # the two heads' dh differ in the order of sums
+        g = grads[0]
+
+
+def test_checkpoint8_holds_less():
+    """The forward's acts keep a lower layer's saved buffer in about a quarter of its bytes."""
+    d, _ = case([16, 32, 16], True, 46, (1, 1, 1))
+    out = net.network_forward(d["x"], d["layers"], d["fcs"], d["head"], d["labels"], training=True, norms=d["norms"],
+                              checkpoint8=True)
+    for li, act in enumerate(out["acts"]):
+        size = P.pyramid_lstm_saved_size(P.shape_for(act["in"], d["layers"][li].O))
+        if li == 2:
+            assert act["saved"].numel() == size
+        else:
+            held = sum(t.numel() * t.element_size() for pair in act["packed"] for t in pair)
+            assert act["saved"] is None and held <= 0.26 * size + 1024
+
+
+@pytest.mark.parametrize("axis", ["z", "y", "x"])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_volume_scan_runs_along_its_axis(axis, reverse):
+    gen = torch.Generator().manual_seed(7)
+    shape = (2, 5, 6, 7, 3)
+    g, u, dh = (torch.randn(shape, generator=gen) for _ in range(3))
+    say("volume scan", axis, reverse)
+    h, saved = net.scan_forward(g.to(DEV), u.to(DEV), axis, reverse, training=True)
+    dg, du = net.scan_backward(g.to(DEV), u.to(DEV), saved, dh.to(DEV), axis, reverse)
+    k = {"z": 1, "y": 2, "x": 3}[axis]
+
+    def seq(v):     # sequences along the axis by moving it, not by views of the layout
+        return v.movedim(k, 3).reshape(-1, shape[k], shape[4])
+
+    rh, e, _, _, before, eb = R.scan_forward(seq(g), seq(u), reverse, None, None)
+    (rg, eg), (ru, eu), _ = R.scan_backward(seq(g), seq(u), before, eb, seq(dh), reverse, None, None)
+    for got, ref, err in ((h, rh, e), (dg, rg, eg), (du, ru, eu)):
+        assert ((seq(got.cpu()).double() - ref).abs() <= R.rounded(ref, err, torch.float32)).all()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_block_of_norm_and_six_sweeps(eight):
+    """A pre-normed block: norm, six linear sweeps of the normed volume summed,
+    trained with its inputs held as they are or in 8 bits; against autograd in
+    64 bits of the formulas (on the values that the checkpoints stand for)."""
+    gen = torch.Generator().manual_seed(8)
+    shape, C = (1, 6, 18, 21, 16), 16
+    x, gates, dh = (torch.randn(shape, generator=gen) for _ in range(3))
+    gamma, beta = torch.rand(C, generator=gen) + .5, torch.randn(C, generator=gen) * .1
+    say("block", eight)
+    xd, gd, dhd = x.to(DEV), gates.to(DEV), dh.to(DEV)
+    sweeps = [(a, r) for a in "zyx" for r in (False, True)]
+    y, kept = net.norm_forward(xd, gamma.to(DEV), beta.to(DEV), EPS, True, eight)
+    runs = [net.scan_forward(gd, y, a, r, training=True) for a, r in sweeps]
+    h = sum(t[0] for t in runs)
+    gk, yk = gd, y
+    if eight:
+        gk, yk = P.checkpoint8_empty(gd), P.checkpoint8_empty(y)
+        P.pyramid_checkpoint8_pack(gd, *gk)
+        P.pyramid_checkpoint8_pack(y, *yk)
+    grads = [net.scan_backward(gk, yk, s, dhd, a, r) for (a, r), (_, s) in zip(sweeps, runs)]
+    dg, dy = sum(t[0] for t in grads), sum(t[1] for t in grads)
+    dx, dgamma, dbeta = net.norm_backward(kept, gamma.to(DEV), dy)
+
+    if eight:
+        # the formulas of the backward passes on the values that the checkpoints stand for; states
+        # before every 16th position are the forward's
+        def seq(v, axis):
+            k = {"z": 1, "y": 2, "x": 3}[axis]
+            return v.movedim(k, 3).reshape(-1, shape[k], C)
+
+        def back(v, axis):
+            k = {"z": 1, "y": 2, "x": 3}[axis]
+            moved = torch.empty(shape).movedim(k, 3).shape
+            return v.reshape(moved).movedim(3, k)
+
+        yc = y.cpu()
+        gv, yv = R.codes(gates)[2], R.codes(yc)[2]
+        rdg, rdy = torch.zeros(shape, dtype=torch.float64), torch.zeros(shape, dtype=torch.float64)
+        for a, r in sweeps:
+            _, _, _, _, before, eb = R.scan_forward(seq(gates, a), seq(yc, a), r, None, None)
+            before, eb = R.scan_forward(seq(gv, a), seq(yv, a), r, None, None, run=(before, eb))[4:]
+            (tg, _), (tu, _), _ = R.scan_backward(seq(gv, a), seq(yv, a), before, eb, seq(dh, a), r, None, None)
+            rdg, rdy = rdg + back(tg, a), rdy + back(tu, a)
+        rows = x.view(-1, C)
+        _, _, mean, rstd = R.norm_forward(rows, gamma, beta, EPS, torch.float32)
+        rdx, rga, rbe = R.norm_backward(R.codes(rows)[2], mean, rstd, gamma, rdy.view(-1, C), torch.float32)
+        want = {"dx": rdx[0].view(shape), "dg": rdg, "dgamma": rga[0], "dbeta": rbe[0]}
+    else:
+        leaves = [t.double().requires_grad_() for t in (x, gates, gamma, beta)]
+        xx, gg, ga, be = leaves
+        m = xx.mean(-1, keepdim=True)
+        yy = (xx - m) / torch.sqrt(((xx - m) ** 2).mean(-1, keepdim=True) + EPS) * ga + be
+
+        def sweep(g, u, axis, reverse):
+            k = {"z": 1, "y": 2, "x": 3}[axis]
+            g, u = g.unbind(k), u.unbind(k)
+            v, out = torch.zeros_like(u[0]), []
+            for t in (range(len(u) - 1, -1, -1) if reverse else range(len(u))):
+                f = torch.sigmoid(g[t])
+                v = f * v + (1 - f) * u[t]
+                out.append(v)
+            return torch.stack(out[::-1] if reverse else out, k)
+
+        ref = sum(sweep(gg, yy, a, r) for a, r in sweeps)
+        # 21 steps, each off by (8 + 2 |g|) 2^-24 of its terms: 21 x 16 x 2^-24 = 2e-5 if all added up;
+        # the state forgets half of it a step
+        assert normwise(host(h), ref.detach().numpy()) <= 1e-5
+        ref.backward(dh.double())
+        want = dict(zip(("dx", "dg", "dgamma", "dbeta"), (t.grad for t in leaves)))
+    for name, got in (("dx", dx), ("dg", dg), ("dgamma", dgamma), ("dbeta", dbeta)):
+        assert normwise(host(got), want[name].numpy()) <= 1e-5, name
+
+
+def test_chain_wait_that_gives_up_is_reported():
+    """Failure path of the chained scan, driven by the test mode: every wait
+    gives up at once, the states behind the first chunk are NaN, the status
+    bit is set, and the next call is right again."""
+    gen = torch.Generator().manual_seed(9)
+    g, u = (torch.randn((1, 2000, 70), generator=gen) for _ in range(2))
+    gd, ud, h, hT = g.to(DEV), u.to(DEV), torch.empty((1, 2000, 70), device=DEV), torch.empty((1, 70), device=DEV)
+    saved = torch.empty(P.pyramid_scan_saved_size(1, 2000, 70), dtype=torch.uint8, device=DEV)
+    P.pyramid_lstm_device_status(clear=True)
+    say("chain gives up")
+    try:
+        P.pyramid_lstm_set_wait_test(True)
+        P.pyramid_scan_forward(gd, ud, h, hT=hT, saved=saved)
+        torch.cuda.synchronize()
+    finally:
+        P.pyramid_lstm_set_wait_test(False)
+    assert P.pyramid_lstm_device_status(clear=True) & P.PLSTM_DEVICE_WAIT_GAVE_UP
+    assert torch.isnan(h[0, -1]).all() and torch.isnan(hT).all()
+    P.pyramid_scan_forward(gd, ud, h, hT=hT, saved=saved)
+    ref, e = R.scan_forward(g, u, False, None, None)[:2]
+    assert ((h.cpu().double() - ref).abs() <= R.rounded(ref, e, torch.float32)).all()
+    dg, du, dh0 = torch.empty_like(h), torch.empty_like(h), torch.empty_like(hT)
+    try:
+        P.pyramid_lstm_set_wait_test(True)
+        P.pyramid_scan_backward(gd, ud, saved, h, dg, du, dh0=dh0)
+        torch.cuda.synchronize()
+    finally:
+        P.pyramid_lstm_set_wait_test(False)
+    assert P.pyramid_lstm_device_status(clear=True) & P.PLSTM_DEVICE_WAIT_GAVE_UP
+    assert torch.isnan(dh0).all()
+    P.pyramid_scan_backward(gd, ud, saved, h, dg, du, dh0=dh0)
+    assert torch.isfinite(dg).all() and torch.isfinite(dh0).all() and P.pyramid_lstm_device_status() == 0
