@@ -281,8 +281,9 @@ struct Shared {
 
 // The state before the wave's run, `carry` being the one before the workgroup's
 // first (CHAIN: taken from the chain); carry becomes the one after its last.
-// Every wave of the workgroup is here at once.
-template <int W, bool CHAIN>
+// Every wave of the workgroup is here at once.  U: steps of the folds at a time, which
+// decides the registers.
+template <int W, bool CHAIN, int U>
 __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &ch, long long cols,
                                    const Column &c, int chunk, int wave, int lane, float A, float H,
                                    float &carry)
@@ -294,7 +295,7 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
         const int g = chunk / ch.group, first = g * ch.group, share = ch.group / W;
         if (wave == 0 && chunk + 1 < ch.chunks) {
             float a = 1.0f, h = 0.0f;
-#pragma unroll
+#pragma unroll U
             for (int w = 0; w < W; ++w) {
                 const float2 p = part[w][lane];
                 a *= p.x;
@@ -323,14 +324,14 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
         }
         __syncthreads();
         carry = sh.start[lane];
-#pragma unroll
+#pragma unroll U
         for (int w = 0; w < W; ++w) {
             const float2 p = sh.prev[w][lane];
             carry = fmaf(p.x, carry, p.y);
         }
     }
     float v = carry, at = carry;
-#pragma unroll
+#pragma unroll U
     for (int w = 0; w < W; ++w) {
         const float2 p = part[w][lane];
         at = w == wave ? v : at;
@@ -355,6 +356,10 @@ __global__ void __launch_bounds__(64 * W)
 k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ u,
            const float *h0, T *__restrict__ h, float *hT, float *__restrict__ saved)
 {
+    // bf16: folds by four keep a chained chunk to 64 registers, two workgroups a CU
+    // (65536 steps of 1024 channels 116 -> 101 us); fp32 has as many bytes on the
+    // way with one (16384 steps of 1024 channels 48 us, with two 54)
+    constexpr int folds = CHAIN && sizeof(T) == 2 ? 4 : W;
     __shared__ Shared<W, CHAIN> sh;
     const int lane = threadIdx.x & 63;
     const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
@@ -406,7 +411,7 @@ k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ 
         }
         float st = carry;
         if constexpr (W > 1)
-            st = before_run(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
+            st = before_run<W, CHAIN, folds>(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
         if (saved && count > 0 && c.has) put(saved, c.saved + run * a.I, c.soff, st);
         if (full && c.has) {
 #pragma unroll
@@ -550,7 +555,7 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
                 A *= f[k];
                 H = f[k] * (d[k] + H);
             }
-            cin = before_run(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
+            cin = before_run<W, CHAIN, W>(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
         }
         if (full && c.has) {
 #pragma unroll
