@@ -536,6 +536,17 @@ def _tensor(name, t, shape, dtype, device):
     return t.data_ptr()
 
 
+def _temporary(nbytes, device, stream):
+    """A workspace of the call's stream: memory that torch may give away again
+    once what the stream has by then been told is done."""
+    if stream is None:
+        return _workspace(nbytes, device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device)
+    with torch.cuda.stream(stream):
+        return _workspace(nbytes, device)
+
+
 def _bytes(ws, device):
     if ws.device != device or not ws.is_contiguous():
         raise ValueError("ws must be contiguous and on %s" % device)
@@ -552,16 +563,17 @@ def _run(name, x, stream, *args):
     """Calls entry point `name` with x's device current, on `stream` or that
     device's current stream."""
     dev = x.get_device()
+    fn = getattr(_lib or load(), name)
     if stream is None:
         stream = torch._C._cuda_getCurrentRawStream(dev)
     else:
         stream = _stream(stream)
-    if dev == torch.cuda.current_device():
-        rc = getattr(load(), name)(*args, stream)
+    if dev == torch._C._cuda_getDevice():
+        rc = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            rc = getattr(load(), name)(*args, stream)
-    if rc != 0:
+            rc = fn(*args, stream)
+    if rc:
         raise PyramidLSTMError(name, rc)
 
 
@@ -597,7 +609,7 @@ def pyramid_layer_norm_backward(x, gamma, stats, dy, dx, dgamma, dbeta, xscale=N
     else:
         px, ps = _codes("x", x, xscale, dy, dev)
     if ws is None:
-        ws = _workspace(pyramid_layer_norm_workspace_size(M, C), dev)
+        ws = _temporary(pyramid_layer_norm_workspace_size(M, C), dev, stream)
     _run("pyramid_layer_norm_backward", dy, stream, M, C, dt, px, ps,
          _tensor("gamma", gamma, (C,), dy.dtype, dev),
          _tensor("stats", stats, (M, 2), torch.float32, dev), pdy,
@@ -628,14 +640,14 @@ def _saved(saved, B, T, I, device):
 _scan_ws = {}
 
 
-def _scan_workspace(ws, B, T, I, device):
+def _scan_workspace(ws, B, T, I, device, stream):
     """Pointer and bytes of `ws`, or of one made with torch.  A call that needs
     none takes 256 bytes as every call does, and shares them: it does not touch
     them."""
     if ws is None:
         need = pyramid_scan_workspace_size(B, T, I)
         if need > 256:
-            ws = _workspace(need, device)
+            ws = _temporary(need, device, stream)
         else:
             ws = _scan_ws.get(device)
             if ws is None:
@@ -653,7 +665,7 @@ def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None,
     needs.  ws=None allocates the workspace with torch."""
     (dt, pg), dev = _main("g", g, 3), g.device
     B, T, I = g.shape
-    ws, pws = _scan_workspace(ws, B, T, I, dev)
+    ws, pws = _scan_workspace(ws, B, T, I, dev, stream)
     _run("pyramid_scan_forward", g, stream, B, T, I, dt, int(bool(reverse)), pg,
          _tensor("u", u, g.shape, g.dtype, dev), _tensor("lengths", lengths, (B,), torch.int32, dev),
          _tensor("h0", h0, (B, I), torch.float32, dev), _tensor("h", h, g.shape, g.dtype, dev),
@@ -675,7 +687,7 @@ def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, 
     else:
         pg, pgs = _codes("g", g, gscale, dh, dev)
         pu, pus = _codes("u", u, uscale, dh, dev)
-    ws, pws = _scan_workspace(ws, B, T, I, dev)
+    ws, pws = _scan_workspace(ws, B, T, I, dev, stream)
     _run("pyramid_scan_backward", dh, stream, B, T, I, dt, int(bool(reverse)), pg, pgs, pu, pus,
          _tensor("lengths", lengths, (B,), torch.int32, dev), _saved(saved, B, T, I, dev),
          pdh, _tensor("dhT", dhT, (B, I), torch.float32, dev),
@@ -690,7 +702,7 @@ def pyramid_checkpoint8_scales(n: int) -> int:
 def checkpoint8_empty(x):
     """Uninitialised 8-bit checkpoint of a tensor like x: (codes of x's shape
     int8, scales bf16, one per 64 elements)."""
-    return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
+    return (torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format),
             torch.empty(-(-x.numel() // 64), dtype=torch.bfloat16, device=x.device))
 
 

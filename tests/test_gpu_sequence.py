@@ -560,6 +560,43 @@ def test_operators_in_a_graph_and_on_streams(B, T, I, ckpt, dtype):
     assert all(torch.equal(a, b) for a, b in zip(got[1], want_other))
 
 
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+def test_workspace_belongs_to_the_calls_stream(raw):
+    """A call given another stream than the current one, which is still busy
+    when the call returns: its workspace is not handed to the next tensors of
+    the current stream."""
+    M, C = 4096, 1024
+    x, dy = rand(1, (M, C), F32).to(DEV), rand(2, (M, C), F32).to(DEV)
+    w = [rand(3, (C,), F32, 0.2, 1.0).to(DEV), rand(4, (C,), F32).to(DEV)]
+    g, u = rand(5, (1, 6000, 256), F32).to(DEV), rand(6, (1, 6000, 256), F32).to(DEV)
+    a = torch.randn(4096, 4096, device=DEV)
+
+    def calls(stream):
+        y, stats, dx = torch.empty_like(x), torch.empty((M, 2), device=DEV), torch.empty_like(x)
+        dg, db, h = torch.empty(C, device=DEV), torch.empty(C, device=DEV), torch.empty_like(g)
+        if stream is not None:
+            torch.cuda.synchronize()        # the outputs' memory is free
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    a @ a
+            if raw:
+                stream = stream.cuda_stream
+        P.pyramid_layer_norm_forward(x, w[0], w[1], y, stats, stream=stream)
+        P.pyramid_layer_norm_backward(x, w[0], stats, dy, dx, dg, db, stream=stream)
+        P.pyramid_scan_forward(g, u, h, stream=stream)
+        return [y, dx, dg, db, h]
+
+    want = calls(None)
+    side = torch.cuda.Stream()
+    say("workspace and stream", raw)
+    got = calls(side)
+    junk = [torch.full((P.pyramid_layer_norm_workspace_size(M, C) // 4,), float("nan"), device=DEV),
+            torch.full((P.pyramid_scan_workspace_size(1, 6000, 256) // 4,), float("nan"), device=DEV)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    del junk
+
+
 def test_refusals_of_the_binding():
     """Wrong shapes, types, places and layouts are refused before a launch."""
     x, v = torch.zeros((4, 8), device=DEV), torch.zeros(8, device=DEV)
