@@ -34,18 +34,21 @@ __device__ inline float group_sum(float v, float *lds)
 {
     v = lanes_sum<(G < 64 ? G : 64)>(v);
     if (G <= 64) return v;
-    const int wave = threadIdx.x / 64, first = wave / (G / 64) * (G / 64);
+    constexpr int waves = G > 64 ? G / 64 : 1;
+    const int wave = threadIdx.x / 64, first = wave / waves * waves;
     if ((threadIdx.x & 63) == 0) lds[wave] = v;
     __syncthreads();
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < G / 64; ++w) s += lds[first + w];
+    for (int w = 0; w < waves; ++w) s += lds[first + w];
     return s;
 }
 
-// CODE: also the 8-bit checkpoint of x, where its blocks of 64 elements are
-// aligned lanes of a wave (fused_codes).
-template <typename T, int G, int K, bool CODE>
+// CODE: also the 8-bit checkpoint of x.  1: its blocks of 64 elements are aligned
+// lanes of a wave.  2: they are not, but the rows of a turn are whole blocks: those go
+// through LDS, and lanes take pieces of blocks there.
+enum { kNoCode = 0, kCodeInLanes = 1, kCodeInLds = 2 };
+template <typename T, int G, int K, int CODE>
 __global__ void __launch_bounds__(G > 256 ? G : 256)
 k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__restrict__ beta,
            T *__restrict__ y, float2 *__restrict__ stats, int8_t *__restrict__ xq,
@@ -54,6 +57,7 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
     constexpr int N = Rows<T, G, K>::N, U = Rows<T, G, K>::U;
     constexpr int threads = G > 256 ? G : 256, rows = threads / G;
     __shared__ float lds[2][2][threads / 64];
+    __shared__ __align__(16) T span[CODE == kCodeInLds ? rows * U * G * N : 8];
     const int j = threadIdx.x % G, group = threadIdx.x / G;
     const float inv = 1.0f / (float)C;
     float ga[K][N], be[K][N];
@@ -83,7 +87,13 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
             float v[K][N];
 #pragma unroll
             for (int k = 0; k < K; ++k) Piece<T>::unpack(raw[t][k], v[k]);
-            if (CODE) {
+            if (CODE == kCodeInLds) {
+                const int c = j * N, at = (t * rows + group) * C + c;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (c + i < C) Store<T>::store(span, at + i, v[0][i]);
+            }
+            if (CODE == kCodeInLanes) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     const int c = (j + G * k) * N;
@@ -133,6 +143,25 @@ k_norm_fwd(const T *__restrict__ x, const T *__restrict__ gamma, const T *__rest
                 }
                 if (stats && j == 0) stats[m] = make_float2(mean, rstd);
             }
+        }
+        if (CODE == kCodeInLds) {
+            __syncthreads();
+            const int size = rows * U * C;
+#pragma unroll
+            for (int t = 0; t < U; ++t) {
+                const int e = (t * threads + (int)threadIdx.x) * N;
+                if (e >= size) continue;        // all 64 elements of a block or none
+                float v[N];
+                Piece<T>::unpack(*(const u32x4 *)(span + e), v);
+                const uint16_t s = code_scale(lanes_max<kCodeBlock / N>(top_bits<N>(v)));
+                const Coder cd(s);
+                uint32_t code[N];
+                code_piece<T>(cd, v, code);
+                const long long at = m0 * C + e, left = M * C - at;
+                store_codes<N>(xq + at, left < N ? (int)left : N, code, cd.keep);
+                if (e % kCodeBlock == 0 && left > 0) xscale[at >> 6] = s;
+            }
+            __syncthreads();
         }
     }
 }
@@ -335,27 +364,46 @@ int with_rows(int C, F fn)
     return PLSTM_EUNSUPPORTED;
 }
 
-// Blocks of 64 elements lie in whole rows, or whole rows of pieces in a block.
-template <typename T> bool fused_codes(int C)
+// How the forward codes rows of C elements, G lanes each with U rows in a turn:
+// in its lanes where blocks of 64 elements lie in whole rows or whole rows of pieces in a
+// block; through LDS where a turn's rows are whole blocks (fp32, 360000 rows of 45: 33 us, 41
+// with the pack kernel after it); not at all otherwise.
+template <typename T, int G, int K> constexpr int code_rows() { return (G > 256 ? G : 256) / G * Rows<T, G, K>::U; }
+template <typename T, int G, int K> int code_mode(int C)
 {
-    return C % kCodeBlock == 0 || (kCodeBlock % C == 0 && C >= Piece<T>::N);
+    if (C % kCodeBlock == 0 || (kCodeBlock % C == 0 && C >= Piece<T>::N)) return kCodeInLanes;
+    if (G <= 64 && K == 1 && code_rows<T, G, K>() * C % kCodeBlock == 0) return kCodeInLds;
+    return kNoCode;
 }
 
 template <typename T>
 int norm_forward(long long M, int C, float eps, const T *x, const T *gamma, const T *beta, T *y,
-                 float2 *stats, int8_t *xq, uint16_t *xscale, hipStream_t st)
+                 float2 *stats, int8_t *xq, uint16_t *xscale, int *launches, hipStream_t st)
 {
     return with_rows<T>(C, [&](auto g, auto k) -> int {
         constexpr int G = decltype(g)::value, K = decltype(k)::value;
-        constexpr int threads = G > 256 ? G : 256, rows = threads / G * Rows<T, G, K>::U;
+        constexpr int threads = G > 256 ? G : 256, rows = code_rows<T, G, K>();
         const long long need = (M + rows - 1) / rows;
         const unsigned grid = (unsigned)(need < kNormFwdBlocks ? need : kNormFwdBlocks);
-        if (xq)
-            k_norm_fwd<T, G, K, true><<<grid, threads, 0, st>>>(x, gamma, beta, y, stats, xq,
-                                                               xscale, M, C, eps);
-        else
-            k_norm_fwd<T, G, K, false><<<grid, threads, 0, st>>>(x, gamma, beta, y, stats,
-                                                                nullptr, nullptr, M, C, eps);
+        const int mode = xq ? code_mode<T, G, K>(C) : kNoCode;
+        *launches = 1;
+        if (mode == kCodeInLanes) {
+            k_norm_fwd<T, G, K, kCodeInLanes><<<grid, threads, 0, st>>>(
+                x, gamma, beta, y, stats, xq, xscale, M, C, eps);
+        } else if (mode == kCodeInLds) {
+            if constexpr (G <= 64 && K == 1)
+                k_norm_fwd<T, G, K, kCodeInLds><<<grid, threads, 0, st>>>(
+                    x, gamma, beta, y, stats, xq, xscale, M, C, eps);
+        } else {
+            k_norm_fwd<T, G, K, kNoCode><<<grid, threads, 0, st>>>(x, gamma, beta, y, stats,
+                                                                  nullptr, nullptr, M, C, eps);
+            if (xq) {
+                PLSTM_LAUNCH_CHECK();
+                *launches = 2;
+                return checkpoint8_pack(M * C, sizeof(T) == 4 ? PLSTM_F32 : PLSTM_BF16, x, xq,
+                                        xscale, st);
+            }
+        }
         PLSTM_LAUNCH_CHECK();
         return PLSTM_OK;
     });
@@ -434,20 +482,15 @@ int pyramid_layer_norm_forward(int64_t M, int32_t C, int32_t dtype, float eps, c
         return PLSTM_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     timing_begin("norm_fwd", st);
-    const bool fused = dtype == PLSTM_F32 ? fused_codes<float>(C) : fused_codes<uint16_t>(C);
-    if (xq && !fused) {
-        rc = checkpoint8_pack((long long)M * C, dtype, x, (int8_t *)xq, (uint16_t *)xscale, st);
-        if (rc != PLSTM_OK) return rc;
-    }
-    int8_t *q = fused ? (int8_t *)xq : nullptr;
+    int launches = 0;
     rc = dtype == PLSTM_F32
              ? norm_forward(M, C, eps, (const float *)x, (const float *)gamma,
-                            (const float *)beta, (float *)y, (float2 *)stats, q,
-                            (uint16_t *)xscale, st)
+                            (const float *)beta, (float *)y, (float2 *)stats, (int8_t *)xq,
+                            (uint16_t *)xscale, &launches, st)
              : norm_forward(M, C, eps, (const uint16_t *)x, (const uint16_t *)gamma,
-                            (const uint16_t *)beta, (uint16_t *)y, (float2 *)stats, q,
-                            (uint16_t *)xscale, st);
-    if (rc == PLSTM_OK) timing_end(xq && !fused ? 2 : 1, st);
+                            (const uint16_t *)beta, (uint16_t *)y, (float2 *)stats, (int8_t *)xq,
+                            (uint16_t *)xscale, &launches, st);
+    if (rc == PLSTM_OK) timing_end(launches, st);
     return rc;
 }
 

@@ -110,7 +110,9 @@ def test_norm_rows(M, C, dtype):
 
 @DTYPES
 @pytest.mark.parametrize("M,C", [(1, 1), (7, 1), (65, 3), (33, 8), (9, 16), (130, 16), (50, 32), (77, 64), (20, 45),
-                                 (31, 128), (12, 192), (9, 320), (6, 1024), (3, 2048), (3, 5000), (2, 8192), (2, 16384)])
+                                 (31, 128), (12, 192), (9, 320), (6, 1024), (3, 2048), (3, 5000), (2, 8192), (2, 16384),
+                                 (300, 45), (64, 45), (65, 25), (1000, 5), (513, 7), (129, 12), (200, 63), (100, 33),
+                                 (70, 90), (65, 100), (33, 130), (40, 250), (30, 131), (600, 2), (257, 17), (90, 500)])
 def test_norm_from_checkpoint(M, C, dtype):
     say("norm ckpt", M, C, dtype)
     norm_step(M, C, dtype, ckpt=True, seed=M + C)
