@@ -394,7 +394,8 @@ int pyramid_stitch_finish(int32_t D, int32_t H, int32_t W, int32_t K, const void
 /* Slices of larger tensors (the next token's rows) are ordinary arguments here:
  * tensors of `dtype`, states, lengths, dgamma and dbeta are aligned to their
  * element, stats to 8 bytes; saved, ws and the codes and scales of 8-bit
- * checkpoints (and what is packed into them or unpacked) to 16 bytes. */
+ * checkpoints (and what is packed into them or unpacked) to 16 bytes.
+ * Outputs overlap neither inputs nor each other, but where it says so. */
 
 /* Layer norm over the C channels of each of M rows (voxels, tokens):
  *   mean = sum_c x / C, var = sum_c (x - mean)^2 / C, rstd = 1/sqrt(var + eps),
@@ -434,7 +435,8 @@ int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void 
  * (clamped to 0..T; T where lengths is NULL), position s = 0..n-1 is step
  * t = s, or n - 1 - s with reverse = 1:
  *   f = sigmoid(g[b][t]),  h_s = f h_{s-1} + (1 - f) u[b][t],  h_{-1} = h0[b],
- * per channel.  Steps t >= n hold nothing: they are not read, h there is 0.
+ * per channel.  Steps t >= n hold nothing: what g and u have there does not
+ * matter, h there is 0.
  * Any axis of a channels-last volume is such a tensor: z of [N][D][H][W][O]
  * is [N][D][H W O], y is [N D][H][W O], x is [N D H][W][O].
  *   g, u, h     : [B][T][I] in `dtype`; h overwritten.

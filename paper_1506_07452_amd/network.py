@@ -254,10 +254,12 @@ def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch
 
 
 def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
-    """Layer li and its norm on input a: 'h' is what the FC reads; for training
+    """Layer li and its norm on input a (norms: one entry per layer): 'h' is what the FC reads; for training
     'saved' and, with a norm, 'kept'.  With checkpoint8 a layer below the last
     one keeps its saved buffer, and its norm's input, in 8 bits ('packed'): until
     its backward they lie idle."""
+    if norms is not None and len(norms) != len(layers):
+        raise ValueError("norms must have an entry (gamma, beta) or None per layer")
     L = layers[li]
     eight = training and checkpoint8 and li < len(layers) - 1
     h, saved = layer_forward(a, L, training, ws, stream)

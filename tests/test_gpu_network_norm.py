@@ -111,6 +111,15 @@ def test_normed_training_step_matches_oracle(last_fc, fused, normed):
     assert [g.shape for g in grads] == [p.shape for p in params]
 
 
+def test_norms_have_to_be_one_per_layer():
+    d, _ = case([16, 32], True, 42, (1, 1))
+    for norms in (d["norms"][:1], d["norms"] + [None]):
+        with pytest.raises(ValueError):
+            net.network_forward(d["x"], d["layers"], d["fcs"], d["head"], norms=norms)
+        with pytest.raises(ValueError):
+            net.network_train_step(d["x"], d["layers"], d["fcs"], d["head"], d["labels"], norms=norms)
+
+
 def test_network_without_norms_is_as_before():
     d, _ = case([16, 32], True, 43, (0, 0))
     a = net.network_train_step(d["x"], d["layers"], d["fcs"], d["head"], d["labels"])
