@@ -18,6 +18,7 @@
 namespace plstm {
 namespace {
 
+constexpr int kChainWaves = 16;     // waves of a chained workgroup, at most
 constexpr int kRun = 16;            // positions between kept states, and of a wave's run
 constexpr int kGroup = 16;          // chunks between chained states, at least
 constexpr uint64_t kEmpty = ~0ull;  // a word that its chunk has not written
@@ -372,6 +373,7 @@ k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ 
         const int count = run < a.runs ? (int)min((long long)kRun, a.T - s0) : 0;
         const RunAt<RAGGED> at(a, c, s0);
         const bool full = count == kRun && (!RAGGED || __all(at.live == kRun));
+        const bool any = count > 0 && (!RAGGED || !__all(at.live == 0));
         float f[kRun], v[kRun];
         if (full) {
 #pragma unroll
@@ -386,7 +388,7 @@ k_scan_fwd(ScanArgs a, Chain ch, const T *__restrict__ g, const T *__restrict__ 
                 f[k] = __builtin_inff();
                 v[k] = 0.0f;
             }
-            if (count > 0) {
+            if (any) {
 #pragma unroll
                 for (int k = 0; k < kRun; ++k) {
                     long long b;
@@ -501,6 +503,7 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
         const int count = run >= 0 ? (int)min((long long)kRun, a.T - s0) : 0;
         const RunAt<RAGGED> at(a, c, s0);
         const bool full = count == kRun && (!RAGGED || __all(at.live == kRun));
+        const bool any = count > 0 && (!RAGGED || !__all(at.live == 0));
         float f[kRun], k1[kRun], d[kRun], v[kRun];      // f, 1 - f, dh, h before - u
         float st = 0.0f;
         if (count > 0) st = value<float>(get(saved, c.saved + run * a.I, c.soff));
@@ -522,7 +525,7 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
                 f[k] = __builtin_inff();
                 v[k] = d[k] = 0.0f;
             }
-            if (count > 0) {
+            if (any) {
 #pragma unroll
                 for (int k = 0; k < kRun; ++k) {
                     long long b;
@@ -555,7 +558,7 @@ k_scan_bwd(ScanArgs a, Chain ch, const X *__restrict__ g, const uint16_t *__rest
                 A *= f[k];
                 H = f[k] * (d[k] + H);
             }
-            cin = before_run<W, CHAIN, W>(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
+            cin = before_run<W, CHAIN, CHAIN && W == kChainWaves ? 4 : W>(sh, turn, ch, a.cols, c, chunk, wave, lane, A, H, carry);
         }
         if (full && c.has) {
 #pragma unroll
@@ -596,8 +599,10 @@ int check_scan(int64_t B, int64_t T, int64_t I, int32_t dtype)
 constexpr int kWaves = 8, kFewWaves = 4;
 // Waves of a chained chunk of the forward: sixteen, so half the links, and one
 // workgroup a CU (bf16, 16384 steps of 1024 channels: 31 us; with eight, four
-// workgroups a CU, 39).  The backward's registers do not leave room for them.
-constexpr int kChainWaves = 16;
+// workgroups a CU, 39).  The backward's registers leave room for one such workgroup a
+// CU, or two of eight: sixteen while that is at most two rounds of the card (bf16, 4096
+// steps of 2048 channels 28 -> 25 us), else eight (two sequences of 8192 steps 88 and 80).
+constexpr long long kShortChain = 512;
 // Columns from which a card is filled without chains: at 16384 (fp32, eight sequences of
 // 2048 steps of 2048 channels) 88 us, 97 chained; at 4096 189 and 93.
 constexpr long long kChainCols = 16384;
@@ -606,13 +611,13 @@ constexpr long long kChainCols = 16384;
 struct Plan {
     ScanArgs a;
     long long blocks;               // workgroups across the columns
-    int waves;
+    int waves, chain_waves;
     Chain ch;                       // chunks 0: none
     size_t ws;
 };
 
 Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *lengths, void *ws,
-               int chain_waves = kWaves)
+               bool backward)
 {
     Plan p{};
     p.a = ScanArgs{T, I, B * I, reverse, lengths, (T + kRun - 1) / kRun, 0};
@@ -624,7 +629,9 @@ Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *
         p.a.across = (I + 63) / 64;
         p.blocks = B * p.a.across;
     }
-    const long long chunks = (p.a.runs + chain_waves - 1) / chain_waves;
+    const long long few = (p.a.runs + kChainWaves - 1) / kChainWaves;
+    p.chain_waves = backward && few * p.blocks > kShortChain ? kWaves : kChainWaves;
+    const long long chunks = (p.a.runs + p.chain_waves - 1) / p.chain_waves;
     p.waves = p.a.runs == 1 ? 1 : p.a.runs <= kFewWaves ? kFewWaves : kWaves;
     Carve cv(ws);
     if (chunks > 1 && p.a.cols < kChainCols && chunks * p.blocks <= (1 << 21)) {
@@ -701,7 +708,10 @@ int scan_backward(Plan &p, const void *g, const void *gscale, const void *u, con
     if (p.ch.chunks) {
         const int rc = start_chain(p, (const float *)dhT, st);
         if (rc != PLSTM_OK) return rc;
-        launch_bwd<T, X, kWaves, RAGGED, true>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
+        if (p.chain_waves == kChainWaves)
+            launch_bwd<T, X, kChainWaves, RAGGED, true>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
+        else
+            launch_bwd<T, X, kWaves, RAGGED, true>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
     } else if (p.waves == kWaves) {
         launch_bwd<T, X, kWaves, RAGGED, false>(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
     } else if (p.waves == kFewWaves) {
@@ -729,7 +739,9 @@ size_t pyramid_scan_saved_size(int64_t B, int64_t T, int64_t I)
 size_t pyramid_scan_workspace_size(int64_t B, int64_t T, int64_t I)
 {
     if (check_scan(B, T, I, PLSTM_F32) != PLSTM_OK) return 0;
-    return scan_plan(B, T, I, 0, nullptr, nullptr).ws;
+    const size_t f = scan_plan(B, T, I, 0, nullptr, nullptr, false).ws;
+    const size_t b = scan_plan(B, T, I, 0, nullptr, nullptr, true).ws;
+    return f > b ? f : b;
 }
 
 int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t reverse,
@@ -745,7 +757,7 @@ int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t
         return PLSTM_EINVAL;
     if (ws_bytes < pyramid_scan_workspace_size(B, T, I)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    Plan p = scan_plan(B, T, I, reverse, lengths, ws, kChainWaves);
+    Plan p = scan_plan(B, T, I, reverse, lengths, ws, false);
     timing_begin("scan_fwd", st);
     rc = dtype == PLSTM_F32
              ? (lengths ? scan_forward<float, true> : scan_forward<float, false>)(p, g, u, h0, h, hT,
@@ -775,7 +787,7 @@ int pyramid_scan_backward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_
         return PLSTM_EINVAL;
     if (ws_bytes < pyramid_scan_workspace_size(B, T, I)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
-    Plan p = scan_plan(B, T, I, reverse, lengths, ws);
+    Plan p = scan_plan(B, T, I, reverse, lengths, ws, true);
     timing_begin("scan_bwd", st);
     const auto run = [&](auto fn) {
         return fn(p, g, gscale, u, uscale, saved, dh, dhT, dg, du, dh0, st);
