@@ -466,7 +466,9 @@ int pyramid_scan_forward(int64_t B, int64_t T, int64_t I, int32_t dtype, int32_t
  *   g, u        : the forward's, in `dtype` (gscale and uscale NULL), or codes of
  *                 8-bit checkpoints with their scales (both coded): f, u and
  *                 the states between kept ones are then those of the codes'
- *                 values.
+ *                 values.  Blocks of codes know no lengths: padding that
+ *                 shares one with steps has to be finite, and so have gates
+ *                 (an infinite one, f = 0 or 1, makes its block NaN).
  *   saved       : the forward's.   lengths, reverse: the forward's.
  *   dh          : [B][T][I] in `dtype`;  dhT: NULL (zeros), or fp32 [B][I].
  *   dg, du      : [B][T][I] in `dtype`, overwritten.

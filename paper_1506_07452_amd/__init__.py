@@ -507,31 +507,34 @@ def pyramid_stitch_finish(acc, wsum, out, stream=None):
 
 
 # The operators below run down to a few microseconds, so their marshalling keeps
-# to plain integers: data_ptr() and the raw stream instead of ctypes and torch
-# objects, and no device switch where the tensors' device is current.
+# to plain integers: data_ptr(), device numbers and the raw stream instead of ctypes
+# and torch objects, and no device switch where the tensors' device is current.
 def _main(name, t, dims):
-    """Storage type code and pointer of an operator's main tensor of `dims` dimensions (None: any)."""
+    """Storage type code, pointer and device number of an operator's main tensor of
+    `dims` dimensions (None: any)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("expected a torch.Tensor, got %r" % type(t))
-    if t.dtype not in _DT or dims not in (None, t.dim()):
+    code = _DT.get(t.dtype)
+    if code is None or dims not in (None, t.dim()):
         raise ValueError("%s must be float32 or bfloat16%s" % (
             name, "" if dims is None else " with %d dimensions" % dims))
     if not t.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    return _DT[t.dtype], t.data_ptr()
+    return code, t.data_ptr(), t.get_device()
 
 
-def _tensor(name, t, shape, dtype, device):
+def _tensor(name, t, shape, dtype, dev):
     """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
     if t is None:
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError("expected a torch.Tensor, got %r" % type(t))
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be %s %s on %s and contiguous, got %s %s on %s%s" % (
-            name, dtype, list(shape), device, t.dtype, list(t.shape), t.device,
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.get_device() != dev or \
+            not t.is_contiguous():
+        raise ValueError("%s must be %s %s on cuda:%d and contiguous, got %s %s on %s%s" % (
+            name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device,
             "" if t.is_contiguous() else ", not contiguous"))
     return t.data_ptr()
 
@@ -547,22 +550,21 @@ def _temporary(nbytes, device, stream):
         return _workspace(nbytes, device)
 
 
-def _bytes(ws, device):
-    if ws.device != device or not ws.is_contiguous():
-        raise ValueError("ws must be contiguous and on %s" % device)
+def _bytes(ws, dev):
+    if not ws.is_cuda or ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous and on cuda:%d" % dev)
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _codes(name, q, scale, x, device):
+def _codes(name, q, scale, x, dev):
     """Pointers of an 8-bit checkpoint of a tensor of x's shape."""
-    return (_tensor(name, q, x.shape, torch.int8, device),
-            _tensor(name + "'s scale", scale, (-(-x.numel() // 64),), torch.bfloat16, device))
+    return (_tensor(name, q, x.shape, torch.int8, dev),
+            _tensor(name + "'s scale", scale, (-(-x.numel() // 64),), torch.bfloat16, dev))
 
 
-def _run(name, x, stream, *args):
-    """Calls entry point `name` with x's device current, on `stream` or that
+def _run(name, dev, stream, *args):
+    """Calls entry point `name` with device `dev` current, on `stream` or that
     device's current stream."""
-    dev = x.get_device()
     fn = getattr(_lib or load(), name)
     if stream is None:
         stream = torch._C._cuda_getCurrentRawStream(dev)
@@ -586,12 +588,12 @@ def pyramid_layer_norm_forward(x, gamma, beta, y, stats=None, xq=None, xscale=No
     """Layer norm of the rows of x [M][C] (gamma, beta [C], y [M][C], one
     dtype).  stats [M][2] fp32 takes each row's (mean, rstd) for the backward;
     xq, xscale (see checkpoint8_empty) take x's 8-bit checkpoint."""
-    (dt, px), dev = _main("x", x, 2), x.device
+    dt, px, dev = _main("x", x, 2)
     M, C = x.shape
     if (xq is None) != (xscale is None):
         raise ValueError("xq and xscale go together")
     q, qs = _codes("xq", xq, xscale, x, dev) if xq is not None else (None, None)
-    _run("pyramid_layer_norm_forward", x, stream, M, C, dt, eps, px,
+    _run("pyramid_layer_norm_forward", dev, stream, M, C, dt, eps, px,
          _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
          _tensor("y", y, x.shape, x.dtype, dev), _tensor("stats", stats, (M, 2), torch.float32, dev),
          q, qs)
@@ -602,15 +604,15 @@ def pyramid_layer_norm_backward(x, gamma, stats, dy, dx, dgamma, dbeta, xscale=N
     """Gradients of pyramid_layer_norm_forward: dx [M][C] (or None), dgamma and
     dbeta [C] fp32, from dy [M][C] and the forward's input x, or its codes x
     with their scales xscale."""
-    (dt, pdy), dev = _main("dy", dy, 2), dy.device
+    dt, pdy, dev = _main("dy", dy, 2)
     M, C = dy.shape
     if xscale is None:
         px, ps = _tensor("x", x, dy.shape, dy.dtype, dev), None
     else:
         px, ps = _codes("x", x, xscale, dy, dev)
     if ws is None:
-        ws = _temporary(pyramid_layer_norm_workspace_size(M, C), dev, stream)
-    _run("pyramid_layer_norm_backward", dy, stream, M, C, dt, px, ps,
+        ws = _temporary(pyramid_layer_norm_workspace_size(M, C), dy.device, stream)
+    _run("pyramid_layer_norm_backward", dev, stream, M, C, dt, px, ps,
          _tensor("gamma", gamma, (C,), dy.dtype, dev),
          _tensor("stats", stats, (M, 2), torch.float32, dev), pdy,
          _tensor("dx", dx, dy.shape, dy.dtype, dev),
@@ -628,31 +630,32 @@ def pyramid_scan_saved_size(B: int, T: int, I: int) -> int:
     return int(load().pyramid_scan_saved_size(B, T, I))
 
 
-def _saved(saved, B, T, I, device):
+def _saved(saved, B, T, I, dev):
     if saved is None:
         return None
-    if saved.device != device or not saved.is_contiguous() or \
+    if not saved.is_cuda or saved.get_device() != dev or not saved.is_contiguous() or \
             saved.numel() * saved.element_size() < pyramid_scan_saved_size(B, T, I):
-        raise ValueError("saved must hold pyramid_scan_saved_size bytes on %s" % device)
+        raise ValueError("saved must hold pyramid_scan_saved_size bytes on cuda:%d" % dev)
     return saved.data_ptr()
 
 
 _scan_ws = {}
 
 
-def _scan_workspace(ws, B, T, I, device, stream):
-    """Pointer and bytes of `ws`, or of one made with torch.  A call that needs
-    none takes 256 bytes as every call does, and shares them: it does not touch
-    them."""
+def _scan_workspace(ws, x, dev, stream):
+    """`ws`, or one made with torch, its pointer and its bytes.  A call that
+    needs none takes 256 bytes as every call does, and shares them: it does not
+    touch them."""
     if ws is None:
-        need = pyramid_scan_workspace_size(B, T, I)
-        if need > 256:
-            ws = _temporary(need, device, stream)
-        else:
-            ws = _scan_ws.get(device)
-            if ws is None:
-                ws = _scan_ws[device] = _workspace(256, device)
-    return ws, _bytes(ws, device)
+        need = pyramid_scan_workspace_size(*x.shape)
+        if need <= 256:
+            shared = _scan_ws.get(dev)
+            if shared is None:
+                ws = _workspace(256, x.device)
+                shared = _scan_ws[dev] = (ws,) + _bytes(ws, dev)
+            return shared
+        ws = _temporary(need, x.device, stream)
+    return (ws,) + _bytes(ws, dev)
 
 
 def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None, saved=None,
@@ -663,13 +666,13 @@ def pyramid_scan_forward(g, u, h, reverse=False, lengths=None, h0=None, hT=None,
     number of steps; h0, hT [B][I] fp32 are the state before and after (hT may
     be h0); saved (pyramid_scan_saved_size bytes) keeps what the backward
     needs.  ws=None allocates the workspace with torch."""
-    (dt, pg), dev = _main("g", g, 3), g.device
+    dt, pg, dev = _main("g", g, 3)
     B, T, I = g.shape
-    ws, pws = _scan_workspace(ws, B, T, I, dev, stream)
-    _run("pyramid_scan_forward", g, stream, B, T, I, dt, int(bool(reverse)), pg,
+    ws, pws, nws = _scan_workspace(ws, g, dev, stream)
+    _run("pyramid_scan_forward", dev, stream, B, T, I, dt, int(bool(reverse)), pg,
          _tensor("u", u, g.shape, g.dtype, dev), _tensor("lengths", lengths, (B,), torch.int32, dev),
          _tensor("h0", h0, (B, I), torch.float32, dev), _tensor("h", h, g.shape, g.dtype, dev),
-         _tensor("hT", hT, (B, I), torch.float32, dev), _saved(saved, B, T, I, dev), *pws)
+         _tensor("hT", hT, (B, I), torch.float32, dev), _saved(saved, B, T, I, dev), pws, nws)
 
 
 def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, dhT=None, dh0=None,
@@ -677,7 +680,7 @@ def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, 
     """Gradients of pyramid_scan_forward: dg, du [B][T][I] and dh0 [B][I] fp32
     (or None) from dh, dhT (or None) and the forward's inputs and saved
     buffer; g and u may be codes with their scales gscale and uscale."""
-    (dt, pdh), dev = _main("dh", dh, 3), dh.device
+    dt, pdh, dev = _main("dh", dh, 3)
     B, T, I = dh.shape
     if (gscale is None) != (uscale is None):
         raise ValueError("g and u are both coded or neither")
@@ -687,12 +690,12 @@ def pyramid_scan_backward(g, u, saved, dh, dg, du, reverse=False, lengths=None, 
     else:
         pg, pgs = _codes("g", g, gscale, dh, dev)
         pu, pus = _codes("u", u, uscale, dh, dev)
-    ws, pws = _scan_workspace(ws, B, T, I, dev, stream)
-    _run("pyramid_scan_backward", dh, stream, B, T, I, dt, int(bool(reverse)), pg, pgs, pu, pus,
+    ws, pws, nws = _scan_workspace(ws, dh, dev, stream)
+    _run("pyramid_scan_backward", dev, stream, B, T, I, dt, int(bool(reverse)), pg, pgs, pu, pus,
          _tensor("lengths", lengths, (B,), torch.int32, dev), _saved(saved, B, T, I, dev),
          pdh, _tensor("dhT", dhT, (B, I), torch.float32, dev),
          _tensor("dg", dg, dh.shape, dh.dtype, dev), _tensor("du", du, dh.shape, dh.dtype, dev),
-         _tensor("dh0", dh0, (B, I), torch.float32, dev), *pws)
+         _tensor("dh0", dh0, (B, I), torch.float32, dev), pws, nws)
 
 
 def pyramid_checkpoint8_scales(n: int) -> int:
@@ -708,16 +711,16 @@ def checkpoint8_empty(x):
 
 def pyramid_checkpoint8_pack(x, q, scale, stream=None):
     """Codes q (x's shape, int8) and scales of x (float32 or bfloat16, any shape)."""
-    dt, px = _main("x", x, None)
-    pq, ps = _codes("q", q, scale, x, x.device)
-    _run("pyramid_checkpoint8_pack", x, stream, x.numel(), dt, px, pq, ps)
+    dt, px, dev = _main("x", x, None)
+    pq, ps = _codes("q", q, scale, x, dev)
+    _run("pyramid_checkpoint8_pack", dev, stream, x.numel(), dt, px, pq, ps)
 
 
 def pyramid_checkpoint8_unpack(q, scale, x, stream=None):
     """x (float32 or bfloat16, q's shape) = the values of a checkpoint."""
-    dt, px = _main("x", x, None)
-    pq, ps = _codes("q", q, scale, x, x.device)
-    _run("pyramid_checkpoint8_unpack", x, stream, x.numel(), dt, pq, ps, px)
+    dt, px, dev = _main("x", x, None)
+    pq, ps = _codes("q", q, scale, x, dev)
+    _run("pyramid_checkpoint8_unpack", dev, stream, x.numel(), dt, pq, ps, px)
 
 
 def pyramid_lstm_timing_enable(on: bool) -> None:
