@@ -253,6 +253,15 @@ def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch
     return out
 
 
+def _until_read(t, stream):
+    """Before t is dropped here: its memory is not given to another tensor until what
+    `stream` has been told by then is done."""
+    if stream is not None and t is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), t.device)
+        t.record_stream(stream)
+
+
 def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
     """Layer li and its norm on input a (norms: one entry per layer): 'h' is what the FC reads; for training
     'saved' and, with a norm, 'kept'.  With checkpoint8 a layer below the last
@@ -267,9 +276,11 @@ def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
     if eight:
         act["packed"] = saved_pack(saved, shape_for(a, L.O, L.K), stream)
         act["saved"] = None
+        _until_read(saved, stream)
     if norms is not None and norms[li] is not None:
         act["h"], act["kept"] = norm_forward(h, *norms[li], training=training, checkpoint8=eight,
                                              stream=stream)
+        _until_read(h, stream)
     return act
 
 
@@ -285,6 +296,10 @@ def _layer_act_backward(act, li, layers, norms, dh, ws, stream):
         saved = saved_unpack(act["packed"], shape_for(act["in"], L.O, L.K), stream)
     dx, dwx, dwh, db = layer_backward(act["in"], L, saved, dh.view(act["h"].shape),
                                       want_dx=li > 0, ws=ws, stream=stream)
+    if "kept" in act:
+        _until_read(dh, stream)
+    if "packed" in act:
+        _until_read(saved, stream)
     return dx, (dwx, dwh, db), dn
 
 

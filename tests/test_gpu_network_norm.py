@@ -324,3 +324,38 @@ def test_chain_wait_that_gives_up_is_reported():
     assert torch.isnan(dh0).all()
     P.pyramid_scan_backward(gd, ud, saved, h, dg, du, dh0=dh0)
     assert torch.isfinite(dg).all() and torch.isfinite(dh0).all() and P.pyramid_lstm_device_status() == 0
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+@pytest.mark.parametrize("training", [False, True])
+def test_dropped_tensors_belong_to_the_calls_stream(training, raw):
+    """A forward on another stream than the current one, still busy when the call
+    returns: what the norms and the 8-bit checkpoints dropped is not handed to the
+    next tensors of the current stream."""
+    d, _ = case([16, 32, 16], True, 47, (1, 1, 1))
+    N, D, H, W, _ = d["x"].shape
+    ws = net.workspace_for(d["x"].shape, [16, 32, 16], True, torch.float32, training, DEV)
+    a = torch.randn(4096, 4096, device=DEV)
+    kw = dict(norms=d["norms"], training=training, checkpoint8=training, ws=ws)
+    args = (d["x"], d["layers"], d["fcs"], d["head"], d["labels"])
+    want = net.network_forward(*args, **kw)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    say("dropped tensors and stream", training, raw)
+    with torch.cuda.stream(side):
+        for _ in range(40):
+            a @ a
+    got = net.network_forward(*args, stream=side.cuda_stream if raw else side, **kw)
+    junk = []
+    for li, L in enumerate(d["layers"]):
+        shape = P.shape_for(got["acts"][li]["in"], L.O, L.K)
+        for _ in range(4):
+            junk.append(torch.full((N, D, H, W, L.O), float("nan"), device=DEV))
+            junk.append(torch.full((P.pyramid_lstm_saved_size(shape) // 4,), float("nan"), device=DEV))
+    torch.cuda.synchronize()
+    assert torch.equal(got["p"], want["p"]) and torch.equal(got["loss"], want["loss"])
+    for g, w in zip(got["acts"], want["acts"]):
+        assert torch.equal(g["h"], w["h"])
+        for (gq, gs), (wq, ws_) in zip(g.get("packed", ()), w.get("packed", ())):
+            assert torch.equal(gq, wq) and torch.equal(gs, ws_)
+    del junk
