@@ -219,6 +219,13 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _torch_stream(stream, device):
+    """A stream argument (torch's or a handle) as a torch stream."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
+
+
 def _check(fn, rc):
     if rc != 0:
         raise PyramidLSTMError(fn, rc)
@@ -544,9 +551,7 @@ def _temporary(nbytes, device, stream):
     once what the stream has by then been told is done."""
     if stream is None:
         return _workspace(nbytes, device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         return _workspace(nbytes, device)
 
 

@@ -10,12 +10,14 @@ backward in 8 bits (`checkpoint8`).
 """
 from __future__ import annotations
 
+import functools
+import inspect
 from dataclasses import dataclass
 from typing import List, Optional, Tuple
 
 import torch
 
-from . import (checkpoint8_empty, plstm_shape, pyramid_checkpoint8_pack,
+from . import (_torch_stream, checkpoint8_empty, plstm_shape, pyramid_checkpoint8_pack,
                pyramid_checkpoint8_unpack, pyramid_fc_tanh_backward, pyramid_fc_tanh_forward,
                pyramid_head_forward, pyramid_head_forward_supported,
                pyramid_head_train, pyramid_head_workspace_size, pyramid_layer_norm_backward,
@@ -193,6 +195,37 @@ def workspace_for_layers(x_shape, shapes, dtype, training: bool, device):
     return torch.empty(need, dtype=torch.uint8, device=device)
 
 
+def _tensors(out):
+    """The tensors in a result, however deep."""
+    if isinstance(out, torch.Tensor):
+        yield out
+    elif isinstance(out, (dict, list, tuple)):
+        for v in out.values() if isinstance(out, dict) else out:
+            yield from _tensors(v)
+
+
+def _on_its_stream(fn):
+    """A network call given `stream` takes all its memory from that stream: what it
+    drops on its way or when it returns goes to later work of that stream alone,
+    never to tensors that another stream may write while the call's work has yet to
+    read them.  What it returns is the caller's current stream's as well."""
+    at = list(inspect.signature(fn).parameters).index("stream")
+
+    @functools.wraps(fn)
+    def call(x, *args, **kw):
+        stream = args[at - 1] if len(args) >= at else kw.get("stream")
+        if stream is None:
+            return fn(x, *args, **kw)
+        caller = torch.cuda.current_stream(x.device)
+        with torch.cuda.stream(_torch_stream(stream, x.device)):
+            out = fn(x, *args, **kw)
+        for t in _tensors(out):
+            t.record_stream(caller)
+        return out
+    return call
+
+
+@_on_its_stream
 def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch.Tensor]],
                     head: Tuple[torch.Tensor, torch.Tensor], labels: Optional[torch.Tensor] = None,
                     training: bool = False, ws=None, stream=None, loss: str = "ce", norms=None,
@@ -253,15 +286,6 @@ def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch
     return out
 
 
-def _until_read(t, stream):
-    """Before t is dropped here: its memory is not given to another tensor until what
-    `stream` has been told by then is done."""
-    if stream is not None and t is not None:
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream), t.device)
-        t.record_stream(stream)
-
-
 def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
     """Layer li and its norm on input a (norms: one entry per layer): 'h' is what the FC reads; for training
     'saved' and, with a norm, 'kept'.  With checkpoint8 a layer below the last
@@ -276,11 +300,9 @@ def _layer_act(a, li, layers, norms, training, checkpoint8, ws, stream):
     if eight:
         act["packed"] = saved_pack(saved, shape_for(a, L.O, L.K), stream)
         act["saved"] = None
-        _until_read(saved, stream)
     if norms is not None and norms[li] is not None:
         act["h"], act["kept"] = norm_forward(h, *norms[li], training=training, checkpoint8=eight,
                                              stream=stream)
-        _until_read(h, stream)
     return act
 
 
@@ -296,13 +318,10 @@ def _layer_act_backward(act, li, layers, norms, dh, ws, stream):
         saved = saved_unpack(act["packed"], shape_for(act["in"], L.O, L.K), stream)
     dx, dwx, dwh, db = layer_backward(act["in"], L, saved, dh.view(act["h"].shape),
                                       want_dx=li > 0, ws=ws, stream=stream)
-    if "kept" in act:
-        _until_read(dh, stream)
-    if "packed" in act:
-        _until_read(saved, stream)
     return dx, (dwx, dwh, db), dn
 
 
+@_on_its_stream
 def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused_head=True,
                        loss="ce", norms=None, checkpoint8=False):
     """Forward + back-propagation through the whole network (fp32).
@@ -440,6 +459,7 @@ def grid_axis(extent, size, stride):
     return [min(i * stride, span) for i in range(n)], size
 
 
+@_on_its_stream
 def network_infer_volume(x, layers, fcs, head, tile, stride=None, sigma_scale=0.25, ws=None,
                          stream=None, origins=None, norms=None):
     """Class probabilities [N][D][H][W][K] of a volume processed as sub-volumes
