@@ -255,6 +255,16 @@ def _workspace(nbytes, device):
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _temporary(nbytes, device, stream):
+    """A workspace of the call's stream: memory that torch may give away again
+    once what the stream has by then been told is done."""
+    if stream is None or device.type != "cuda" or \
+            (_stream(stream).value or 0) == torch._C._cuda_getCurrentRawStream(device.index):
+        return _workspace(nbytes, device)
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        return _workspace(nbytes, device)
+
+
 # --------------------------------------------------------------- entry points
 def pyramid_lstm_status_string(status: int) -> str:
     return load().pyramid_lstm_status_string(int(status)).decode()
@@ -272,7 +282,7 @@ def pyramid_lstm_forward(shape, x, wx, wh, b, h, saved=None, ws=None, stream=Non
     """Layer forward.  ws=None allocates the workspace with torch."""
     lib = load()
     if ws is None:
-        ws = _workspace(pyramid_lstm_workspace_size(shape, saved is not None), x.device)
+        ws = _temporary(pyramid_lstm_workspace_size(shape, saved is not None), x.device, stream)
     _check("pyramid_lstm_forward", lib.pyramid_lstm_forward(
         ctypes.byref(shape), _ptr(x), _ptr(wx), _ptr(wh), _ptr(b), _ptr(h), _ptr(saved),
         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
@@ -290,7 +300,7 @@ def pyramid_lstm_backward(shape, x, wx, wh, b, saved, dh, dx, dwx, dwh, db, ws=N
                           stream=None):
     lib = load()
     if ws is None:
-        ws = _workspace(pyramid_lstm_workspace_size(shape, 1), x.device)
+        ws = _temporary(pyramid_lstm_workspace_size(shape, 1), x.device, stream)
     _check("pyramid_lstm_backward", lib.pyramid_lstm_backward(
         ctypes.byref(shape), _ptr(x), _ptr(wx), _ptr(wh), _ptr(b), _ptr(saved), _ptr(dh),
         _ptr(dx), _ptr(dwx), _ptr(dwh), _ptr(db), _ptr(ws), ws.numel() * ws.element_size(),
@@ -309,7 +319,7 @@ def pyramid_lstm2d_forward(shape, x, wx, wh, b, h, saved=None, ws=None, stream=N
     """2D layer forward over x [N][H][W][C].  ws=None allocates the workspace with torch."""
     lib = load()
     if ws is None:
-        ws = _workspace(pyramid_lstm2d_workspace_size(shape, saved is not None), x.device)
+        ws = _temporary(pyramid_lstm2d_workspace_size(shape, saved is not None), x.device, stream)
     _check("pyramid_lstm2d_forward", lib.pyramid_lstm2d_forward(
         ctypes.byref(shape), _ptr(x), _ptr(wx), _ptr(wh), _ptr(b), _ptr(h), _ptr(saved),
         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
@@ -319,7 +329,7 @@ def pyramid_lstm2d_backward(shape, x, wx, wh, b, saved, dh, dx, dwx, dwh, db, ws
                             stream=None):
     lib = load()
     if ws is None:
-        ws = _workspace(pyramid_lstm2d_workspace_size(shape, 1), x.device)
+        ws = _temporary(pyramid_lstm2d_workspace_size(shape, 1), x.device, stream)
     _check("pyramid_lstm2d_backward", lib.pyramid_lstm2d_backward(
         ctypes.byref(shape), _ptr(x), _ptr(wx), _ptr(wh), _ptr(b), _ptr(saved), _ptr(dh),
         _ptr(dx), _ptr(dwx), _ptr(dwh), _ptr(db), _ptr(ws), ws.numel() * ws.element_size(),
@@ -342,7 +352,7 @@ def pyramid_fc_tanh_backward(x, w, y, dy, dx, dw, db, ws=None, stream=None):
     M, Cin = x.shape
     Cout = w.shape[0]
     if ws is None:
-        ws = _workspace(pyramid_fc_workspace_size(M, Cin, Cout), x.device)
+        ws = _temporary(pyramid_fc_workspace_size(M, Cin, Cout), x.device, stream)
     _check("pyramid_fc_tanh_backward", load().pyramid_fc_tanh_backward(
         M, Cin, Cout, _ptr(x), _ptr(w), _ptr(y), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(db),
         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
@@ -355,7 +365,7 @@ def pyramid_softmax_ce(x, w, b, p, labels=None, loss=None, dx=None, dw=None, db=
     M, Cin = x.shape
     K = w.shape[0]
     if labels is not None and ws is None:
-        ws = _workspace(pyramid_fc_workspace_size(M, Cin, K), x.device)
+        ws = _temporary(pyramid_fc_workspace_size(M, Cin, K), x.device, stream)
     name = "pyramid_softmax_sq" if squared else "pyramid_softmax_ce"
     _check(name, getattr(load(), name)(
         M, Cin, K, _DT[x.dtype], _ptr(x), _ptr(w), _ptr(b), _ptr(labels), _ptr(p), _ptr(loss),
@@ -379,7 +389,7 @@ def pyramid_head_train(x, w1, b1, w2, b2, labels, p, loss, dx, dw1, db1, dw2, db
     M, Cin = x.shape
     F, K = w1.shape[0], w2.shape[0]
     if ws is None:
-        ws = _workspace(max(pyramid_head_workspace_size(M, Cin, F, K), 256), x.device)
+        ws = _temporary(max(pyramid_head_workspace_size(M, Cin, F, K), 256), x.device, stream)
     _check("pyramid_head_train", load().pyramid_head_train(
         M, Cin, F, K, _ptr(x), _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), _ptr(labels), _ptr(p),
         _ptr(loss), _ptr(dx), _ptr(dw1), _ptr(db1), _ptr(dw2), _ptr(db2), _ptr(ws),
@@ -544,15 +554,6 @@ def _tensor(name, t, shape, dtype, dev):
             name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device,
             "" if t.is_contiguous() else ", not contiguous"))
     return t.data_ptr()
-
-
-def _temporary(nbytes, device, stream):
-    """A workspace of the call's stream: memory that torch may give away again
-    once what the stream has by then been told is done."""
-    if stream is None:
-        return _workspace(nbytes, device)
-    with torch.cuda.stream(_torch_stream(stream, device)):
-        return _workspace(nbytes, device)
 
 
 def _bytes(ws, dev):

@@ -5,6 +5,7 @@ from __future__ import annotations
 import pytest
 import torch
 
+import paper_1506_07452_amd as P
 from paper_1506_07452_amd import network as net
 from tests.gpu_util import DEV, say
 from tests.test_gpu_network_norm import case
@@ -105,3 +106,66 @@ def test_results_are_the_callers_too():
     torch.cuda.synchronize()
     assert torch.equal(got, want)
     del junk
+
+
+def entry_points():
+    """name: (call(stream) on tensors made here, its outputs)."""
+    gen = torch.Generator().manual_seed(54)
+
+    def rand(*shape):
+        return (torch.randn(shape, generator=gen) * 0.2).to(DEV)
+
+    def empty(*like):
+        return [torch.empty_like(t) for t in like]
+
+    out = {}
+    # channels and units of the plane steps, whose workspace is large
+    x, h, dh = rand(1, 6, 24, 25, 20), rand(1, 6, 24, 25, 32), rand(1, 6, 24, 25, 32)
+    wx, wh, b = rand(6, 128, 20, 3, 3), rand(6, 128, 32, 3, 3), rand(6, 128)
+    s = P.shape_for(x, 32)
+    saved = torch.empty(P.pyramid_lstm_saved_size(s), dtype=torch.uint8, device=DEV)
+    P.pyramid_lstm_forward(s, x, wx, wh, b, h, saved)
+    h1, g1 = torch.empty_like(h), empty(x, wx, wh, b)
+    out["lstm_forward"] = (lambda st: P.pyramid_lstm_forward(s, x, wx, wh, b, h1, stream=st), [h1])
+    out["lstm_backward"] = (lambda st: P.pyramid_lstm_backward(s, x, wx, wh, b, saved, dh, *g1, stream=st), g1)
+    x2, h2, dh2 = rand(2, 24, 25, 20), rand(2, 24, 25, 32), rand(2, 24, 25, 32)
+    wx2, wh2, b2 = rand(4, 128, 20, 3), rand(4, 128, 32, 3), rand(4, 128)
+    s2 = P.shape2d_for(x2, 32)
+    saved2 = torch.empty(P.pyramid_lstm2d_saved_size(s2), dtype=torch.uint8, device=DEV)
+    P.pyramid_lstm2d_forward(s2, x2, wx2, wh2, b2, h2, saved2)
+    h3, g3 = torch.empty_like(h2), empty(x2, wx2, wh2, b2)
+    out["lstm2d_forward"] = (lambda st: P.pyramid_lstm2d_forward(s2, x2, wx2, wh2, b2, h3, stream=st), [h3])
+    out["lstm2d_backward"] = (
+        lambda st: P.pyramid_lstm2d_backward(s2, x2, wx2, wh2, b2, saved2, dh2, *g3, stream=st), g3)
+    M = 5000
+    rows, w, bias, dy = rand(M, 32), rand(64, 32), rand(64), rand(M, 64)
+    y = torch.empty_like(dy)
+    P.pyramid_fc_tanh_forward(rows, w, bias, y)
+    g4 = empty(rows, w, bias)
+    out["fc_backward"] = (lambda st: P.pyramid_fc_tanh_backward(rows, w, y, dy, *g4, stream=st), g4)
+    labels = torch.randint(0, 4, (M,), generator=gen, dtype=torch.int32).to(DEV)
+    hw, hb = rand(4, 32), rand(4)
+    for squared in (False, True):
+        g5 = [torch.empty((M, 4), device=DEV), torch.empty(1, device=DEV)] + empty(rows, hw, hb)
+
+        def softmax(st, g=g5, sq=squared):
+            P.pyramid_softmax_ce(rows, hw, hb, g[0], labels, *g[1:], stream=st, squared=sq)
+        out["softmax_sq" if squared else "softmax_ce"] = (softmax, g5)
+    hw2 = rand(4, 64)
+    g6 = [torch.empty((M, 4), device=DEV), torch.empty(1, device=DEV)] + empty(rows, w, bias, hw2, hb)
+    out["head_train"] = (lambda st: P.pyramid_head_train(rows, w, bias, hw2, hb, labels, *g6, stream=st), g6)
+    return out
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+@pytest.mark.parametrize("name", ["lstm_forward", "lstm_backward", "lstm2d_forward", "lstm2d_backward", "fc_backward",
+                                  "softmax_ce", "softmax_sq", "head_train"])
+def test_workspace_made_by_the_binding(name, raw):
+    call, outs = entry_points()[name]
+    say("workspace of", name, raw)
+    call(None)
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.fill_(NAN)
+    beside_busy_stream(call, raw)
+    same(outs, want)
