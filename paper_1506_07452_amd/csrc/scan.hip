@@ -639,6 +639,9 @@ Plan scan_plan(int64_t B, int64_t T, int64_t I, int32_t reverse, const int32_t *
     p.chain_waves = backward && few * p.blocks > kShortChain ? kWaves : kChainWaves;
     const long long chunks = (p.a.runs + p.chain_waves - 1) / p.chain_waves;
     p.waves = p.a.runs == 1 ? 1 : p.a.runs <= kFewWaves ? kFewWaves : kWaves;
+    // a launch has fewer than 2^32 work items: columns past that (2^29 of over 64 steps)
+    // fill the card many times over with one wave each
+    if (p.blocks * 64 * p.waves >= (1LL << 32)) p.waves = 1;
     Carve cv(ws);
     if (chunks > 1 && p.a.cols < kChainCols && chunks * p.blocks <= (1 << 21)) {
         p.ch.agg = cv.take<uint64_t>(chunks * p.a.cols);

@@ -657,3 +657,37 @@ def test_scan_sequences_far_apart(I):
                          R.rounded(ref, err, BF16)[:, keep])
                 if end < T:
                     assert not h[b, end:].any() and not dg[b, end:].any() and not du[b, end:].any()
+
+
+def test_scan_columns_past_a_wide_launch():
+    """The most columns that there may be, of more than one run: 2^24 workgroups, which
+    a launch takes with one wave each alone.  The columns repeat those of the first 341
+    sequences (37 GB a tensor)."""
+    P0, T, I = 341, 17, 63
+    B = (1 << 30) // I
+    assert B % P0 == 0 and B * I > (1 << 30) - 64
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 140 << 30:
+        pytest.skip("needs 140 GB of free memory")
+    one = rand(1, (P0, T, I), BF16, 1.5, 1.0)
+    g = torch.empty((B, T, I), dtype=BF16, device=DEV)
+    g.view(-1, P0, T, I).copy_(one.to(DEV))
+    h, saved = torch.empty_like(g), torch.empty(P.pyramid_scan_saved_size(B, T, I), dtype=torch.uint8, device=DEV)
+    say("scan of 2^30 columns")
+    P.pyramid_scan_forward(g, g, h, True, saved=saved)
+
+    def whole(name, t, ref, err):
+        rows = t.view(B // P0, -1)
+        near(name, t[:P0].cpu(), ref, R.rounded(ref, err, BF16))
+        for k in range(0, rows.shape[0], 4096):
+            assert bool((rows[k:k + 4096] == rows[:1]).all()), (name, k)
+
+    ref, e, _, _, before, eb = R.scan_forward(one, one, True, None, None)
+    whole("h", h, ref, e)
+    dg, du = h, torch.empty_like(g)
+    P.pyramid_scan_backward(g, g, saved, g, dg, du, True)
+    (rg, eg), (ru, eu), _ = R.scan_backward(one, one, before, eb, one, True, None, None)
+    whole("dg", dg, rg, eg)
+    whole("du", du, ru, eu)
+    del g, h, saved, dg, du
+    torch.cuda.empty_cache()
