@@ -400,9 +400,11 @@ int pyramid_stitch_finish(int32_t D, int32_t H, int32_t W, int32_t K, const void
 /* Layer norm over the C channels of each of M rows (voxels, tokens):
  *   mean = sum_c x / C, var = sum_c (x - mean)^2 / C, rstd = 1/sqrt(var + eps),
  *   y[m][c] = (x[m][c] - mean) rstd gamma[c] + beta[c].
- *   x, y [M][C], gamma, beta [C] in `dtype`; statistics in fp32; eps > 0.
+ *   x, y [M][C], gamma, beta [C] in `dtype`; statistics in fp32 (squares of
+ *   differences that add up past it give rstd 0); eps > 0.
  *   stats       : NULL, or fp32 [M][2], overwritten with (mean, rstd) of each
- *                 row for the backward.
+ *                 row for the backward, whose (x - mean) is that of the rounded
+ *                 mean: off by half a step of it.
  *   xq, xscale  : both NULL, or the 8-bit checkpoint of x (codes [M][C] and
  *                 pyramid_checkpoint8_scales(M * C) scales), written in the
  *                 same call with the values of pyramid_checkpoint8_pack.

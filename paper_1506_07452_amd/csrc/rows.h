@@ -175,6 +175,24 @@ __device__ inline float lanes_sum(float v)
         return float_bits(bits_float(a) + bits_float(b));
     }));
 }
+template <int CTRL>
+__device__ inline double moved(double v)
+{
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = moved<CTRL>((uint32_t)w), hi = moved<CTRL>((uint32_t)(w >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int G>
+__device__ inline double lanes_sum(double v)
+{
+    if (G >= 2) v += moved<0xb1>(v);
+    if (G >= 4) v += moved<0x4e>(v);
+    if (G >= 8) v += moved<0x141>(v);
+    if (G >= 16) v += moved<0x140>(v);
+    if (G >= 32) v += __shfl_xor(v, 16);
+    if (G >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
 template <int G>
 __device__ inline uint32_t lanes_max(uint32_t v)
 {

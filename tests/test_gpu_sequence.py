@@ -691,3 +691,67 @@ def test_scan_columns_past_a_wide_launch():
     whole("du", du, ru, eu)
     del g, h, saved, dg, du
     torch.cuda.empty_cache()
+
+
+def full_mantissa(seed, n):
+    """fp32 values whose 24 bits are all in use, of magnitudes 1e-3 to 1e6, and three round ones in decimal."""
+    v = rand(seed, (n,), F32) * 10.0 ** rand(seed + 1, (n,), F32, 2.0).clamp(-3, 6)
+    v[:3] = torch.tensor([0.1, 1000.1, -33333.3])
+    return v
+
+
+@pytest.mark.parametrize("C", [2, 3, 7, 25, 45, 48, 64, 100, 130, 1000, 2048, 4096, 5000, 12001, 16384])
+def test_norm_rows_of_one_value(C):
+    """A row of one value has that value as its mean, whatever its bits: y is beta to the
+    last bit, rstd that of eps, and dx that of a row whose xh is 0."""
+    M = 200 if C < 1000 else 40
+    x = full_mantissa(C, M)[:, None].expand(M, C).contiguous()
+    gamma, beta, dy = rand(1, (C,), F32, 0.2, 1.0), rand(2, (C,), F32), rand(3, (M, C), F32)
+    beta[: C // 2] = 0
+    y, stats, dx = Out((M, C), F32), Out((M, 2), F32), Out((M, C), F32)
+    dgamma, dbeta = Out((C,), F32), Out((C,), F32)
+    dev = [t.to(DEV) for t in (x, gamma, beta, dy)]
+    say("norm rows of one value", C)
+    P.pyramid_layer_norm_forward(dev[0], dev[1], dev[2], y.t, stats.t)
+    P.pyramid_layer_norm_backward(dev[0], dev[1], stats.t, dev[3], dx.t, dgamma.t, dbeta.t)
+    assert torch.equal(stats.get()[:, 0], x[:, 0])
+    assert torch.equal(y.get(), beta.expand(M, C))
+    assert torch.equal(dgamma.get(), torch.zeros(C))
+    rstd = torch.full((M, 1), 1e-5, dtype=torch.float64) ** -0.5
+    a = (dy * gamma.double())
+    want = rstd * (a - a.mean(1, keepdim=True))
+    # a and its mean (64 serial additions at most), rstd: the root of eps, rounded itself
+    near("dx", dx.get(), want, R.rounded(want, R.U * rstd * (6 * a.abs() + 70 * a.abs().mean(1, keepdim=True)), F32))
+
+
+@pytest.mark.parametrize("offset,spread", [(1000.0, 1e-3), (1e6, 0.5), (-3e4, 0.02), (200.0, 1.0), (1e22, 1e16)])
+@pytest.mark.parametrize("C", [16, 45, 1000, 5000])
+def test_norm_far_above_the_spread(C, offset, spread):
+    """fp32 rows far from zero, down to spreads of a few steps of their values: y is right to
+    the bits of the differences, not of the values."""
+    M = 60
+    x = (rand(C, (M, C), F32).double() * spread + offset).float()
+    gamma, beta = rand(1, (C,), F32, 0.2, 1.0), rand(2, (C,), F32)
+    y, stats = Out((M, C), F32), Out((M, 2), F32)
+    say("norm offset", C, offset, spread)
+    P.pyramid_layer_norm_forward(x.to(DEV), gamma.to(DEV), beta.to(DEV), y.t, stats.t)
+    ry, _, mean, rstd = R.norm_forward(x, gamma, beta, 1e-5, F32)
+    near("mean", stats.get()[:, 0], mean[:, 0], 1.01 * R.U * mean[:, 0].abs())
+    near("rstd", stats.get()[:, 1], rstd[:, 0], 40 * R.U * rstd[:, 0])
+    # a difference from the mean is off by 3 U of itself (two subtractions, the mean's second
+    # part) and U^2 of the mean; the variance by 70 U of itself, rstd by half of that and 4 U
+    xh = (x.double() - mean) * rstd
+    bound = (R.U * 44 * xh.abs() + 2 * R.U ** 2 * mean.abs() * rstd) * gamma.double().abs() + \
+        R.U * (2 * ry.abs() + beta.double().abs())
+    near("y", y.get(), ry, R.rounded(ry, bound, F32))
+
+
+@pytest.mark.parametrize("C", [3, 45, 1000, 4099, 16384])
+def test_norm_bf16_rows_of_one_value(C):
+    x = full_mantissa(C, 60).to(BF16)[:, None].expand(60, C).contiguous()
+    gamma, beta = rand(1, (C,), BF16, 0.2, 1.0), rand(2, (C,), BF16)
+    beta[: C // 2] = 0
+    y, stats = Out((60, C), BF16), Out((60, 2), F32)
+    say("norm bf16 rows of one value", C)
+    P.pyramid_layer_norm_forward(x.to(DEV), gamma.to(DEV), beta.to(DEV), y.t, stats.t)
+    assert torch.equal(stats.get()[:, 0], x[:, 0].float()) and torch.equal(y.get(), beta.expand(60, C))
