@@ -289,7 +289,10 @@ k_norm_bwd(const X *__restrict__ x, const uint16_t *__restrict__ xscale,
             for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float xh = (v[k][i] - st[t].x) * st[t].y, a = d[k][i] * ga[k][i];
+                    // a channel that the row does not have has d = 0, but the mean times
+                    // rstd may be infinite
+                    const float xh = (j + G * k) * N + i < C ? (v[k][i] - st[t].x) * st[t].y : 0.0f;
+                    const float a = d[k][i] * ga[k][i];
                     v[k][i] = xh;
                     ta += a;
                     tb = fmaf(a, xh, tb);

@@ -755,3 +755,29 @@ def test_norm_bf16_rows_of_one_value(C):
     say("norm bf16 rows of one value", C)
     P.pyramid_layer_norm_forward(x.to(DEV), gamma.to(DEV), beta.to(DEV), y.t, stats.t)
     assert torch.equal(stats.get()[:, 0], x[:, 0].float()) and torch.equal(y.get(), beta.expand(60, C))
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("C", [3, 45, 64, 1000, 5000])
+def test_norm_backward_of_huge_rows(C, ckpt):
+    """Rows of one value whose mean times rstd passes fp32: channels that a row does not
+    have do not get into its gradient."""
+    M = 9
+    x = torch.full((M, C), 2.0 ** 120)
+    if not ckpt:        # blocks of codes span rows: one value in all of them
+        x[1::2] *= -1.5
+    gamma, dy = rand(1, (C,), F32, 0.2, 1.0), rand(2, (M, C), F32)
+    dev = [t.to(DEV) for t in (x, gamma, dy)]
+    y, stats, dx = Out((M, C), F32), Out((M, 2), F32), Out((M, C), F32)
+    dgamma, dbeta = Out((C,), F32), Out((C,), F32)
+    q, s = P.checkpoint8_empty(dev[0]) if ckpt else (None, None)
+    say("norm huge rows", C, ckpt)
+    P.pyramid_layer_norm_forward(dev[0], dev[1], dev[1], y.t, stats.t, q, s)
+    if ckpt:        # the mean of the codes' values, so that their xh is 0
+        stats.t[:, 0] = R.codes(x)[2][:, 0].float().to(DEV)
+    P.pyramid_layer_norm_backward(dev[0] if q is None else q, dev[1], stats.t, dev[2], dx.t, dgamma.t, dbeta.t, xscale=s)
+    assert torch.equal(dgamma.get(), torch.zeros(C))
+    rstd = torch.full((M, 1), 1e-5, dtype=torch.float64) ** -0.5
+    a = dy * gamma.double()
+    want = rstd * (a - a.mean(1, keepdim=True))
+    near("dx", dx.get(), want, R.rounded(want, R.U * rstd * (6 * a.abs() + 70 * a.abs().mean(1, keepdim=True)), F32))
