@@ -781,3 +781,77 @@ def test_norm_backward_of_huge_rows(C, ckpt):
     a = dy * gamma.double()
     want = rstd * (a - a.mean(1, keepdim=True))
     near("dx", dx.get(), want, R.rounded(want, R.U * rstd * (6 * a.abs() + 70 * a.abs().mean(1, keepdim=True)), F32))
+
+
+def slow(shape, seed):
+    """Waves along the steps, of other phases per channel: what a chunk inherits differs from
+    one group of chunks to the next."""
+    T, I = shape[1], shape[2]
+    t, i = torch.arange(T, dtype=torch.float32)[:, None], torch.arange(I, dtype=torch.float32)[None]
+    return torch.sin(t * (2 * 3.14159265 / 7000) + i * 0.7 + seed).expand(shape)
+
+
+def scan_chain(B, T, I, dtype, cols, reverse=False, lengths=None, ckpt=False):
+    """A chained scan of long memories, forward and backward, against the 64-bit form of the
+    channels `cols`: all positions, hT and dh0."""
+    g = rand(T + I, (B, T, I), dtype, 1.0, 7.5)
+    u, dh = ((rand(T + I + k, (B, T, I), F32, 0.5) + slow((B, T, I), k)).to(dtype) for k in (1, 2))
+    h0, dhT = rand(T + I + 3, (B, I), F32), rand(T + I + 4, (B, I), F32, 100.0)
+    gd, ud, dhd, h0d, dhTd = (t.to(DEV) for t in (g, u, dh, h0, dhT))
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32).to(DEV)
+    h_, dg_, du_ = (Out((B, T, I), dtype) for _ in range(3))
+    hT_, dh0_ = Out((B, I), F32), Out((B, I), F32)
+    saved = torch.empty(P.pyramid_scan_saved_size(B, T, I), dtype=torch.uint8, device=DEV)
+    P.pyramid_scan_forward(gd, ud, h_.t, reverse, ln, h0d, hT_.t, saved)
+    gs = us = None
+    gr, ur = g, u
+    if ckpt:
+        gk, gs = P.checkpoint8_empty(gd)
+        uk, us = P.checkpoint8_empty(ud)
+        P.pyramid_checkpoint8_pack(gd, gk, gs)
+        P.pyramid_checkpoint8_pack(ud, uk, us)
+        gd, ud = gk, uk
+        gr, ur = R.codes(g)[2], R.codes(u)[2]
+    P.pyramid_scan_backward(gd, ud, saved, dhd, dg_.t, du_.t, reverse, ln, dhTd, dh0_.t, gscale=gs, uscale=us)
+    torch.cuda.synchronize()
+    g, u, dh, gr, ur, h0, dhT = (t[..., cols].contiguous() for t in (g, u, dh, gr, ur, h0, dhT))
+    h, e, hT, eT, before, eb = R.scan_forward(g, u, reverse, lengths, h0)
+    near("h", h_.get()[..., cols], h, R.rounded(h, e, dtype))
+    near("hT", hT_.get()[..., cols], hT, eT)
+    if ckpt:
+        before, eb = R.scan_forward(gr, ur, reverse, lengths, h0, run=(before, eb))[4:]
+    (dg, eg), (du, eu), (dh0, e0) = R.scan_backward(gr, ur, before, eb, dh, reverse, lengths, dhT)
+    near("dg", dg_.get()[..., cols], dg, R.rounded(dg, eg, dtype))
+    near("du", du_.get()[..., cols], du, R.rounded(du, eu, dtype))
+    near("dh0", dh0_.get()[..., cols], dh0, e0)
+
+
+@DTYPES
+@pytest.mark.parametrize("reverse", [False, True], ids=["fwd", "rev"])
+@pytest.mark.parametrize("T,I,cols", [(20000, 3, [0, 1, 2]), (9000, 520, [0, 63, 64, 300, 511, 512, 519])],
+                         ids=["groups-of-32", "groups-of-16"])
+def test_scan_state_across_groups(T, I, cols, reverse, dtype):
+    """States and their gradients from one group of chunks to the next, with groups of
+    either size, in both directions."""
+    say("scan groups", T, I, reverse, dtype)
+    scan_chain(1, T, I, dtype, cols, reverse)
+
+
+@DTYPES
+@pytest.mark.parametrize("ckpt", [False, True], ids=["plain", "ckpt"])
+@pytest.mark.parametrize("lengths", [None, [10000, 7777], [300, 10000]], ids=["even", "ragged", "ragged-short-first"])
+def test_scan_chained_backward_of_eight_waves(lengths, ckpt, dtype):
+    """More than 512 workgroups of sixteen waves: the backward takes eight."""
+    B, I = (1, 1000) if lengths is None else (2, 500)
+    assert -(-10000 // 256) * -(-B * I // 64) > 512
+    say("scan eight waves", lengths, ckpt, dtype)
+    scan_chain(B, 10000, I, dtype, [0, 63, 250, I - 1], lengths == [300, 10000], lengths, ckpt)
+
+
+@DTYPES
+@pytest.mark.parametrize("reverse", [False, True], ids=["fwd", "rev"])
+@pytest.mark.parametrize("I", [64, 100, 192, 256])
+def test_scan_ragged_codes_of_one_sequence(I, reverse, dtype):
+    """Codes with lengths where a workgroup's columns are of one sequence."""
+    say("scan ragged codes", I, reverse, dtype)
+    scan_step(4, 290, I, dtype, reverse, [290, 0, 161, 288], ckpt=True, seed=I)
