@@ -855,3 +855,44 @@ def test_scan_ragged_codes_of_one_sequence(I, reverse, dtype):
     """Codes with lengths where a workgroup's columns are of one sequence."""
     say("scan ragged codes", I, reverse, dtype)
     scan_step(4, 290, I, dtype, reverse, [290, 0, 161, 288], ckpt=True, seed=I)
+
+
+@pytest.mark.parametrize("M,C,dtype,ckpt", [
+    ((1 << 21) + 300, 16, F32, True), ((1 << 22) + 700, 16, BF16, True),        # codes in lanes
+    ((1 << 19) + 90, 45, F32, True), ((1 << 20) + 200, 45, BF16, True),         # codes through LDS
+    ((1 << 20) + 77, 7, F32, True),                                             # codes by the pack kernel
+    (8192 + 55, 2048, BF16, True), (8192 + 9, 1088, F32, True), (8192 + 20, 5000, F32, False),
+    (8192 + 20, 4096, BF16, False), (8192 + 7, 9000, BF16, True), (8192 + 3, 16384, F32, False)],
+    ids=lambda v: IDS.get(v, v) if isinstance(v, torch.dtype) else str(v))
+def test_norm_workgroups_that_turn(M, C, dtype, ckpt):
+    """More rows than the forward's 8192 workgroups (and the backward's 512) take at once:
+    all rows, their codes and the weights' gradients."""
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    x, dy = (torch.empty((M, C), dtype=dtype, device=DEV).normal_(k * 0.3, 0.8, generator=gen) for k in (1, 0))
+    gamma, beta = rand(1, (C,), dtype, 0.2, 1.0).to(DEV), rand(2, (C,), dtype, 0.1).to(DEV)
+    y, stats, dx = torch.empty_like(x), torch.empty((M, 2), device=DEV), torch.empty_like(x)
+    dgamma, dbeta = torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+    q, s = P.checkpoint8_empty(x) if ckpt else (None, None)
+    say("norm turns", M, C, dtype, ckpt)
+    P.pyramid_layer_norm_forward(x, gamma, beta, y, stats, q, s)
+    P.pyramid_layer_norm_backward(x if q is None else q, gamma, stats, dy, dx, dgamma, dbeta, xscale=s)
+    want = [torch.zeros(C, dtype=torch.float64, device=DEV) for _ in range(4)]
+    step = 1 << 18 if C < 100 else 1 << 11      # rows, a multiple of 64: blocks of codes end with them
+    for m in range(0, M, step):
+        at = slice(m, m + step)
+        ry, by, mean, rstd = R.norm_forward(x[at], gamma, beta, 1e-5, dtype)
+        near("y", y[at], ry, by)
+        kept = x[at]
+        if ckpt:
+            rq, rs, kept = R.codes(kept)
+            assert torch.equal(q[at], rq) and torch.equal(s[m * C // 64:][:rs.numel()], rs)
+        rdx, (dg, bg), (db, bb) = R.norm_backward(kept, mean, rstd, gamma, dy[at], dtype)
+        near("dx", dx[at], *rdx)
+        # the bounds of a part of the rows, with the chain of all of them
+        more = (M - kept.shape[0]) / 256 * R.U
+        xh = (kept.double() - mean) * rstd
+        for t, v in zip(want, (dg, bg + more * (dy[at].double() * xh).abs().sum(0), db,
+                               bb + more * dy[at].double().abs().sum(0))):
+            t += v
+    near("dgamma", dgamma, want[0], want[1])
+    near("dbeta", dbeta, want[2], want[3])
