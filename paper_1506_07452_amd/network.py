@@ -154,6 +154,9 @@ def _saved_arrays(saved, s: plstm_shape):
         off = -(-off // 256) * 256
         out.append(saved[off:off + 4 * n].view(torch.float32))
         off += 4 * n
+    if not saved.numel() == off == pyramid_lstm_saved_size(s):
+        raise ValueError("saved has %d bytes, its arrays %d and a buffer of this shape %d" % (
+            saved.numel(), off, pyramid_lstm_saved_size(s)))
     return out
 
 

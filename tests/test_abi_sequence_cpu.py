@@ -154,3 +154,17 @@ def test_code_forms():
     assert (below * 127 < top).all()
     assert ((v.view(-1, 64) - blocks).abs() <= sd[:, None] / 2).all()
     assert q.abs().max() <= 127
+
+
+def test_saved_buffers_of_another_shape_are_refused():
+    """The arrays that 8-bit checkpoints pack cover a saved buffer of their shape exactly."""
+    from paper_1506_07452_amd import network as net
+    for N, D, H, W, C, O, K in ((1, 3, 4, 5, 2, 16, 3), (2, 1, 1, 1, 1, 4, 1), (1, 5, 7, 3, 9, 32, 5)):
+        s = P.plstm_shape(N, D, H, W, C, O, 0, K)
+        size = P.pyramid_lstm_saved_size(s)
+        arrays = net._saved_arrays(torch.empty(size, dtype=torch.uint8), s)
+        cells = 6 * N * D * H * W * O
+        assert [a.numel() for a in arrays] == [4 * cells, cells, cells]
+        for bad in (size - 4, size + 256, size // 2):
+            with pytest.raises(ValueError):
+                net._saved_arrays(torch.empty(bad, dtype=torch.uint8), s)
