@@ -450,7 +450,9 @@ int pyramid_layer_norm_backward(int64_t M, int32_t C, int32_t dtype, const void 
  *   saved       : NULL, or pyramid_scan_saved_size() bytes for the backward:
  *                 fp32 [B][ceil(T/16)][I], the state before positions 0, 16, ...
  *   ws          : at least pyramid_scan_workspace_size() bytes.
- * States are fp32 whatever the storage type.  B, T, I >= 1, B I <= 2^30,
+ * States are fp32 whatever the storage type, and so is f: a step is off by up
+ * to 2^-23 of the state, which adds up where gates keep nearly all of it for
+ * very long (0.4% after 65536 steps at g = 15).  B, T, I >= 1, B I <= 2^30,
  * T <= 2^31, B T I <= 2^38.  Long sequences are cut into chunks that wait for
  * each other on the device, every wait bounded: one that gives up makes the
  * states behind it NaN and raises PLSTM_DEVICE_WAIT_GAVE_UP. */

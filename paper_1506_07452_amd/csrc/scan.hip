@@ -6,7 +6,11 @@
 //   G_s = dh_t + f_{s+1} G_{s+1}  (the last one takes dhT as well)
 //   du_t = (1 - f) G_s,  dg_t = G_s (h_{s-1} - u_t) f (1 - f),  dh0 = f_0 G_0
 // States and gradients of states are fp32.  1 - f is sigmoid(-g), not a
-// difference: a gate that keeps all but 1e-5 of the state keeps its bits.
+// difference: what a gate takes keeps its bits however little it is.  f itself is rounded
+// next to 1, so a step that keeps the state is off by up to 2^-23 of it, always the same
+// way under a constant gate (g = 15: a state of 1 fed with 1 is 0.996 after 65536 steps).
+// Folding 1 - f instead would mend that and lose states that are infinite (0 times infinity
+// where f = 1).
 // A training forward keeps the state before every 16th position; the backward
 // computes the others again from g and u (in the storage type or from 8-bit
 // checkpoints), which costs 1/4 byte an element where reading h would cost 2
@@ -69,7 +73,7 @@ k_scan_chain_init(Chain ch, long long cols, const float *start)
 }
 
 // f and 1 - f of sigmoid's argument.  exp(-|g|) <= 1: nothing overflows, and
-// neither is a difference.
+// neither is a difference (their sum is 1 to 2^-23).
 __device__ inline void gate(float g, float &keep, float &take)
 {
     const float e = __builtin_amdgcn_exp2f(fabsf(g) * -1.44269504f);
@@ -347,9 +351,9 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
     return at;
 }
 
-// Bound by bytes where columns fill the card (11520 x 240 x 16 fp32 in 109 us, 4.9 TB/s; 64 x 512
-// x 512 bf16 in 20 us, 5.1 TB/s), in chains by their phases (2 x 8192 x 2048 fp32 in 80 us, 5.0 TB/s;
-// 65536 x 1024 bf16 in 93 us, 4.3 TB/s; 4096 x 512 in about 10 us with the clearing launch).
+// Bound by bytes where columns fill the card (11520 x 240 x 16 fp32 in 111 us, 4.8 TB/s; 64 x 512
+// x 512 bf16 in 20 us, 5.1 TB/s), in chains by their phases (2 x 8192 x 2048 fp32 in 89 us, 4.5 TB/s;
+// 65536 x 1024 bf16 in 95 us, 4.2 TB/s; 4096 x 512 in about 10 us with the clearing launch).
 // A workgroup of W waves advances 64 columns by W runs of 16 positions at a
 // time, wave w holding run w in registers.  W = 1 walks its runs one after
 // another; with more, each wave folds its run to (A, H), and starts it again from

@@ -318,7 +318,7 @@ def _layer_act_backward(act, li, layers, norms, dh, ws, stream):
         dn = (dgamma, dbeta)
     saved = act["saved"]
     if "packed" in act:
-        saved = saved_unpack(act["packed"], shape_for(act["in"], L.O, L.K), stream)
+        saved = saved_unpack(act.pop("packed"), shape_for(act["in"], L.O, L.K), stream)
     dx, dwx, dwh, db = layer_backward(act["in"], L, saved, dh.view(act["h"].shape),
                                       want_dx=li > 0, ws=ws, stream=stream)
     return dx, (dwx, dwh, db), dn
@@ -380,6 +380,7 @@ def network_train_step(x, layers, fcs, head, labels, ws=None, stream=None, fused
             fc_grads[li] = (dwf, dbf)
         g, layer_grads[li], norm_grads[li] = _layer_act_backward(act, li, layers, norms, dh, ws,
                                                                  stream)
+        act = acts[li] = None       # before the next layer's buffers are there
     out = {"loss": lval, "p": p, "head": (dw, db), "fcs": fc_grads, "layers": layer_grads}
     if norms is not None:
         out["norms"] = norm_grads
@@ -411,6 +412,7 @@ def _train_step_unfused(x, layers, fcs, head, labels, ws=None, stream=None, loss
             dh = g      # the output layer reads h directly
         dx, layer_grads[li], norm_grads[li] = _layer_act_backward(act, li, layers, norms, dh, ws,
                                                                   stream)
+        act = acts[li] = None       # before the next layer's buffers are there
         if li > 0:
             g = dx
     res = {"loss": out["loss"], "p": out["p"], "head": out["head_grad"], "fcs": fc_grads,

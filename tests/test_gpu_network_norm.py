@@ -359,3 +359,28 @@ def test_dropped_tensors_belong_to_the_calls_stream(training, raw):
         for (gq, gs), (wq, ws_) in zip(g.get("packed", ()), w.get("packed", ())):
             assert torch.equal(gq, wq) and torch.equal(gs, ws_)
     del junk
+
+
+@pytest.mark.parametrize("last_fc,fused", [(True, True), (True, False), (False, True)])
+def test_checkpoint8_step_needs_less_memory(last_fc, fused):
+    """The most memory that a step has at once is less by most of what the lower layer saves:
+    a layer's buffers are gone before the next one's are unpacked."""
+    wl = synth.Workload("memory", 1, 12, 32, 40, 3, [16, 16], fc=True, classes=4, labels=True, seed=48)
+    inst = synth.make(wl)
+    fcs, head = [(dev(w), dev(b)) for w, b in inst.fcs], tuple(dev(v) for v in inst.head)
+    if not last_fc:
+        fcs, head = fcs[:1], (torch.rand((4, 16), device=DEV), head[1])
+    x, layers, labels = dev(inst.x), [layer_dev(L) for L in inst.layers], torch.from_numpy(inst.labels).to(DEV)
+    ws = net.workspace_for(x.shape, [16, 16], True, torch.float32, True, DEV)
+    say("memory of a step", last_fc, fused)
+    peak = []
+    for eight in (False, True):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        out = net.network_train_step(x, layers, fcs, head, labels, ws=ws, fused_head=fused, checkpoint8=eight)
+        peak.append(torch.cuda.max_memory_allocated() - before)
+        del out
+    lower = P.pyramid_lstm_saved_size(P.shape_for(x, 16))
+    # saved: 144 bytes of fp32 a voxel and unit; packed 1.03 for 4; all else of a layer: 3 to 5 volumes of 16 or 32 units
+    assert peak[1] <= peak[0] - 0.6 * lower, (peak, lower)
