@@ -169,3 +169,31 @@ def test_workspace_made_by_the_binding(name, raw):
         t.fill_(NAN)
     beside_busy_stream(call, raw)
     same(outs, want)
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["plain", "checkpoint8"])
+def test_training_step_captured_on_a_forked_stream(eight):
+    """A graph whose step runs on a stream forked from the captured one, replayed with other
+    work between the replays."""
+    d, _ = case([16, 32, 16], True, 55, (1, 0, 1))
+    args = (d["layers"], d["fcs"], d["head"], d["labels"])
+    x = d["x"].clone()
+    kw = dict(norms=d["norms"], checkpoint8=eight)
+    want = net.network_train_step(x, *args, **kw)
+    other = x * 0.5
+    want_other = net.network_train_step(other, *args, **kw)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    say("captured step", eight)
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = net.network_train_step(x, *args, stream=side, **kw)
+        torch.cuda.current_stream().wait_stream(side)
+    first = x.clone()
+    for turn in range(3):
+        for v, w in ((first, want), (other, want_other)):
+            x.copy_(v)
+            graph.replay()
+            net.network_train_step(other, *args, **kw)
+            torch.cuda.synchronize()
+            same(got, w)
