@@ -79,8 +79,8 @@ template <> struct Mean<uint16_t> {
 };
 
 // Forward: two sums over a row that is read once, mean first, so that the variance is that of
-// the differences.  Bound by bytes: 2764800 fp32 rows of 16 in 58 us (6.1 TB/s, part of y
-// staying in the cache), 8192 bf16 rows of 4096 in 28 us (4.7 TB/s).
+// the differences.  Bound by bytes: 2764800 fp32 rows of 16 in 59 us (6.0 TB/s, part of y
+// staying in the cache), 8192 bf16 rows of 4096 in 29 us (4.7 TB/s).
 // CODE: also the 8-bit checkpoint of x.  1: its blocks of 64 elements are aligned
 // lanes of a wave.  2: they are not, but the rows of a turn are whole blocks: those go
 // through LDS, and lanes take pieces of blocks there.
@@ -228,9 +228,9 @@ template <typename T> struct RawX<T, int8_t> {
 };
 
 // Backward in one pass over x and dy: the row's two sums give dx, and the same values
-// go into the columns' sums.  Bound by bytes: 2764800 fp32 rows of 16 in 114 us (4.7
-// TB/s), 8192 bf16 rows of 4096 in 42 us (4.8 TB/s), 360000 fp32 rows of 45 from codes in 31
-// us (4.7 TB/s).
+// go into the columns' sums.  Bound by bytes: 2764800 fp32 rows of 16 in 116 us (4.6
+// TB/s), 8192 bf16 rows of 4096 in 44 us (4.6 TB/s), 360000 fp32 rows of 45 from codes in 32
+// us (4.6 TB/s).
 // A workgroup walks every gridDim-th stretch of rows with its columns' sums of
 // dy xh and dy in registers; at the end its lane groups' sums are added in
 // order and written as its part [2][C] of `part` (dgamma and dbeta themselves
@@ -417,7 +417,7 @@ int with_rows(int C, F fn)
 
 // How the forward codes rows of C elements, G lanes each with U rows in a turn:
 // in its lanes where blocks of 64 elements lie in whole rows or whole rows of pieces in a
-// block; through LDS where a turn's rows are whole blocks (fp32, 360000 rows of 45: 33 us, 41
+// block; through LDS where a turn's rows are whole blocks (fp32, 360000 rows of 45: 34 us, 41
 // with the pack kernel after it); not at all otherwise.
 template <typename T, int G, int K> constexpr int code_rows() { return (G > 256 ? G : 256) / G * Rows<T, G, K>::U; }
 template <typename T, int G, int K> int code_mode(int C)

@@ -351,9 +351,9 @@ __device__ inline float before_run(Shared<W, CHAIN> &sh, int turn, const Chain &
     return at;
 }
 
-// Bound by bytes where columns fill the card (11520 x 240 x 16 fp32 in 111 us, 4.8 TB/s; 64 x 512
-// x 512 bf16 in 20 us, 5.1 TB/s), in chains by their phases (2 x 8192 x 2048 fp32 in 89 us, 4.5 TB/s;
-// 65536 x 1024 bf16 in 95 us, 4.2 TB/s; 4096 x 512 in about 10 us with the clearing launch).
+// Bound by bytes where columns fill the card (11520 x 240 x 16 fp32 in 110 us, 4.8 TB/s; 64 x 512
+// x 512 bf16 in 20 us, 5.1 TB/s), in chains by their phases (2 x 8192 x 2048 fp32 in 88 us, 4.6 TB/s;
+// 65536 x 1024 bf16 in 95 to 100 us, 4.0 to 4.2 TB/s; 4096 x 512 in about 10 us with the clearing launch).
 // A workgroup of W waves advances 64 columns by W runs of 16 positions at a
 // time, wave w holding run w in registers.  W = 1 walks its runs one after
 // another; with more, each wave folds its run to (A, H), and starts it again from
