@@ -499,6 +499,161 @@ int pyramid_checkpoint8_pack(int64_t n, int32_t dtype, const void *x, void *q, v
 int pyramid_checkpoint8_unpack(int64_t n, int32_t dtype, const void *q, const void *scale,
                                void *x, void *stream);
 
+/* ---- the selective scan, its convolution, group norm and AdamW ----------- */
+
+/* Tensors of `dtype` and fp32 ones are aligned to their element here, ws, saved and
+ * 8-bit moments to 16 bytes.  Inputs named with a pitch may be slices of wider rows (a half of a
+ * projection's output): row (b, t) starts at element (b T + t) pitch; 0 means
+ * dense.  Everything else is contiguous.  Outputs overlap neither inputs nor each
+ * other, but where it says so.  Sequences, positions, lengths and reverse are those
+ * of pyramid_scan_forward: outputs at steps that a sequence does not have are 0,
+ * and what inputs hold there does not matter. */
+
+/* Short causal convolution along the middle axis of [B][T][I], K taps a channel:
+ *   a_s = bias + sum_k w[i][k] x_{s - (K - 1) + k},  y_s = act(a_s),
+ * x at positions below 0 being the K - 1 rows of `state`, oldest first.
+ *   x, y        : [B][T][I] in `dtype`;  w [I][K], bias [I] (or NULL) in `dtype`.
+ *   act         : 0 none, 1 SiLU a sigmoid(a).
+ *   state       : NULL (zeros), or [B][K - 1][I] in `dtype`.
+ *   state_out   : NULL, or [B][K - 1][I]: the last K - 1 inputs of each sequence
+ *                 (of the state, where it is shorter), overwritten; may be
+ *                 `state` itself, so single steps (T = 1) carry it in place.
+ * B, T, I >= 1, 1 <= K <= 8, B I <= 2^30, T <= 2^31, B T I <= 2^38. */
+size_t pyramid_causal_conv_workspace_size(int64_t B, int64_t T, int64_t I, int32_t K);
+int pyramid_causal_conv_forward(int64_t B, int64_t T, int64_t I, int32_t K, int32_t dtype,
+                                int32_t act, int32_t reverse, const void *x, int64_t x_pitch,
+                                const void *w, const void *bias, const int32_t *lengths,
+                                const void *state, void *y, void *state_out, void *stream);
+
+/* Gradient of pyramid_causal_conv_forward (arguments as there):
+ *   dy          : [B][T][I] in `dtype`;  dstate_out: NULL (zeros), or fp32
+ *                 [B][K - 1][I], the gradient of state_out.
+ *   dx          : [B][T][I] in `dtype`, overwritten.
+ *   dw          : fp32 [I][K], db: NULL or fp32 [I], overwritten (fixed order of the sums).
+ *   dstate      : NULL, or fp32 [B][K - 1][I], the gradient of `state`.
+ *   ws          : at least pyramid_causal_conv_workspace_size() bytes. */
+int pyramid_causal_conv_backward(int64_t B, int64_t T, int64_t I, int32_t K, int32_t dtype,
+                                 int32_t act, int32_t reverse, const void *x, int64_t x_pitch,
+                                 const void *w, const void *bias, const int32_t *lengths,
+                                 const void *state, const void *dy, const void *dstate_out,
+                                 void *dx, void *dw, void *db, void *dstate, void *ws,
+                                 size_t ws_bytes, void *stream);
+
+/* Selective state space scan along the middle axis of [B][T][I]: S states a channel
+ * that decay and take in the input as each step says.
+ *   d_s = delta + delta_bias, of it softplus(d) = log(1 + exp(d)) with softplus = 1,
+ *   h_s[i][k] = exp(d_s A[i][k]) h_{s-1}[i][k] + d_s u_s[i] B_s[k],  h_{-1} = h0,
+ *   p_s[i] = sum_k C_s[k] h_s[i][k] + D[i] u_s[i],
+ *   y_s = p_s, or p_s z_s sigmoid(z_s) with z.
+ *   u, delta, z : [B][T][I] in `dtype` with pitches (z may be NULL).
+ *   A           : fp32 [I][S];  D, delta_bias: NULL (zeros), or fp32 [I].
+ *   Bm, Cm      : [B][T][S] in `dtype` with pitches: the same for all channels.
+ *   h0, hT      : NULL, or fp32 [B][I][S]: the state before (NULL: zeros) and after; hT may
+ *                 be h0 itself, so single steps (T = 1) update a state in place.
+ *   saved       : NULL, or pyramid_selective_scan_saved_size() bytes for the
+ *                 backward: fp32 [B][ceil(T/n)][I][S], the state before positions
+ *                 0, n, ...; n = 64, or 32 for S > 16, 16 for S > 32.
+ *   ws          : at least pyramid_selective_scan_workspace_size() bytes (`backward`: 0
+ *                 for the forward, 1 for the backward).
+ * States are fp32 whatever the storage type.  B, T, I >= 1, 1 <= S <= 64,
+ * B I <= 2^30, T <= 2^31, B T I <= 2^38, B I S <= 2^34, B ceil(I/16) <= 2^22. */
+size_t pyramid_selective_scan_workspace_size(int64_t B, int64_t T, int64_t I, int32_t S,
+                                             int32_t backward);
+size_t pyramid_selective_scan_saved_size(int64_t B, int64_t T, int64_t I, int32_t S);
+int pyramid_selective_scan_forward(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype,
+                                   int32_t reverse, int32_t softplus, const void *u, int64_t u_pitch,
+                                   const void *delta, int64_t delta_pitch, const void *A,
+                                   const void *Bm, int64_t B_pitch, const void *Cm, int64_t C_pitch,
+                                   const void *D, const void *z, int64_t z_pitch,
+                                   const void *delta_bias, const int32_t *lengths, const void *h0,
+                                   void *y, void *hT, void *saved, void *ws, size_t ws_bytes,
+                                   void *stream);
+
+/* Gradient of pyramid_selective_scan_forward (arguments as there, saved the
+ * forward's).  Sums over channels, steps and sequences are made in a fixed order.
+ *   dy          : [B][T][I] in `dtype`;  dhT: NULL (zeros), or fp32 [B][I][S].
+ *   du, ddelta, dz : [B][T][I] in `dtype`, overwritten (dz with z, else NULL).
+ *   dA          : fp32 [I][S], overwritten;  dD, ddelta_bias: NULL, or fp32 [I].
+ *   dB, dC      : [B][T][S] in `dtype`, overwritten.
+ *   dh0         : NULL, or fp32 [B][I][S], overwritten; may be dhT itself. */
+int pyramid_selective_scan_backward(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype,
+                                    int32_t reverse, int32_t softplus, const void *u, int64_t u_pitch,
+                                    const void *delta, int64_t delta_pitch, const void *A,
+                                    const void *Bm, int64_t B_pitch, const void *Cm, int64_t C_pitch,
+                                    const void *D, const void *z, int64_t z_pitch,
+                                    const void *delta_bias, const int32_t *lengths, const void *saved,
+                                    const void *dy, const void *dhT, void *du, void *ddelta, void *dA,
+                                    void *dB, void *dC, void *dD, void *dz, void *ddelta_bias,
+                                    void *dh0, void *ws, size_t ws_bytes, void *stream);
+
+/* Group norm over volumes of V voxels (any number of axes) of C channels, channels
+ * last, with an activation: group g of a volume is channels g C/G .. (g + 1) C/G - 1 of all
+ * its voxels,
+ *   mean, var over the group, xh = (x - mean) / sqrt(var + eps),
+ *   v = gamma[c] xh + beta[c],  y = act(v)   (act: 0 none, 1 SiLU).
+ *   x, y        : [N][V][C], gamma, beta [C] in `dtype`; sums of the statistics in 64
+ *                 bits; eps > 0.
+ *   stats       : NULL, or fp32 [N][G][2], overwritten with (mean, rstd) for the
+ *                 backward, whose (x - mean) is that of the rounded mean.
+ *   ws          : at least pyramid_group_norm_workspace_size() bytes.
+ * 1 <= C <= 16384, G divides C, N <= 2^22, V <= 2^36, N V C <= 2^38. */
+size_t pyramid_group_norm_workspace_size(int64_t N, int64_t V, int32_t C, int32_t G);
+int pyramid_group_norm_forward(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype, int32_t act,
+                               float eps, const void *x, const void *gamma, const void *beta, void *y,
+                               void *stats, void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of pyramid_group_norm_forward: with dv = dy act'(v) and a = gamma dv,
+ *   dx = (a - mean(a) - xh mean(a xh)) rstd (means over the group),
+ *   dgamma = sum dv xh, dbeta = sum dv over all voxels (fixed order of the sums).
+ *   dx          : NULL, or [N][V][C] in `dtype`;  dgamma, dbeta: fp32 [C]. */
+int pyramid_group_norm_backward(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype, int32_t act,
+                                const void *x, const void *gamma, const void *beta, const void *stats,
+                                const void *dy, void *dx, void *dgamma, void *dbeta, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/* AdamW over `count` tensors, in place:
+ *   g = grad grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   theta -= lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay theta).
+ *   theta       : fp32;  copy: NULL, or bf16, overwritten with theta rounded.
+ *   grad        : `grad_dtype`;  n: elements (0: the segment is skipped).
+ *   m, v        : bits = 32: fp32.  bits = 8: one byte an element and, for each
+ *                 256 consecutive elements, an fp32 scale (pyramid_adamw_scales(n) of
+ *                 them in mscale and in vscale): the largest |m|, the largest v.  A code k
+ *                 stands for scale times  2^(k/8 - E) (1 + (k mod 8) / 8)  from k = 8 on
+ *                 (k/8 the integer quotient) and k 2^(-E - 2) below; E = 15 for m, whose top bit is its sign,
+ *                 31 for v.  Zeros are an empty state.  A value is held as the code on
+ *                 either side of it, the upper one with the probability of how near it is, by 16
+ *                 random bits: of element i of segment k, with h the hash mix32 of
+ *                 csrc/adamw.hip, h(i_low xor h(h(h(seed) + t) + k) xor h(i_high)) (32-bit halves of i),
+ *                 the low half for m, the high one for v.  A v above 0 is never held as 0.
+ *                 A block with an infinity or a NaN becomes NaN.
+ *   step        : t, from 1.  clock: NULL, or PLSTM_ADAMW_CLOCK_BYTES on the device,
+ *                 aligned to 8, whose first int64 is the number of updates so far: the call
+ *                 counts it up and takes t from there (`step` is ignored), so that
+ *                 replays of a captured call go on counting.
+ *   lr_dev, grad_scale : NULL, or one fp32 on the device: instead of lr; a factor of
+ *                 the gradients (clipping, a loss scale).
+ * 0 <= beta < 1, lr, weight_decay >= 0, eps > 0 (as fp32), n <= 2^34. */
+enum { PLSTM_ADAMW_CLOCK_BYTES = 24 };
+typedef struct plstm_adamw_segment {
+    float *theta;
+    void *copy;
+    const void *grad;
+    void *m, *v;
+    float *mscale, *vscale;
+    int64_t n;
+    float weight_decay;
+    int32_t reserved;
+} plstm_adamw_segment;
+int64_t pyramid_adamw_scales(int64_t n);
+int pyramid_adamw_step(int32_t count, const plstm_adamw_segment *segs, int32_t bits,
+                       int32_t grad_dtype, double lr, double beta1, double beta2, double eps,
+                       int64_t step, uint32_t seed, void *clock, const void *lr_dev,
+                       const void *grad_scale, void *stream);
+/* The fp32 values of 8-bit moments: m[k] and v[k] [n] take those of segment k. */
+int pyramid_adamw_moments(int32_t count, const plstm_adamw_segment *segs, void *const *m,
+                          void *const *v, void *stream);
+
 /* Forward implementation selection, for testing and tuning (process-wide):
  * 0 = automatic (default): the persistent MFMA sweep where it supports the
  * shape (fp32, O = 16, C <= 4, grid co-resident), else the plane-step MFMA

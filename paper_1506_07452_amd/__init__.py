@@ -37,6 +37,13 @@ __all__ = [
     "pyramid_layer_norm_backward", "pyramid_scan_workspace_size", "pyramid_scan_saved_size",
     "pyramid_scan_forward", "pyramid_scan_backward", "pyramid_checkpoint8_scales",
     "pyramid_checkpoint8_pack", "pyramid_checkpoint8_unpack", "checkpoint8_empty",
+    "pyramid_causal_conv_workspace_size", "pyramid_causal_conv_forward",
+    "pyramid_causal_conv_backward", "pyramid_selective_scan_workspace_size",
+    "pyramid_selective_scan_saved_size", "pyramid_selective_scan_forward",
+    "pyramid_selective_scan_backward", "pyramid_group_norm_workspace_size",
+    "pyramid_group_norm_forward", "pyramid_group_norm_backward", "plstm_adamw_segment",
+    "pyramid_adamw_scales", "pyramid_adamw_step", "pyramid_adamw_moments", "AdamW",
+    "PLSTM_ADAMW_CLOCK_BYTES",
 ]
 
 PLSTM_F32 = 0
@@ -46,6 +53,7 @@ PLSTM_MAX_CUBES = 64
 PLSTM_DEVICE_WAIT_GAVE_UP = 1
 PLSTM_NOALLOC_SCRATCH_BYTES = 256 << 20
 PLSTM_ESCRATCH = -6
+PLSTM_ADAMW_CLOCK_BYTES = 24
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libpyramid_lstm.so")
@@ -79,6 +87,13 @@ class plstm_cube(ctypes.Structure):
 class plstm_param_segment(ctypes.Structure):
     _fields_ = [("theta", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("ms", ctypes.c_void_p),
                 ("mom", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class plstm_adamw_segment(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("mscale", ctypes.c_void_p),
+                ("vscale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -172,6 +187,36 @@ def load():
     lib.pyramid_checkpoint8_pack.restype = ctypes.c_int
     lib.pyramid_checkpoint8_unpack.argtypes = [i64, i32] + [vp] * 4
     lib.pyramid_checkpoint8_unpack.restype = ctypes.c_int
+    lib.pyramid_causal_conv_workspace_size.argtypes = [i64] * 3 + [i32]
+    lib.pyramid_causal_conv_workspace_size.restype = sz
+    lib.pyramid_causal_conv_forward.argtypes = [i64] * 3 + [i32] * 4 + [vp, i64] + [vp] * 7
+    lib.pyramid_causal_conv_forward.restype = ctypes.c_int
+    lib.pyramid_causal_conv_backward.argtypes = [i64] * 3 + [i32] * 4 + [vp, i64] + [vp] * 11 + \
+        [sz, vp]
+    lib.pyramid_causal_conv_backward.restype = ctypes.c_int
+    lib.pyramid_selective_scan_workspace_size.argtypes = [i64] * 3 + [i32] * 2
+    lib.pyramid_selective_scan_workspace_size.restype = sz
+    lib.pyramid_selective_scan_saved_size.argtypes = [i64] * 3 + [i32]
+    lib.pyramid_selective_scan_saved_size.restype = sz
+    select = [i64] * 3 + [i32] * 4 + [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp]
+    lib.pyramid_selective_scan_forward.argtypes = select + [vp] * 5 + [sz, vp]
+    lib.pyramid_selective_scan_forward.restype = ctypes.c_int
+    lib.pyramid_selective_scan_backward.argtypes = select + [vp] * 13 + [sz, vp]
+    lib.pyramid_selective_scan_backward.restype = ctypes.c_int
+    lib.pyramid_group_norm_workspace_size.argtypes = [i64] * 2 + [i32] * 2
+    lib.pyramid_group_norm_workspace_size.restype = sz
+    lib.pyramid_group_norm_forward.argtypes = [i64] * 2 + [i32] * 4 + [f32] + [vp] * 6 + [sz, vp]
+    lib.pyramid_group_norm_forward.restype = ctypes.c_int
+    lib.pyramid_group_norm_backward.argtypes = [i64] * 2 + [i32] * 4 + [vp] * 9 + [sz, vp]
+    lib.pyramid_group_norm_backward.restype = ctypes.c_int
+    f64, segp = ctypes.c_double, ctypes.POINTER(plstm_adamw_segment)
+    lib.pyramid_adamw_scales.argtypes = [i64]
+    lib.pyramid_adamw_scales.restype = i64
+    lib.pyramid_adamw_step.argtypes = [i32, segp, i32, i32, f64, f64, f64, f64, i64,
+                                       ctypes.c_uint32, vp, vp, vp, vp]
+    lib.pyramid_adamw_step.restype = ctypes.c_int
+    lib.pyramid_adamw_moments.argtypes = [i32, segp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]
+    lib.pyramid_adamw_moments.restype = ctypes.c_int
     lib.pyramid_lstm_timing_enable.argtypes = [ctypes.c_int]
     lib.pyramid_lstm_timing_enable.restype = ctypes.c_int
     lib.pyramid_lstm_timing_read.argtypes = [ctypes.c_int, ctypes.c_char_p,
@@ -648,6 +693,15 @@ def _saved(saved, B, T, I, dev):
 _scan_ws = {}
 
 
+def _shared_ws(x, dev):
+    """256 bytes that calls which need no workspace share: they do not touch them."""
+    shared = _scan_ws.get(dev)
+    if shared is None:
+        ws = _workspace(256, x.device)
+        shared = _scan_ws[dev] = (ws,) + _bytes(ws, dev)
+    return shared[0]
+
+
 def _scan_workspace(ws, x, dev, stream):
     """`ws`, or one made with torch, its pointer and its bytes.  A call that
     needs none takes 256 bytes as every call does, and shares them: it does not
@@ -655,11 +709,8 @@ def _scan_workspace(ws, x, dev, stream):
     if ws is None:
         need = pyramid_scan_workspace_size(*x.shape)
         if need <= 256:
-            shared = _scan_ws.get(dev)
-            if shared is None:
-                ws = _workspace(256, x.device)
-                shared = _scan_ws[dev] = (ws,) + _bytes(ws, dev)
-            return shared
+            _shared_ws(x, dev)
+            return _scan_ws[dev]
         ws = _temporary(need, x.device, stream)
     return (ws,) + _bytes(ws, dev)
 
@@ -727,6 +778,376 @@ def pyramid_checkpoint8_unpack(q, scale, x, stream=None):
     dt, px, dev = _main("x", x, None)
     pq, ps = _codes("q", q, scale, x, dev)
     _run("pyramid_checkpoint8_unpack", dev, stream, x.numel(), dt, pq, ps, px)
+
+
+_ACT = {"none": 0, "silu": 1}
+
+
+def _act(act):
+    if act not in _ACT:
+        raise ValueError("act must be one of %s" % ", ".join(_ACT))
+    return _ACT[act]
+
+
+def _pitched(name, t, shape, dtype, dev):
+    """Pointer and pitch of an input [B][T][n] that may be a slice of wider rows: the
+    elements of a row next to each other, rows (b, t) at (b T + t) pitch (0: dense)."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch.Tensor, got %r" % type(t))
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.get_device() != dev:
+        raise ValueError("%s must be %s %s on cuda:%d, got %s %s on %s" % (
+            name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device))
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    B, T, n = shape
+    sb, st, sn = t.stride()
+    pitch = st if T > 1 else sb if B > 1 else n
+    if (n > 1 and sn != 1) or pitch < n or (B > 1 and sb != T * pitch):
+        raise ValueError("%s must be contiguous or a slice of contiguous rows, got strides %s" % (
+            name, list(t.stride())))
+    return t.data_ptr(), pitch
+
+
+def _main_pitched(name, t):
+    """As _main, for a main input [B][T][n] that may be a slice of wider rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch.Tensor, got %r" % type(t))
+    code = _DT.get(t.dtype)
+    if code is None or t.dim() != 3:
+        raise ValueError("%s must be float32 or bfloat16 with 3 dimensions" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    dev = t.get_device()
+    return (code, dev) + _pitched(name, t, t.shape, t.dtype, dev)
+
+
+@functools.lru_cache(maxsize=256)
+def pyramid_causal_conv_workspace_size(B: int, T: int, I: int, K: int) -> int:
+    return int(load().pyramid_causal_conv_workspace_size(B, T, I, K))
+
+
+def pyramid_causal_conv_forward(x, w, bias, y, act="none", reverse=False, lengths=None, state=None,
+                                state_out=None, stream=None):
+    """Short causal convolution along axis 1 of x [B][T][I] (contiguous, or a slice of
+    wider rows) into y [B][T][I]: w [I][K], bias [I] or None, one dtype; act "none" or
+    "silu".  state, state_out [B][K-1][I] of that dtype are the last inputs
+    before and after (state_out may be state); lengths, reverse as in
+    pyramid_scan_forward."""
+    dt, dev, px, pitch = _main_pitched("x", x)
+    B, T, I = x.shape
+    K = w.shape[-1] if w.dim() == 2 else 0
+    _run("pyramid_causal_conv_forward", dev, stream, B, T, I, K, dt, _act(act), int(bool(reverse)),
+         px, pitch, _tensor("w", w, (I, K), x.dtype, dev), _tensor("bias", bias, (I,), x.dtype, dev),
+         _tensor("lengths", lengths, (B,), torch.int32, dev),
+         _tensor("state", state, (B, K - 1, I), x.dtype, dev) or None,
+         _tensor("y", y, x.shape, x.dtype, dev),
+         _tensor("state_out", state_out, (B, K - 1, I), x.dtype, dev) or None)
+
+
+def pyramid_causal_conv_backward(x, w, bias, dy, dx, dw, db, act="none", reverse=False, lengths=None,
+                                 state=None, dstate_out=None, dstate=None, ws=None, stream=None):
+    """Gradients of pyramid_causal_conv_forward: dx [B][T][I], dw [I][K] and db [I] (or None) fp32,
+    dstate [B][K-1][I] fp32 (or None), from dy, dstate_out fp32 (or None) and the
+    forward's inputs."""
+    dt, dev, px, pitch = _main_pitched("x", x)
+    B, T, I = x.shape
+    K = w.shape[-1] if w.dim() == 2 else 0
+    if ws is None:
+        ws = _temporary(pyramid_causal_conv_workspace_size(B, T, I, K), x.device, stream)
+    _run("pyramid_causal_conv_backward", dev, stream, B, T, I, K, dt, _act(act), int(bool(reverse)),
+         px, pitch, _tensor("w", w, (I, K), x.dtype, dev), _tensor("bias", bias, (I,), x.dtype, dev),
+         _tensor("lengths", lengths, (B,), torch.int32, dev),
+         _tensor("state", state, (B, K - 1, I), x.dtype, dev) or None,
+         _tensor("dy", dy, x.shape, x.dtype, dev),
+         _tensor("dstate_out", dstate_out, (B, K - 1, I), torch.float32, dev) or None,
+         _tensor("dx", dx, x.shape, x.dtype, dev), _tensor("dw", dw, (I, K), torch.float32, dev),
+         _tensor("db", db, (I,), torch.float32, dev),
+         _tensor("dstate", dstate, (B, K - 1, I), torch.float32, dev) or None, *_bytes(ws, dev))
+
+
+@functools.lru_cache(maxsize=256)
+def pyramid_selective_scan_workspace_size(B: int, T: int, I: int, S: int, backward: int = 0) -> int:
+    return int(load().pyramid_selective_scan_workspace_size(B, T, I, S, int(backward)))
+
+
+@functools.lru_cache(maxsize=256)
+def pyramid_selective_scan_saved_size(B: int, T: int, I: int, S: int) -> int:
+    return int(load().pyramid_selective_scan_saved_size(B, T, I, S))
+
+
+def _select_saved(saved, B, T, I, S, dev):
+    if saved is None:
+        return None
+    if not saved.is_cuda or saved.get_device() != dev or not saved.is_contiguous() or \
+            saved.numel() * saved.element_size() < pyramid_selective_scan_saved_size(B, T, I, S):
+        raise ValueError("saved must hold pyramid_selective_scan_saved_size bytes on cuda:%d" % dev)
+    return saved.data_ptr()
+
+
+def _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev):
+    B, T, I = u.shape
+    S = A.shape[-1] if A.dim() == 2 else 0
+    f32 = torch.float32
+    return (B, T, I, S, dt, int(bool(reverse)), int(bool(softplus)),
+            *_pitched("u", u, u.shape, u.dtype, dev),
+            *_pitched("delta", delta, u.shape, u.dtype, dev), _tensor("A", A, (I, S), f32, dev),
+            *_pitched("Bm", Bm, (B, T, S), u.dtype, dev), *_pitched("Cm", Cm, (B, T, S), u.dtype, dev),
+            _tensor("D", D, (I,), f32, dev), *_pitched("z", z, u.shape, u.dtype, dev),
+            _tensor("delta_bias", delta_bias, (I,), f32, dev),
+            _tensor("lengths", lengths, (B,), torch.int32, dev))
+
+
+def pyramid_selective_scan_forward(u, delta, A, Bm, Cm, y, D=None, z=None, delta_bias=None,
+                                   softplus=False, reverse=False, lengths=None, h0=None, hT=None,
+                                   saved=None, ws=None, stream=None):
+    """Selective state space scan along axis 1 of u [B][T][I] into y (its shape and
+    dtype): with d = delta + delta_bias (softplus of it, if asked), per channel i and
+    state k: h = exp(d A[i][k]) h + d u Bm[t][k], y = sum_k Cm[t][k] h + D[i] u, times
+    z sigmoid(z) with z.  delta, z [B][T][I], Bm, Cm [B][T][S] have u's dtype; u, delta, z, Bm and
+    Cm may be slices of wider rows; A [I][S], D, delta_bias [I] are fp32.  lengths and
+    reverse as in pyramid_scan_forward; h0, hT [B][I][S] fp32 are the state before and
+    after (hT may be h0); saved (pyramid_selective_scan_saved_size bytes) keeps what
+    the backward needs."""
+    dt, dev, _, _ = _main_pitched("u", u)
+    args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev)
+    B, T, I, S = args[:4]
+    if ws is None:
+        need = pyramid_selective_scan_workspace_size(B, T, I, S)
+        ws = _shared_ws(u, dev) if need <= 256 else _temporary(need, u.device, stream)
+    _run("pyramid_selective_scan_forward", dev, stream, *args,
+         _tensor("h0", h0, (B, I, S), torch.float32, dev), _tensor("y", y, u.shape, u.dtype, dev),
+         _tensor("hT", hT, (B, I, S), torch.float32, dev), _select_saved(saved, B, T, I, S, dev),
+         *_bytes(ws, dev))
+
+
+def pyramid_selective_scan_backward(u, delta, A, Bm, Cm, saved, dy, du, ddelta, dA, dB, dC, D=None,
+                                    z=None, delta_bias=None, softplus=False, dD=None, dz=None,
+                                    ddelta_bias=None, reverse=False, lengths=None, dhT=None, dh0=None,
+                                    ws=None, stream=None):
+    """Gradients of pyramid_selective_scan_forward: du, ddelta (dz, with z) [B][T][I] and
+    dB, dC [B][T][S] in u's dtype; dA [I][S], dD and ddelta_bias [I] (or None), dh0 [B][I][S]
+    (or None) in fp32, from dy, dhT (or None) and the forward's inputs and saved buffer."""
+    dt, dev, _, _ = _main_pitched("u", u)
+    args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev)
+    B, T, I, S = args[:4]
+    if ws is None:
+        ws = _temporary(pyramid_selective_scan_workspace_size(B, T, I, S, 1), u.device, stream)
+    f32 = torch.float32
+    _run("pyramid_selective_scan_backward", dev, stream, *args, _select_saved(saved, B, T, I, S, dev),
+         _tensor("dy", dy, u.shape, u.dtype, dev), _tensor("dhT", dhT, (B, I, S), f32, dev),
+         _tensor("du", du, u.shape, u.dtype, dev), _tensor("ddelta", ddelta, u.shape, u.dtype, dev),
+         _tensor("dA", dA, (I, S), f32, dev), _tensor("dB", dB, (B, T, S), u.dtype, dev),
+         _tensor("dC", dC, (B, T, S), u.dtype, dev), _tensor("dD", dD, (I,), f32, dev),
+         _tensor("dz", dz, u.shape, u.dtype, dev), _tensor("ddelta_bias", ddelta_bias, (I,), f32, dev),
+         _tensor("dh0", dh0, (B, I, S), f32, dev), *_bytes(ws, dev))
+
+
+@functools.lru_cache(maxsize=256)
+def pyramid_group_norm_workspace_size(N: int, V: int, C: int, G: int) -> int:
+    return int(load().pyramid_group_norm_workspace_size(N, V, C, G))
+
+
+def _volumes(name, x):
+    """Type code, pointer, device, N, V and C of x [N][...][C]."""
+    dt, px, dev = _main(name, x, None)
+    if x.dim() < 2:
+        raise ValueError("%s must be [N][...][C]" % name)
+    N, C = x.shape[0], x.shape[-1]
+    return dt, px, dev, N, x.numel() // max(N * C, 1), C
+
+
+def _group_norm_ws(ws, N, V, C, G, x, dev, stream):
+    if ws is None:
+        need = pyramid_group_norm_workspace_size(N, V, C, G)
+        ws = _shared_ws(x, dev) if need <= 256 else _temporary(need, x.device, stream)
+    return _bytes(ws, dev)
+
+
+def pyramid_group_norm_forward(x, gamma, beta, y, groups, act="none", stats=None, eps=1e-5, ws=None,
+                               stream=None):
+    """Group norm over the voxels and C / groups consecutive channels of each volume of x
+    [N][...][C], times gamma plus beta [C], act ("none" or "silu") of it into y; one dtype.
+    stats [N][groups][2] fp32 takes (mean, rstd) for the backward."""
+    dt, px, dev, N, V, C = _volumes("x", x)
+    _run("pyramid_group_norm_forward", dev, stream, N, V, C, groups, dt, _act(act), eps, px,
+         _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
+         _tensor("y", y, x.shape, x.dtype, dev),
+         _tensor("stats", stats, (N, groups, 2), torch.float32, dev),
+         *_group_norm_ws(ws, N, V, C, groups, x, dev, stream))
+
+
+def pyramid_group_norm_backward(x, gamma, beta, stats, dy, dx, dgamma, dbeta, groups, act="none",
+                                ws=None, stream=None):
+    """Gradients of pyramid_group_norm_forward: dx (or None) of x's shape, dgamma and dbeta [C]
+    fp32, from dy, the forward's inputs and its stats."""
+    dt, px, dev, N, V, C = _volumes("x", x)
+    _run("pyramid_group_norm_backward", dev, stream, N, V, C, groups, dt, _act(act), px,
+         _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
+         _tensor("stats", stats, (N, groups, 2), torch.float32, dev),
+         _tensor("dy", dy, x.shape, x.dtype, dev), _tensor("dx", dx, x.shape, x.dtype, dev),
+         _tensor("dgamma", dgamma, (C,), torch.float32, dev),
+         _tensor("dbeta", dbeta, (C,), torch.float32, dev),
+         *_group_norm_ws(ws, N, V, C, groups, x, dev, stream))
+
+
+def pyramid_adamw_scales(n: int) -> int:
+    return int(load().pyramid_adamw_scales(n))
+
+
+def _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay):
+    """Segments of an AdamW call without its gradients, the bits of its moments and its device."""
+    count = len(params)
+    if count < 1 or not len(m) == len(v) == count or (copies is not None and len(copies) != count):
+        raise ValueError("params, m, v (and copies) must have the same length, at least 1")
+    if m[0].dtype not in (torch.float32, torch.uint8):
+        raise ValueError("moments must be float32 or (8-bit codes) uint8")
+    bits = 32 if m[0].dtype == torch.float32 else 8
+    if bits == 8 and (mscale is None or vscale is None or not len(mscale) == len(vscale) == count):
+        raise ValueError("8-bit moments need mscale and vscale, one tensor per parameter")
+    decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+    if len(decay) != count:
+        raise ValueError("one weight decay, or one per parameter")
+    segs = (plstm_adamw_segment * count)()
+    f32 = torch.float32
+    for k, p in enumerate(params):
+        dt, pp, dev = _main("params", p, None)
+        if dt != PLSTM_F32 or (k and dev != dev0):
+            raise ValueError("parameters must be float32 on one device")
+        dev0 = dev
+        n = p.numel()
+        segs[k].theta, segs[k].n, segs[k].weight_decay = pp, n, float(decay[k])
+        segs[k].m = _tensor("m", m[k], p.shape, m[0].dtype, dev)
+        segs[k].v = _tensor("v", v[k], p.shape, m[0].dtype, dev)
+        if bits == 8:
+            segs[k].mscale = _tensor("mscale", mscale[k], (-(-n // 256),), f32, dev)
+            segs[k].vscale = _tensor("vscale", vscale[k], (-(-n // 256),), f32, dev)
+        if copies is not None:
+            segs[k].copy = _tensor("copies", copies[k], p.shape, torch.bfloat16, dev)
+    return segs, bits, dev0
+
+
+def _adamw_grads(segs, params, grads, dev):
+    """Puts the gradients into the segments (None: the tensor is left alone); their type."""
+    if len(grads) != len(params):
+        raise ValueError("one gradient (or None) per parameter")
+    dtype = None
+    for seg, p, g in zip(segs, params, grads):
+        if g is None:
+            seg.n = 0
+            continue
+        if dtype is None:
+            dtype = g.dtype
+            if dtype not in _DT:
+                raise ValueError("gradients must be float32 or bfloat16")
+        seg.grad = _tensor("grads", g, p.shape, dtype, dev)
+        seg.n = g.numel()
+    return PLSTM_F32 if dtype is None else _DT[dtype]
+
+
+def _adamw_run(segs, bits, grad_dtype, dev, stream, lr, betas, eps, step, seed, clock, grad_scale):
+    lr_dev = None
+    if isinstance(lr, torch.Tensor):
+        lr, lr_dev = 0.0, _tensor("lr", lr, (1,), torch.float32, dev)
+    _run("pyramid_adamw_step", dev, stream, len(segs), segs, bits, grad_dtype, lr, betas[0], betas[1],
+         eps, step, seed & 0xffffffff, _tensor("clock", clock, (3,), torch.int64, dev), lr_dev,
+         _tensor("grad_scale", grad_scale, (1,), torch.float32, dev))
+
+
+def pyramid_adamw_step(params, grads, m, v, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+                       mscale=None, vscale=None, copies=None, seed=0, clock=None, grad_scale=None,
+                       stream=None):
+    """AdamW update number `step` (from 1) over lists of device tensors, in place: params fp32, grads
+    fp32 or bf16 (None: that tensor is left alone), m and v fp32, or uint8 codes with their
+    scales mscale and vscale (fp32, one per 256 elements, pyramid_adamw_scales).  copies: bf16
+    tensors that take the updated parameters.  weight_decay: a number, or one per tensor.  lr: a
+    number, or fp32 [1] on the device; grad_scale: None, or such a factor of the gradients.  clock:
+    None, or int64 [3] on the device whose first element counts the updates (`step` is then
+    ignored), for steps in captured graphs.  seed: of the rounding of 8-bit moments."""
+    segs, bits, dev = _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay)
+    dtype = _adamw_grads(segs, params, grads, dev)
+    _adamw_run(segs, bits, dtype, dev, stream, lr, betas, eps, step, seed, clock, grad_scale)
+
+
+def pyramid_adamw_moments(m, v, mscale, vscale, mout, vout, stream=None):
+    """fp32 values mout, vout of lists of 8-bit moments m, v with their scales."""
+    segs, bits, dev = _adamw_segments(mout, m, v, mscale, vscale, None, 0.0)
+    if bits != 8:
+        raise ValueError("m and v must be 8-bit codes")
+    count = len(mout)
+    pm, pv = (ctypes.c_void_p * count)(), (ctypes.c_void_p * count)()
+    for k in range(count):
+        pm[k] = segs[k].theta
+        pv[k] = _tensor("vout", vout[k], mout[k].shape, torch.float32, dev)
+    _run("pyramid_adamw_moments", dev, stream, count, segs, pm, pv)
+
+
+class AdamW:
+    """AdamW for a fixed list of fp32 parameter tensors, beside RMSprop; moments in 32
+    bits or in 8 (`bits`), zero at first or taken from `state` (what state() gives).
+    copies: bf16 tensors (or None each) that take the updated parameters.
+    weight_decay: a number or one per tensor.  capturable=True keeps the number of updates on
+    the device, so that a step captured in a graph goes on counting when it is replayed."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32,
+                 copies=None, seed=0, state=None, capturable=False):
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        self.params = list(params)
+        self.lr, self.betas, self.eps, self.seed, self.bits = lr, betas, eps, seed, bits
+        self.copies = None if copies is None else list(copies)
+        self.mscale = self.vscale = None
+        if state is None:
+            dt = torch.float32 if bits == 32 else torch.uint8
+            self.m, self.v = ([torch.zeros_like(p, dtype=dt, memory_format=torch.contiguous_format)
+                               for p in self.params] for _ in range(2))
+            if bits == 8:
+                self.mscale, self.vscale = ([torch.zeros(-(-p.numel() // 256), device=p.device)
+                                             for p in self.params] for _ in range(2))
+            t = 0
+        else:
+            self.m, self.v, t = list(state["m"]), list(state["v"]), int(state["t"])
+            if bits == 8:
+                self.mscale, self.vscale = list(state["mscale"]), list(state["vscale"])
+        self._segs, got, self._dev = _adamw_segments(self.params, self.m, self.v, self.mscale,
+                                                     self.vscale, self.copies, weight_decay)
+        if got != bits:
+            raise ValueError("state has moments in %d bits" % got)
+        self._t, self._clock = t, None
+        if capturable:
+            self._clock = torch.tensor([t, 0, 0], dtype=torch.int64, device=self.params[0].device)
+
+    @property
+    def t(self):
+        """Updates so far (capturable: read from the device)."""
+        return self._t if self._clock is None else int(self._clock[0])
+
+    def state(self):
+        """The moments, their scales and the number of updates: the tensors themselves."""
+        out = {"m": self.m, "v": self.v, "t": self.t}
+        if self.bits == 8:
+            out.update(mscale=self.mscale, vscale=self.vscale)
+        return out
+
+    def step(self, grads, lr=None, grad_scale=None, stream=None):
+        """One update from `grads` (one per parameter, None to leave it alone); lr and
+        grad_scale as in pyramid_adamw_step."""
+        for seg, p in zip(self._segs, self.params):
+            seg.theta = p.data_ptr()
+        dtype = _adamw_grads(self._segs, self.params, grads, self._dev)
+        _adamw_run(self._segs, self.bits, dtype, self._dev, stream, self.lr if lr is None else lr,
+                   self.betas, self.eps, self._t + 1, self.seed, self._clock, grad_scale)
+        self._t += 1
+
+    def moments(self, stream=None):
+        """fp32 (m, v) of each parameter: the moments themselves, or what their codes stand for."""
+        if self.bits == 32:
+            return list(zip(self.m, self.v))
+        with torch.cuda.device(self._dev):
+            mout, vout = ([torch.empty(p.shape, device=p.device) for p in self.params] for _ in range(2))
+        pyramid_adamw_moments(self.m, self.v, self.mscale, self.vscale, mout, vout, stream)
+        return list(zip(mout, vout))
 
 
 def pyramid_lstm_timing_enable(on: bool) -> None:
