@@ -551,12 +551,13 @@ int pyramid_causal_conv_backward(int64_t B, int64_t T, int64_t I, int32_t K, int
  *   h0, hT      : NULL, or fp32 [B][I][S]: the state before (NULL: zeros) and after; hT may
  *                 be h0 itself, so single steps (T = 1) update a state in place.
  *   saved       : NULL, or pyramid_selective_scan_saved_size() bytes for the
- *                 backward: fp32 [B][ceil(T/n)][I][S], the state before positions
- *                 0, n, ...; n = 64, or 32 for S > 16, 16 for S > 32.
+ *                 backward: fp32 [B][ceil(T/16)][I][S], the state before positions
+ *                 0, 16, ...
  *   ws          : at least pyramid_selective_scan_workspace_size() bytes (`backward`: 0
  *                 for the forward, 1 for the backward).
  * States are fp32 whatever the storage type.  B, T, I >= 1, 1 <= S <= 64,
- * B I <= 2^30, T <= 2^31, B T I <= 2^38, B I S <= 2^34, B ceil(I/16) <= 2^22. */
+ * I and pitches <= 2^24, B I <= 2^30, T <= 2^31, B T I <= 2^38, B I S <= 2^34,
+ * B ceil(I/16) <= 2^22. */
 size_t pyramid_selective_scan_workspace_size(int64_t B, int64_t T, int64_t I, int32_t S,
                                              int32_t backward);
 size_t pyramid_selective_scan_saved_size(int64_t B, int64_t T, int64_t I, int32_t S);

@@ -5,14 +5,15 @@
 //   G_s = C_s dp_s + a_{s+1} G_{s+1}  (the last one takes dhT as well),  dh0 = a_0 G_0
 //   dC = sum_i dp h,  dB = sum_i G d u,  q = sum_k G B,  w = sum_k G a h_{s-1} A
 //   du = d q + D dp,  dd = u q + w,  dA = sum G a h_{s-1} d,  dD = sum dp u,  dz = dy p silu'(z)
-// A workgroup of 8 waves has 16 channels and walks its sequence in tiles.  A lane has one
-// channel and a quarter of its states (SR of them), a wave a run of R positions of a tile: it folds its
-// run to (P, H), last state = P h + H, keeping the decays in registers; the waves
-// exchange these through LDS and run again from the state that reaches them.  So a decay costs one exponential,
-// whatever the run's place: the quarter-rate v_exp_f32 (16 of the some 36 cycles that a
-// state of a position costs a wave) bounds everything but the smallest S.
-// What belongs to an element and not to its states (softplus, d u, the gate) is done once, two
-// elements a thread, and passes through LDS.
+// A wave walks a piece of a sequence by itself.  Its four rows of 16 lanes have a quarter of the
+// states each (SR of them), the lanes of a row CL channels each, so a lane has CL SR states in registers
+// and the rows of B and C that it reads from LDS serve all its channels.  What belongs to an element and
+// not to its states (softplus, d u, the gate) is made once, by the lane whose row the element's sum
+// over the states comes out in, and passes to the other rows through LDS.
+// Few channels and long sequences do not fill the card: a sequence is then cut into chunks whose
+// folds (last state = exp(A sum d) h + H) are made first and chained by a small launch.
+#include <algorithm>
+
 #include "sequence.h"
 #include "timing.h"
 
@@ -20,36 +21,50 @@ namespace plstm {
 namespace {
 
 constexpr int kSelMaxS = 64;
-constexpr int kSelCh = 16;              // channels of a workgroup, in the lanes of a row of 16
-constexpr int kSelW = 8;                // waves
-constexpr int kSelThreads = 64 * kSelW;
-constexpr float kLog2e = 1.44269504f;
+constexpr int kSelKeep = 16;            // positions between the states that a training forward keeps
+constexpr int kSelStage = 8;            // positions that a forward wave stages at a time
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
-// States a lane and positions of a wave's run, so that SR R decays fit its registers.
 inline int sel_sr(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
-__host__ __device__ constexpr int sel_run(int SR) { return SR <= 4 ? 8 : 32 / SR; }
-// Positions of a tile, and between the states that a training forward keeps.
-__host__ __device__ constexpr int sel_tile(int SR) { return kSelW * sel_run(SR); }
+// Channels of a lane in the forward and the folds.
+__host__ __device__ constexpr int sel_cl(int SR) { return SR <= 4 ? 2 : 1; }
 
 struct SelArgs {
     long long B, T, I;
     int S, reverse, softplus;
     long long pu, pd, pz, pB, pC;       // elements from one row to the next
     const int32_t *lengths;
-    long long tiles;                    // workgroups across the channels
+    long long tiles;                    // waves across a sequence's channels
+    long long groups;                   // waves across all channels and sequences
     long long kept;                     // states that a sequence keeps
-    int chunks;                         // of a sequence, each with workgroups of its own
-    long long chunk;                    // positions of a chunk (whole tiles)
-    long long jobs;                     // backward: workgroups down the sequences and chunks
+    int chunks;                         // of a sequence, each with waves of its own
+    long long chunk;                    // positions of a chunk (a multiple of kSelKeep)
+    long long jobs;                     // backward: sequences' chunks that run at the same time
 };
 
-// Two elements from any element on, raw.
-template <typename T> struct Two;
-template <> struct Two<float> {
+// One or two elements from any element on, raw.
+template <typename T, int N> struct Few;
+template <typename T> struct Few<T, 1> {
+    typedef T V;
+    T w;
+    __device__ void load(const T *p, int have) { w = have > 0 ? *p : (T)0; }
+    __device__ void set(V v) { w = v; }
+    __device__ float get(int) const { return Store<T>::load(&w, 0); }
+    __device__ static void store(T *p, int have, const float *v)
+    {
+        if (have > 0) Store<T>::store(p, 0, *v);
+    }
+};
+template <> struct Few<float, 2> {
+    typedef uint32_t V __attribute__((ext_vector_type(2), aligned(4)));
     uint32_t w[2];
+    __device__ void set(V v)
+    {
+        w[0] = v[0];
+        w[1] = v[1];
+    }
     __device__ void load(const float *p, int have)
     {
-        typedef uint32_t V __attribute__((ext_vector_type(2), aligned(4)));
         w[0] = w[1] = 0;
         if (have >= 2) {
             const V r = *(const V *)p;
@@ -59,46 +74,42 @@ template <> struct Two<float> {
             w[0] = float_bits(*p);
         }
     }
-    __device__ float lo() const { return bits_float(w[0]); }
-    __device__ float hi() const { return bits_float(w[1]); }
-    __device__ static void store(float *p, int have, float a, float b)
+    __device__ float get(int e) const { return bits_float(w[e]); }
+    __device__ static void store(float *p, int have, const float *v)
     {
-        typedef uint32_t V __attribute__((ext_vector_type(2), aligned(4)));
-        if (have >= 2) *(V *)p = V{float_bits(a), float_bits(b)};
-        else if (have == 1) *p = a;
+        if (have >= 2) *(V *)p = V{float_bits(v[0]), float_bits(v[1])};
+        else if (have == 1) *p = v[0];
     }
 };
-template <> struct Two<uint16_t> {
+template <> struct Few<uint16_t, 2> {
     typedef uint32_t V __attribute__((aligned(2)));
     uint32_t w;
+    __device__ void set(V v) { w = v; }
     __device__ void load(const uint16_t *p, int have)
     {
         w = 0;
         if (have >= 2) w = *(const V *)p;
         else if (have == 1) w = *p;
     }
-    __device__ float lo() const { return bits_float(w << 16); }
-    __device__ float hi() const { return bits_float(w & 0xffff0000u); }
-    __device__ static void store(uint16_t *p, int have, float a, float b)
+    __device__ float get(int e) const { return bits_float(e ? w & 0xffff0000u : w << 16); }
+    __device__ static void store(uint16_t *p, int have, const float *v)
     {
-        if (have >= 2) *(V *)p = pack_bf16(a, b);
-        else if (have == 1) *p = (uint16_t)pack_bf16(a, a);
+        if (have >= 2) *(V *)p = pack_bf16(v[0], v[1]);
+        else if (have == 1) *p = (uint16_t)pack_bf16(v[0], v[0]);
     }
 };
 
-// log(1 + exp(v)) and its derivative sigmoid(v).  log(1 + e) for e = exp(-|v|): where 1 + e
-// rounds, its logarithm is that of another number, by the factor e / ((1 + e) - 1) (Kahan).
+// log(1 + exp(v)).  With e = exp(-|v|) and w = 1 + e rounded, log(1 + e) is log(w) and to first order what w has
+// lost, e - (w - 1), over w: left out, as what is lost is below 2^-24 and w is 1 where log(w) is small.
 __device__ inline float softplus_of(float v)
 {
-    const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e);
-    const float w = 1.0f + e, x = w - 1.0f;
-    const float l = x == 0.0f ? e : __builtin_amdgcn_logf(w) * 0.69314718f * (e * __builtin_amdgcn_rcpf(x));
-    return v > 0.0f ? v + l : v == v ? l : v;
+    const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), w = 1.0f + e;
+    return fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.0f)) + fmaxf(v, 0.0f);
 }
 
-// Sum over the four rows of 16 lanes (a channel's quarters of states) of R values: lane (row,
-// channel) gets that of value sel_row_value(row) + 4 q in v[q]; R = 2: value row / 2.
-// Two swaps of half waves and rows and three additions make four sums.
+// Sum over the four rows of 16 lanes (a channel's quarters of states) of 4 Q values: lane (row,
+// channel) gets that of value 4 q + row_value(row) in v[q].  Two swaps of half waves, one of rows and
+// three additions make four sums.
 __device__ inline void swap32(float &x, float &y)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(float_bits(x), float_bits(y), false, false);
@@ -111,303 +122,503 @@ __device__ inline void swap16(float &x, float &y)
     x = bits_float(r[0]);
     y = bits_float(r[1]);
 }
-template <int R>
-__device__ inline void sum_rows_of_lanes(float *v)
+template <int Q>
+__device__ inline void sum_states(float *v)
 {
-    if constexpr (R == 2) {
-        swap32(v[0], v[1]);
-        float s = v[0] + v[1], t = s;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        float *x = v + 4 * q;
+        swap32(x[0], x[1]);
+        swap32(x[2], x[3]);
+        float s = x[0] + x[1], t = x[2] + x[3];
         swap16(s, t);
-        v[0] = s + t;
-    } else {
-#pragma unroll
-        for (int q = 0; q < R / 4; ++q) {
-            float *x = v + 4 * q;
-            swap32(x[0], x[1]);
-            swap32(x[2], x[3]);
-            float s = x[0] + x[1], t = x[2] + x[3];
-            swap16(s, t);
-            v[q] = s + t;
-        }
+        v[q] = s + t;
     }
 }
-template <int R> __device__ inline int row_value(int row) { return R == 2 ? row >> 1 : (row & 1) << 1 | row >> 1; }
-// Writes those sums, position first + r of channel ch, to a tile [positions][16].
-template <int R>
-__device__ inline void put_rows(float (*tile)[kSelCh], int first, int row, int ch, const float *v)
+__device__ inline int row_value(int row) { return (row & 1) << 1 | row >> 1; }
+
+// Sums over the 16 lanes of a row of four values: the lanes of the row's k-th four get that of value
+// four_value(k).  Mirrored lanes are added and two sums put into one register by halves, then by quarters.
+template <int BANKS>
+__device__ inline float banks_of(float a, float b)      // b in those fours of lanes, a in the others
 {
-    if constexpr (R == 2) {
-        if (!(row & 1)) tile[first + (row >> 1)][ch] = v[0];
-    } else {
-#pragma unroll
-        for (int q = 0; q < R / 4; ++q) tile[first + 4 * q + row_value<R>(row)][ch] = v[q];
-    }
+    return bits_float((uint32_t)__builtin_amdgcn_update_dpp((int)float_bits(a), (int)float_bits(b), 0xe4, 0xf, BANKS, false));
+}
+template <int CTRL>
+__device__ inline float plus_moved(float v)
+{
+#pragma clang fp contract(off)          // one addition of a moved lane, not a move and a fused product
+    return v + bits_float(moved<CTRL>(float_bits(v)));
+}
+__device__ inline float sum_four(float a, float b, float c, float d)
+{
+    const float x = banks_of<0xc>(plus_moved<0x140>(a), plus_moved<0x140>(b));
+    const float y = banks_of<0xc>(plus_moved<0x140>(c), plus_moved<0x140>(d));
+    float v = banks_of<0xa>(plus_moved<0x141>(x), plus_moved<0x141>(y));
+    v = plus_moved<0xb1>(v);
+    return plus_moved<0x4e>(v);
+}
+__device__ inline int four_value(int k) { return (k & 1) << 1 | k >> 1; }
+
+// The value is made here: its operands' registers end here and not where it is used.
+__device__ inline void made(float &v) { asm volatile("" : "+v"(v)); }
+
+// LDS that only one wave uses: its accesses are in order, the compiler has to leave them so.
+__device__ inline void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Sum over the 16 lanes of a row, in every lane.
-__device__ inline float sum_channels(float v) { return lanes_sum<16>(v); }
+// The wave's number in its workgroup, in a scalar register: what follows from it is the same for all lanes.
+__device__ inline int wave_number() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64); }
 
-// A thread's two elements of a tile: position `row`, channels 2 pair and the next.
-struct Mine {
-    int row, pair, have;                // have: channels that there are (0: an idle thread)
-    __device__ Mine(int TT, long long i0, long long I)
-    {
-        row = threadIdx.x / 8;
-        pair = threadIdx.x % 8;
-        const long long left = I - (i0 + 2 * pair);
-        have = row >= TT || left <= 0 ? 0 : left < 2 ? 1 : 2;
-    }
-};
-
-// One workgroup's place: 16 channels of a sequence, from position `first` on.
-struct Place {
-    long long b, i0, n, first, last;    // last: end of the chunk
-    __device__ Place(const SelArgs &a, long long b_, long long tile, int chunk)
-    {
-        b = b_;
-        i0 = tile * kSelCh;
-        n = length_of(a.lengths, b, a.T);
-        first = chunk * a.chunk;
-        last = min(a.T, first + a.chunk);
-    }
-    __device__ long long row(const SelArgs &a, long long s) const { return b * a.T + step_of(s, n, a.reverse); }
-};
-
-// Workgroups of neighbouring channels of a sequence share lines of its rows: those of an XCD
-// (every eighth) are given consecutive numbers.
+// Workgroups of neighbouring channels share lines of their rows: those of an XCD (every
+// eighth) are given consecutive numbers.
 __device__ inline long long spread(long long id, long long all)
 {
     const long long each = all / 8, rest = all - each * 8, x = id & 7;
     return (x < rest ? x * (each + 1) : rest * (each + 1) + (x - rest) * each) + (id >> 3);
 }
 
-// The raw inputs of a tile that a thread loads: its elements, and two values each of B and C.
-template <typename T, int SR>
-struct RawTile {
-    static constexpr int SP = 4 * SR, TT = sel_tile(SR), PAIRS = TT * SP / 2;
-    static constexpr int NB = (PAIRS + kSelThreads - 1) / kSelThreads;
-    Two<T> u, d, z, g, B[NB], C[NB];
-    bool live;
-    // g: dy, dense
-    __device__ void load(const SelArgs &a, const Place &p, const Mine &m, long long s0, const T *pu, const T *pd,
-                         const T *pz, const T *pg, const T *pB, const T *pC)
+// A lane's sequence and channels.
+struct Lane {
+    long long b, n, i;                  // sequence, its length, first channel
+    int have;                           // channels that there are (0: an idle lane, which stands on the first)
+    // row of position s, the padding's as well
+    __device__ long long row(const SelArgs &a, long long s) const { return b * a.T + step_of(s, n, a.reverse); }
+};
+
+template <int CL>
+__device__ inline Lane lane_of(const SelArgs &a, long long b, long long i)
+{
+    Lane l;
+    l.b = b < a.B ? b : a.B - 1;
+    l.n = length_of(a.lengths, l.b, a.T);
+    l.i = i < a.I ? i : 0;
+    l.have = b < a.B && i < a.I ? (int)min(a.I - i, (long long)CL) : 0;
+    return l;
+}
+
+// A lane's element of a tensor at position s + r, r < SPAN its own: a scalar address that s decides and the
+// lane's 32-bit offset from it (the host keeps rows short enough).
+template <typename T, int SPAN>
+struct Walk {
+    const char *base;                   // of the wave: position 0 of sequence b0 (in reverse the last one's row below)
+    long long step;                     // bytes from a position to the next
+    uint32_t off;
+    __device__ void init(const SelArgs &a, const T *x, long long pitch, long long b0, const Lane &l, int r, long long i)
     {
-        const long long s = s0 + m.row;
-        live = s < p.last && s < p.n;
-        const int have = live ? m.have : 0;
-        const long long r = live ? p.row(a, s) : 0, i = p.i0 + 2 * m.pair;
-        u.load(pu + r * a.pu + i, have);
-        d.load(pd + r * a.pd + i, have);
-        if (pz) z.load(pz + r * a.pz + i, have);
-        if (pg) g.load(pg + r * a.I + i, have);
-#pragma unroll
-        for (int q = 0; q < NB; ++q) {
-            const int e = threadIdx.x + q * kSelThreads, row = e / (SP / 2), k = e % (SP / 2) * 2;
-            const long long t = s0 + row;
-            const int n = row < TT && t < p.last && t < p.n ? (k + 1 < a.S ? 2 : k < a.S ? 1 : 0) : 0;
-            const long long rt = n ? p.row(a, t) : 0;
-            B[q].load(pB + rt * a.pB + k, n);
-            if (pC) C[q].load(pC + rt * a.pC + k, n);
-        }
+        const long long n0 = length_of(a.lengths, b0, a.T);
+        const long long row = (l.b - b0) * a.T + (a.reverse ? l.n - n0 + SPAN - 1 - r : r);
+        base = (const char *)x + (b0 * a.T + (a.reverse ? n0 - SPAN : 0)) * pitch * (long long)sizeof(T);
+        step = (a.reverse ? -pitch : pitch) * (long long)sizeof(T);
+        off = (uint32_t)((row * pitch + i) * (long long)sizeof(T));
+    }
+    __device__ char *at(long long s) const { return (char *)base + s * step; }
+    // whole: there is no other case for any lane
+    template <int N> __device__ void load(Few<T, N> &v, long long s, bool whole, int have) const
+    {
+        const char *p = at(s);
+        if (whole) v.set(*(const typename Few<T, N>::V *)(p + off));
+        else v.load((const T *)(p + off), have);
     }
 };
 
-// d and d u of an element.
+// SR states from `row` SR on of a channel in an array [..][S]; have: of them that there are.
+template <int SR>
+__device__ inline int states_have(const SelArgs &a, int row, bool lane)
+{
+    const int left = a.S - row * SR;
+    return !lane || left <= 0 ? 0 : left < SR ? left : SR;
+}
+template <int SR>
+__device__ inline void load_states(const float *p, int have, float *v)
+{
+    if constexpr (SR >= 4) {
+#pragma unroll
+        for (int j = 0; j < SR; j += 4) Piece<float>::unpack(load_piece<float>(p + j, have - j < 4 ? have - j : 4), v + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < SR; ++j) v[j] = j < have ? p[j] : 0.0f;
+    }
+}
+template <int SR>
+__device__ inline void store_states(float *p, int have, const float *v)
+{
+    if constexpr (SR >= 4) {
+#pragma unroll
+        for (int j = 0; j < SR; j += 4)
+            if (have - j > 0) store_piece<float>(p + j, have - j < 4 ? have - j : 4, v + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < SR; ++j)
+            if (j < have) p[j] = v[j];
+    }
+}
+
+// A lane's states of a row of B or C in LDS, in one access for each four.
+template <int SR>
+__device__ inline void row_states(const float *p, float *v)
+{
+    if constexpr (SR >= 4) {
+#pragma unroll
+        for (int j = 0; j < SR; j += 4) {
+            const float4 w = *(const float4 *)(p + j);
+            v[j] = w.x;
+            v[j + 1] = w.y;
+            v[j + 2] = w.z;
+            v[j + 3] = w.w;
+        }
+    } else if constexpr (SR == 2) {
+        const float2 w = *(const float2 *)p;
+        v[0] = w.x;
+        v[1] = w.y;
+    } else {
+        v[0] = *p;
+    }
+}
+
 __device__ inline float step_size(const SelArgs &a, float raw, float bias, bool live)
 {
     const float v = raw + bias;
     return live ? (a.softplus ? softplus_of(v) : v) : 0.0f;
 }
 
-template <int SR, bool BACK>
-struct alignas(16) SelShared {
-    static constexpr int SP = 4 * SR, TT = sel_tile(SR), TB = BACK ? TT : 1;
-    float2 du[TT][kSelCh];              // d, d u
-    float B[TT][SP], C[TT][SP];
-    float P[kSelW][SR][64], H[kSelW][SR][64], X[BACK ? kSelW : 1][SR][64];
-    float carry[2][SR][64];             // the state (BACK: what the gradient passes on) between tiles, by turns
-    float y[TT][kSelCh];                // BACK: p without D u
-    float dp[TB][kSelCh], q[TB][kSelCh], w[TB][kSelCh];
-    float dB[TB][SP], dC[TB][SP];
+// Two values each of rows of B or C (4 SR of them, the last ones 0) of R positions of NB sequences,
+// by the lanes of a wave, ROWS positions a pass.
+template <typename T, int SR, int R, int NB>
+struct StateRows {
+    static constexpr int SP = 4 * SR, PP = NB * SP / 2;
+    static constexpr int ROWS = 64 / PP < R ? 64 / PP : R, Q = R / ROWS;
+    static_assert(PP <= 64 && Q * ROWS == R, "a pass takes whole rows");
+    Walk<T, ROWS> walk;
+    int r, to, want;                    // the lane's position, place in a row of LDS, values that there are
+    long long n;
+    Few<T, 2> raw[Q];
+    __device__ void init(const SelArgs &a, const T *p, long long pitch, long long b0, int lane)
+    {
+        r = min(lane / PP, ROWS - 1);
+        const int at = lane % PP, seq = at / (SP / 2), k = at % (SP / 2) * 2;
+        const Lane l = lane_of<1>(a, b0 + seq, 0);
+        n = b0 + seq < a.B ? l.n : 0;
+        to = seq * SP + k;
+        want = k + 1 < a.S ? 2 : k < a.S ? 1 : 0;
+        walk.init(a, p, pitch, b0, l, r, want ? k : 0);
+    }
+    __device__ void load(long long s0, long long last, bool whole)
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const long long s = s0 + q * ROWS;
+            walk.load(raw[q], s, whole, s + r < last && s + r < n ? want : 0);
+        }
+    }
+    __device__ void put(float (*rows)[NB * SP]) const
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            *(float2 *)&rows[q * ROWS + r][to] = make_float2(want > 0 ? raw[q].get(0) : 0.0f, want > 1 ? raw[q].get(1) : 0.0f);
+    }
 };
 
-// The part of a lane in the decays: A log2(e) of its channel's states.
-template <int SR>
-__device__ inline void lane_A(const SelArgs &a, const Place &p, const float *A, int row, int ch, float scale, float *out)
+// Positions that all sequences of a wave have, and whether its lanes load whole pieces there.
+template <int CL, int NB>
+__device__ inline long long whole_until(const SelArgs &a, long long b0, long long last)
 {
-    const long long i = p.i0 + ch;
+    if ((CL > 1 && a.I % CL) || a.S % 2) return 0;
+    long long n = last;
 #pragma unroll
-    for (int j = 0; j < SR; ++j) {
-        const int k = row * SR + j;
-        out[j] = i < a.I && k < a.S ? A[i * a.S + k] * scale : 0.0f;
-    }
-}
-// Element (b, i, row SR + j) of a state [..][I][S]; false where there is none.
-template <int SR>
-__device__ inline bool state_at(const SelArgs &a, const Place &p, long long outer, int row, int ch, int j, long long &at)
-{
-    const long long i = p.i0 + ch;
-    const int k = row * SR + j;
-    at = (outer * a.I + i) * a.S + k;
-    return i < a.I && k < a.S;
+    for (int q = 0; q < NB; ++q)
+        if (b0 + q < a.B) n = min(n, length_of(a.lengths, b0 + q, a.T));
+    return n;
 }
 
-// FOLD: the state after each chunk but the last, for workgroups that have a chunk:
-// fold [chunk][b][i][k] (P, H), chunk 0 from h0.
-template <typename T, int SR, bool FOLD>
-__global__ void __launch_bounds__(kSelThreads, SR < 16 ? 4 : 2)
-k_sel_fwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D,
-          const T *z, const float *dbias, const float *h0, T *y, float *hT, float *saved, float2 *fold)
+// What a wave stages: d and d u (the backward fold: d and dp) of its elements, rows of B and C.
+template <int SR, int CL, int NB>
+struct alignas(16) ForwardShared {
+    float du[kSelStage][16][2 * CL];
+    float B[kSelStage][NB * 4 * SR], C[kSelStage][NB * 4 * SR];
+};
+
+// Where a wave of the forward or a fold is: NB sequences share it where 16 / NB lanes have all
+// their channels.
+template <int CL, int NB>
+__device__ inline void wave_place(const SelArgs &a, long long id, int lane, Lane &l, long long &b0, int &chunk)
 {
-    constexpr int R = sel_run(SR), TT = sel_tile(SR), SP = 4 * SR;
-    typedef RawTile<T, SR> Raw;
-    __shared__ SelShared<SR, false> sh;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, row = lane >> 4, ch = lane & 15;
-    const long long id = spread(blockIdx.x, gridDim.x);
-    const int nchunks = FOLD ? a.chunks - 1 : a.chunks;
-    const long long bt = id / a.tiles, b = bt / nchunks;
-    const int chunk = (int)(bt - b * nchunks);
-    const Place p(a, b, id - bt * a.tiles, chunk);
-    const Mine m(TT, p.i0, a.I);
-    float A2[SR];
-    lane_A<SR>(a, p, A, row, ch, kLog2e, A2);
-    if (wave == 0) {
-#pragma unroll
-        for (int j = 0; j < SR; ++j) {
-            long long at;
-            float h = 0.0f;
-            if (state_at<SR>(a, p, b, row, ch, j, at)) {
-                if (a.chunks == 1) {
-                    h = h0 ? h0[at] : 0.0f;
-                } else if (FOLD) {
-                    h = chunk == 0 && h0 ? h0[at] : 0.0f;
-                    // h0 may be where the state after goes
-                    if (chunk == 0) fold[(long long)(a.chunks - 1) * a.B * a.I * a.S + at] = make_float2(0.0f, h);
-                } else if (chunk == 0) {
-                    h = fold[(long long)(a.chunks - 1) * a.B * a.I * a.S + at].y;
-                } else {
-                    h = fold[at].y;
-                    for (int c = 1; c < chunk; ++c) {
-                        const float2 f = fold[(long long)c * a.B * a.I * a.S + at];
-                        h = fmaf(f.x, h, f.y);
-                    }
-                }
-            }
-            sh.carry[0][j][lane] = h;
-        }
+    const long long g = id % a.groups;
+    chunk = (int)(id / a.groups);
+    const int p = lane & 15;
+    if (NB == 1) {
+        b0 = g / a.tiles;
+        l = lane_of<CL>(a, b0, ((g - b0 * a.tiles) * 16 + p) * CL);
+    } else {
+        b0 = g * NB;
+        l = lane_of<CL>(a, b0 + p / (16 / NB), p % (16 / NB) * CL);
     }
-    float bias[2], Dv[2];
+}
+
+template <typename T, int SR, int CL, int NB>
+__global__ void __launch_bounds__(256)
+k_sel_fwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D,
+          const T *z, const float *dbias, const float *h0, T *y, float *hT, float *saved, const float *start)
+{
+    constexpr int R = kSelStage, K = R / 4, SP = 4 * SR;
+    __shared__ ForwardShared<SR, CL, NB> shared[4];
+    const int lane = threadIdx.x & 63, row = lane >> 4, p = lane & 15, rv = row_value(row);
+    const int wave = wave_number();
+    const long long id = spread(blockIdx.x, gridDim.x) * 4 + wave;
+    if (id >= a.groups * a.chunks) return;
+    ForwardShared<SR, CL, NB> &sh = shared[wave];
+    Lane l;
+    long long b0;
+    int chunk;
+    wave_place<CL, NB>(a, id, lane, l, b0, chunk);
+    const long long first = chunk * a.chunk, last = min(a.T, first + a.chunk);
+    const int seq = NB == 1 ? 0 : p / (16 / NB);
+    float A2[CL][SR], h[CL][SR], bias[CL], Dv[CL];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const long long i = p.i0 + 2 * m.pair + e;
-        bias[e] = dbias && e < m.have ? dbias[i] : 0.0f;
-        Dv[e] = D && e < m.have ? D[i] : 0.0f;
+    for (int c = 0; c < CL; ++c) {
+        const int have = states_have<SR>(a, row, c < l.have);
+        const long long at = (l.b * a.I + l.i + c) * a.S + row * SR;
+        load_states<SR>(A + (l.i + c) * a.S + row * SR, have, A2[c]);
+        const float *from = a.chunks > 1 ? start + chunk * a.B * a.I * a.S : h0;
+        load_states<SR>(from + at, from ? have : 0, h[c]);
+#pragma unroll
+        for (int j = 0; j < SR; ++j) A2[c][j] *= kLog2e;
+        bias[c] = dbias && c < l.have ? dbias[l.i + c] : 0.0f;
+        Dv[c] = D && c < l.have ? D[l.i + c] : 0.0f;
     }
-    float Pall[SR];
+    Walk<T, 4> wu, wd, wz, wy;
+    wu.init(a, u, a.pu, b0, l, rv, l.i);
+    wd.init(a, delta, a.pd, b0, l, rv, l.i);
+    if (z) wz.init(a, z, a.pz, b0, l, rv, l.i);
+    wy.init(a, y, a.I, b0, l, rv, l.i);
+    StateRows<T, SR, R, NB> rB, rC;
+    rB.init(a, Bm, a.pB, b0, lane);
+    rC.init(a, Cm, a.pC, b0, lane);
+    const long long whole = whole_until<CL, NB>(a, b0, last);
+    Few<T, CL> ru[K], rd[K], rz[K];
+    const auto fetch_as = [&](long long s0, auto all) {
+        constexpr bool W = decltype(all)::value;
 #pragma unroll
-    for (int j = 0; j < SR; ++j) Pall[j] = 1.0f;
-    Raw raw;
-    raw.load(a, p, m, p.first, u, delta, FOLD ? nullptr : z, nullptr, Bm, FOLD ? nullptr : Cm);
-    int turn = 0;
-    for (long long s0 = p.first; s0 < p.last; s0 += TT, turn ^= 1) {
-        const float u0 = raw.u.lo(), u1 = raw.u.hi();
-        const Two<T> zz = raw.z;
-        const bool live = raw.live;
-        if (m.row < TT) {
-            const float d0 = step_size(a, raw.d.lo(), bias[0], live), d1 = step_size(a, raw.d.hi(), bias[1], live);
-            *(float4 *)&sh.du[m.row][2 * m.pair] = make_float4(d0, d0 * u0, d1, d1 * u1);
+        for (int k = 0; k < K; ++k) {
+            const long long s = s0 + 4 * k;
+            const int have = !W && s + rv < last && s + rv < l.n ? l.have : 0;
+            wu.load(ru[k], s, W, have);
+            wd.load(rd[k], s, W, have);
+            if (z) wz.load(rz[k], s, W, have);
         }
+        rB.load(s0, last, W);
+        rC.load(s0, last, W);
+    };
+    const auto fetch = [&](long long s0) {
+        if (s0 + R <= whole) fetch_as(s0, std::true_type());
+        else fetch_as(s0, std::false_type());
+    };
+    fetch(first);
+    for (long long s0 = first; s0 < last; s0 += R) {
+        float uv[K][CL], zv[K][CL];
 #pragma unroll
-        for (int q = 0; q < Raw::NB; ++q) {
-            const int e = threadIdx.x + q * kSelThreads, r = e / (SP / 2), k = e % (SP / 2) * 2;
-            if (r < TT) {
-                *(float2 *)&sh.B[r][k] = make_float2(raw.B[q].lo(), raw.B[q].hi());
-                if (!FOLD) *(float2 *)&sh.C[r][k] = make_float2(raw.C[q].lo(), raw.C[q].hi());
+        for (int k = 0; k < K; ++k) {
+            const bool live = s0 + 4 * k + rv < l.n;
+            float v[2 * CL];
+#pragma unroll
+            for (int c = 0; c < CL; ++c) {
+                uv[k][c] = ru[k].get(c);
+                zv[k][c] = z ? rz[k].get(c) : 0.0f;
+                v[2 * c] = step_size(a, rd[k].get(c), bias[c], live);
+                v[2 * c + 1] = v[2 * c] * uv[k][c];
             }
+            if constexpr (CL == 2) *(float4 *)&sh.du[4 * k + rv][p][0] = make_float4(v[0], v[1], v[2], v[3]);
+            else *(float2 *)&sh.du[4 * k + rv][p][0] = make_float2(v[0], v[1]);
         }
-        __syncthreads();
-        if (s0 + TT < p.last)
-            raw.load(a, p, m, s0 + TT, u, delta, FOLD ? nullptr : z, nullptr, Bm, FOLD ? nullptr : Cm);
-        const int first = wave * R;
-        float dec[R][SR], h[SR], sum = 0.0f;
+        rB.put(sh.B);
+        rC.put(sh.C);
+        wave_sync();
+        if (s0 + R < last) fetch(s0 + R);
+        if (saved && s0 % kSelKeep == 0)
 #pragma unroll
-        for (int j = 0; j < SR; ++j) h[j] = 0.0f;
+            for (int c = 0; c < CL; ++c)
+                store_states<SR>(saved + ((l.b * a.kept + s0 / kSelKeep) * a.I + l.i + c) * a.S + row * SR,
+                                 states_have<SR>(a, row, c < l.have), h[c]);
+        float yp[CL][R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float2 v = sh.du[first + r][ch];
-            sum += v.x;
+            float v[2 * CL], Bv[SR], Cv[SR];
 #pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                dec[r][j] = __builtin_amdgcn_exp2f(v.x * A2[j]);
-                h[j] = fmaf(dec[r][j], h[j], v.y * sh.B[first + r][row * SR + j]);
-            }
-        }
+            for (int e = 0; e < 2 * CL; ++e) v[e] = sh.du[r][p][e];
+            row_states<SR>(&sh.B[r][seq * SP + row * SR], Bv);
+            row_states<SR>(&sh.C[r][seq * SP + row * SR], Cv);
 #pragma unroll
-        for (int j = 0; j < SR; ++j) {
-            sh.P[wave][j][lane] = __builtin_amdgcn_exp2f(sum * A2[j]);
-            sh.H[wave][j][lane] = h[j];
-        }
-        __syncthreads();
-        const int before = FOLD ? kSelW : wave;
-        if (!FOLD || wave == 0) {
-#pragma unroll
-            for (int j = 0; j < SR; ++j) h[j] = sh.carry[turn][j][lane];
-            for (int w = 0; w < before; ++w)
+            for (int c = 0; c < CL; ++c) {
+                yp[c][r] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < SR; ++j) {
-                    h[j] = fmaf(sh.P[w][j][lane], h[j], sh.H[w][j][lane]);
-                    if (FOLD) Pall[j] *= sh.P[w][j][lane];
+                    const float dec = __builtin_amdgcn_exp2f(v[2 * c] * A2[c][j]);
+                    h[c][j] = fmaf(dec, h[c][j], v[2 * c + 1] * Bv[j]);
+                    yp[c][r] = fmaf(Cv[j], h[c][j], yp[c][r]);
                 }
-        }
-        if (FOLD) {
-            if (wave == 0)
-#pragma unroll
-                for (int j = 0; j < SR; ++j) sh.carry[turn ^ 1][j][lane] = h[j];
-            continue;       // the next tile's first barrier comes before anything that was read is overwritten but du and B
-        }
-        if (saved && wave == 0)
-#pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                long long at;
-                if (state_at<SR>(a, p, b * a.kept + s0 / TT, row, ch, j, at)) saved[at] = h[j];
-            }
-        float yp[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float v = sh.du[first + r][ch].y;
-            yp[r] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                h[j] = fmaf(dec[r][j], h[j], v * sh.B[first + r][row * SR + j]);
-                yp[r] = fmaf(sh.C[first + r][row * SR + j], h[j], yp[r]);
             }
         }
-        sum_rows_of_lanes<R>(yp);
-        put_rows<R>(sh.y, first, row, ch, yp);
-        if (wave == kSelW - 1)
 #pragma unroll
-            for (int j = 0; j < SR; ++j) sh.carry[turn ^ 1][j][lane] = h[j];
-        __syncthreads();
-        const long long s = s0 + m.row;
-        if (m.have && s < p.last) {
-            const float2 v = *(const float2 *)&sh.y[m.row][2 * m.pair];
-            float y0 = fmaf(Dv[0], u0, v.x), y1 = fmaf(Dv[1], u1, v.y);
-            if (z) {
-                y0 *= silu_of(zz.lo());
-                y1 *= silu_of(zz.hi());
+        for (int c = 0; c < CL; ++c) sum_states<K>(yp[c]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const long long s = s0 + 4 * k + rv;
+            float v[CL];
+#pragma unroll
+            for (int c = 0; c < CL; ++c) {
+                v[c] = fmaf(Dv[c], uv[k][c], yp[c][k]);
+                if (z) v[c] *= zv[k][c] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(zv[k][c] * -kLog2e));
+                v[c] = s < l.n ? v[c] : 0.0f;
             }
-            Two<T>::store(y + p.row(a, s) * a.I + p.i0 + 2 * m.pair, m.have, live ? y0 : 0.0f, live ? y1 : 0.0f);
+            if (s0 + R <= whole) {
+                if (l.have) Few<T, CL>::store((T *)(wy.at(s0 + 4 * k) + wy.off), CL, v);
+            } else if (s < last) {
+                Few<T, CL>::store(y + l.row(a, s) * a.I + l.i, l.have, v);
+            }
         }
+        wave_sync();
     }
-    if (wave == 0 && (FOLD || (hT && chunk == a.chunks - 1)))
+    if (hT && chunk == a.chunks - 1)
+#pragma unroll
+        for (int c = 0; c < CL; ++c)
+            store_states<SR>(hT + (l.b * a.I + l.i + c) * a.S + row * SR, states_have<SR>(a, row, c < l.have), h[c]);
+}
+
+// Folds of chunks: sums of d [chunk][b][i], and what a chunk makes of nothing, its last state or
+// (BACK) the gradient that it passes on: H [chunk][b][i][k].
+template <typename T, int SR, int CL, int NB, bool BACK>
+__global__ void __launch_bounds__(256)
+k_sel_fold(SelArgs a, const T *u, const T *delta, const float *A, const T *rows, long long pitch, const T *z,
+           const T *dy, const float *dbias, float *H, float *sums)
+{
+    constexpr int R = kSelStage, K = R / 4, SP = 4 * SR;
+    __shared__ ForwardShared<SR, CL, NB> shared[4];
+    const int lane = threadIdx.x & 63, row = lane >> 4, p = lane & 15, rv = row_value(row);
+    const int wave = wave_number();
+    const long long id = spread(blockIdx.x, gridDim.x) * 4 + wave;
+    if (id >= a.groups * (a.chunks - 1)) return;
+    ForwardShared<SR, CL, NB> &sh = shared[wave];
+    Lane l;
+    long long b0;
+    int chunk;
+    wave_place<CL, NB>(a, id, lane, l, b0, chunk);
+    chunk += BACK ? 1 : 0;
+    const long long first = chunk * a.chunk, last = min(a.T, first + a.chunk);
+    const int seq = NB == 1 ? 0 : p / (16 / NB);
+    float A2[CL][SR], h[CL][SR], bias[CL], sum[CL];
+#pragma unroll
+    for (int c = 0; c < CL; ++c) {
+        load_states<SR>(A + (l.i + c) * a.S + row * SR, states_have<SR>(a, row, c < l.have), A2[c]);
 #pragma unroll
         for (int j = 0; j < SR; ++j) {
-            long long at;
-            if (!state_at<SR>(a, p, b, row, ch, j, at)) continue;
-            const float v = sh.carry[turn][j][lane];
-            if (FOLD) fold[(long long)chunk * a.B * a.I * a.S + at] = make_float2(Pall[j], v);
-            else hT[at] = v;
+            A2[c][j] *= kLog2e;
+            h[c][j] = 0.0f;
         }
+        bias[c] = dbias && c < l.have ? dbias[l.i + c] : 0.0f;
+        sum[c] = 0.0f;
+    }
+    Walk<T, 4> wu, wd, wz;              // BACK: dy in the place of u
+    wu.init(a, BACK ? dy : u, BACK ? a.I : a.pu, b0, l, rv, l.i);
+    wd.init(a, delta, a.pd, b0, l, rv, l.i);
+    if (BACK && z) wz.init(a, z, a.pz, b0, l, rv, l.i);
+    StateRows<T, SR, R, NB> rB;
+    rB.init(a, rows, pitch, b0, lane);
+    const long long whole = whole_until<CL, NB>(a, b0, last);
+    Few<T, CL> ru[K], rd[K], rz[K];
+    const auto fetch_as = [&](long long s0, auto all) {
+        constexpr bool W = decltype(all)::value;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const long long s = s0 + 4 * k;
+            const int have = !W && s + rv < last && s + rv < l.n ? l.have : 0;
+            wu.load(ru[k], s, W, have);
+            wd.load(rd[k], s, W, have);
+            if (BACK && z) wz.load(rz[k], s, W, have);
+        }
+        rB.load(s0, last, W);
+    };
+    const auto fetch = [&](long long s0) {
+        if (s0 + R <= whole) fetch_as(s0, std::true_type());
+        else fetch_as(s0, std::false_type());
+    };
+    const long long stages = (last - first + R - 1) / R;
+    fetch(BACK ? first + (stages - 1) * R : first);
+    for (long long st = 0; st < stages; ++st) {
+        const long long s0 = first + (BACK ? stages - 1 - st : st) * R;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const bool live = s0 + 4 * k + rv < min(l.n, last);
+            float v[2 * CL];
+#pragma unroll
+            for (int c = 0; c < CL; ++c) {
+                v[2 * c] = step_size(a, rd[k].get(c), bias[c], live);
+                const float x = ru[k].get(c);
+                v[2 * c + 1] = BACK ? (z ? x * silu_of(rz[k].get(c)) : x) : v[2 * c] * x;
+            }
+            if constexpr (CL == 2) *(float4 *)&sh.du[4 * k + rv][p][0] = make_float4(v[0], v[1], v[2], v[3]);
+            else *(float2 *)&sh.du[4 * k + rv][p][0] = make_float2(v[0], v[1]);
+        }
+        rB.put(sh.B);
+        wave_sync();
+        if (st + 1 < stages) fetch(BACK ? s0 - R : s0 + R);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const int r = BACK ? R - 1 - q : q;
+            float v[2 * CL], Bv[SR];
+#pragma unroll
+            for (int e = 0; e < 2 * CL; ++e) v[e] = sh.du[r][p][e];
+            row_states<SR>(&sh.B[r][seq * SP + row * SR], Bv);
+#pragma unroll
+            for (int c = 0; c < CL; ++c) {
+                sum[c] += v[2 * c];
+#pragma unroll
+                for (int j = 0; j < SR; ++j) {
+                    const float dec = __builtin_amdgcn_exp2f(v[2 * c] * A2[c][j]);
+                    if (BACK) h[c][j] = dec * fmaf(v[2 * c + 1], Bv[j], h[c][j]);
+                    else h[c][j] = fmaf(dec, h[c][j], v[2 * c + 1] * Bv[j]);
+                }
+            }
+        }
+        wave_sync();
+    }
+    const long long cols = a.B * a.I;
+#pragma unroll
+    for (int c = 0; c < CL; ++c) {
+        const long long at = chunk * cols + l.b * a.I + l.i + c;
+        store_states<SR>(H + at * a.S + row * SR, states_have<SR>(a, row, c < l.have), h[c]);
+        if (row == 0 && c < l.have) sums[at] = sum[c];
+    }
+}
+
+// The state before each chunk (BACK: the gradient behind each), from h0 (dhT) on, in the place of H.
+template <bool BACK>
+__global__ void __launch_bounds__(256)
+k_sel_chain(long long cols, long long I, int S, int chunks, const float *A, const float *from, float *H, const float *sums)
+{
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, col = at / S, states = cols * S;
+    if (at >= states) return;
+    const float A2 = A[col % I * S + (at - col * S)] * kLog2e;
+    float h = from ? from[at] : 0.0f;
+    for (int n = 0; n < chunks; n += 8) {
+        float x[8], s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = BACK ? chunks - 1 - n - e : n + e;
+            const bool has = n + e + 1 < chunks;        // the last one passes nothing on
+            x[e] = has ? H[c * states + at] : 0.0f;
+            s[e] = has ? sums[c * cols + col] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (n + e >= chunks) break;
+            H[(BACK ? chunks - 1 - n - e : n + e) * states + at] = h;
+            h = fmaf(__builtin_amdgcn_exp2f(s[e] * A2), h, x[e]);
+        }
+    }
 }
 
 // A single step: L lanes of 4 states a channel.
@@ -454,316 +665,241 @@ k_sel_step(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, c
     }
 }
 
-// FOLD: what the gradient passes on below each chunk but the first, for workgroups that have
-// a chunk: fold [chunk][b][i][k] (P, X), the last one's from dhT.
-// Else: parts of the sums over channels (dBp, dCp [tile][b][t][S], where there are several tiles) and of those
-// over positions (dAp [job][I][S], dDp [job][I][2]).
-template <typename T, int SR, bool FOLD>
-__global__ void __launch_bounds__(kSelThreads, 2)
+// Positions of a run of the backward, whose decays and states a lane has in registers.
+__host__ __device__ constexpr int sel_run(int SR) { return SR <= 4 ? 8 : 4; }
+
+template <int SR>
+struct alignas(16) BackShared {
+    static constexpr int SP = 4 * SR, R = sel_run(SR), NR = kSelKeep / R;
+    float2 du[kSelKeep][16];            // d, d u
+    float2 own[kSelKeep][16];           // u, the derivative of d: what its own lane takes back
+    float dp[kSelKeep][16], slope[kSelKeep][16];        // slope: dy silu'(z)
+    float B[kSelKeep][SP], C[kSelKeep][SP];
+    float start[NR][SR][64];            // the state before each run
+    float out[2][2][R][SP];             // a run's dB and dC, by turns
+};
+
+// Walks chunks from their ends, kSelKeep positions at a time: the states before the runs from the kept one,
+// then run by run, from the last on, the states in it and back.  WIDE: the waves of a workgroup have neighbouring channels of
+// the same chunk and add up their dB and dC; else each has the only 16 channels of a sequence of its own.
+// dBp, dCp [group of channels][b][t][S] (one group: dB and dC themselves); dAp [job][I][S], dDp [job][I][2].
+template <typename T, int SR, bool WIDE>
+__global__ void __launch_bounds__(256, 2)
 k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D, const T *z,
-          const float *dbias, const float *saved, const T *dy, const float *dhT, T *du, T *ddelta, T *dz, float *dh0,
-          float *dBp, float *dCp, T *dB, T *dC, float *dAp, float *dDp, float2 *fold)
+          const float *dbias, const float *saved, const T *dy, const float *dhT, const float *behind, T *du, T *ddelta,
+          T *dz, float *dh0, float *dBp, float *dCp, T *dB, T *dC, float *dAp, float *dDp)
 {
-    constexpr int R = sel_run(SR), TT = sel_tile(SR), SP = 4 * SR;
-    typedef RawTile<T, SR> Raw;
-    __shared__ SelShared<SR, !FOLD> sh;
-    __shared__ float foldX[FOLD ? kSelW : 1][SR][64];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, row = lane >> 4, ch = lane & 15;
-    const long long id = spread(blockIdx.x, gridDim.x);
-    const long long job0 = id / a.tiles, tile = id - job0 * a.tiles;
-    const int nchunks = FOLD ? a.chunks - 1 : a.chunks;
-    const long long states = a.B * a.I * a.S;
-    float Av[SR], dA[SR], dDv[2] = {0.0f, 0.0f}, dbv[2] = {0.0f, 0.0f};
+    constexpr int R = sel_run(SR), NR = kSelKeep / R, K = R / 4, SP = 4 * SR;
+    extern __shared__ float4 dyn[];
+    BackShared<SR> *shared = (BackShared<SR> *)dyn;
+    const int wave = wave_number(), waves = blockDim.x / 64;
+    const int lane = threadIdx.x & 63, row = lane >> 4, ch = lane & 15, rv = row_value(row), fv = four_value(ch >> 2);
+    BackShared<SR> &sh = shared[wave];
+    const long long id = spread(blockIdx.x, gridDim.x), wide = (a.tiles + waves - 1) / waves;
+    const long long group = WIDE ? id % wide : 0, job0 = WIDE ? id / wide : id * waves + wave;
+    const long long i = (WIDE ? group * waves + wave : 0) * 16 + ch;
+    const bool has = i < a.I;
+    const long long ic = has ? i : 0;
+    const int have = states_have<SR>(a, row, has);
+    float A2[SR], dA[SR], dDv = 0.0f, dbv = 0.0f;
+    load_states<SR>(A + ic * a.S + row * SR, have, A2);
 #pragma unroll
-    for (int j = 0; j < SR; ++j) dA[j] = 0.0f;
-    for (long long job = job0; job < a.B * nchunks; job += a.jobs) {
-        const long long b = job / nchunks;
-        const int chunk = (int)(job - b * nchunks) + (FOLD ? 1 : 0);
-        const Place p(a, b, tile, chunk);
-        const Mine m(TT, p.i0, a.I);
-        lane_A<SR>(a, p, A, row, ch, 1.0f, Av);
-        __syncthreads();                // the job before is done with LDS
-        if (wave == 0) {
+    for (int j = 0; j < SR; ++j) {
+        A2[j] *= kLog2e;
+        dA[j] = 0.0f;
+    }
+    const float bias = dbias && has ? dbias[i] : 0.0f, Dv = D && has ? D[i] : 0.0f;
+    if (!WIDE && job0 >= a.jobs) return;
+    for (long long job = job0; job < a.B * a.chunks; job += a.jobs) {
+        const long long b = job / a.chunks;
+        const int chunk = (int)(job - b * a.chunks);
+        const long long first = chunk * a.chunk, last = min(a.T, first + a.chunk);
+        Lane l = lane_of<1>(a, b, ic);
+        l.have = has;
+        const long long at0 = (b * a.I + ic) * a.S + row * SR;
+        float x[SR];
+        const float *from = a.chunks > 1 ? behind + chunk * a.B * a.I * a.S : dhT;
+        load_states<SR>(from + at0, from ? have : 0, x);
+        Walk<T, 4> wu, wd, wz, wg;
+        wu.init(a, u, a.pu, b, l, rv, ic);
+        wd.init(a, delta, a.pd, b, l, rv, ic);
+        if (z) wz.init(a, z, a.pz, b, l, rv, ic);
+        wg.init(a, dy, a.I, b, l, rv, ic);
+        StateRows<T, SR, kSelKeep, 1> rB, rC;
+        rB.init(a, Bm, a.pB, b, lane);
+        rC.init(a, Cm, a.pC, b, lane);
+        const long long whole = whole_until<1, 1>(a, b, last);
+        Few<T, 1> ru[4], rd[4], rz[4], rg[4];
+        float hs[SR];
+        const auto fetch_as = [&](long long s0, auto all) {
+            constexpr bool W = decltype(all)::value;
 #pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                long long at;
-                float x = 0.0f;
-                if (state_at<SR>(a, p, b, row, ch, j, at)) {
-                    if (a.chunks == 1) {
-                        x = dhT ? dhT[at] : 0.0f;
-                    } else if (FOLD) {
-                        x = chunk == a.chunks - 1 && dhT ? dhT[at] : 0.0f;
-                        // dhT may be where dh0 goes
-                        if (chunk == a.chunks - 1) fold[at] = make_float2(0.0f, x);
-                    } else if (chunk == a.chunks - 1) {
-                        x = fold[at].y;
-                    } else {
-                        x = fold[(a.chunks - 1) * states + at].y;
-                        for (int c = a.chunks - 2; c > chunk; --c) {
-                            const float2 f = fold[c * states + at];
-                            x = fmaf(f.x, x, f.y);
-                        }
-                    }
-                }
-                sh.carry[0][j][lane] = x;
+            for (int k = 0; k < 4; ++k) {
+                const long long s = s0 + 4 * k;
+                const int have = !W && has && s + rv < last && s + rv < l.n;
+                wu.load(ru[k], s, W, have);
+                wd.load(rd[k], s, W, have);
+                wg.load(rg[k], s, W, have);
+                if (z) wz.load(rz[k], s, W, have);
             }
-        }
-        float bias[2], Dv[2], Pall[SR];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const long long i = p.i0 + 2 * m.pair + e;
-            bias[e] = dbias && e < m.have ? dbias[i] : 0.0f;
-            Dv[e] = D && e < m.have ? D[i] : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < SR; ++j) Pall[j] = 1.0f;
+            rB.load(s0, last, W);
+            rC.load(s0, last, W);
+        };
+        const auto fetch = [&](long long s0) {
+            if (s0 + kSelKeep <= whole) fetch_as(s0, std::true_type());
+            else fetch_as(s0, std::false_type());
+            load_states<SR>(saved + ((b * a.kept + s0 / kSelKeep) * a.I + ic) * a.S + row * SR, have, hs);
+        };
+        const long long blocks = (last - first + kSelKeep - 1) / kSelKeep;
+        fetch(first + (blocks - 1) * kSelKeep);
         int turn = 0;
-        const long long tiles = (p.last - p.first + TT - 1) / TT;
-        Raw raw;
-        raw.load(a, p, m, p.first + (tiles - 1) * TT, u, delta, z, dy, Bm, Cm);
-        for (long long tl = tiles - 1; tl >= 0; --tl, turn ^= 1) {
-            const long long s0 = p.first + tl * TT;
-            const float u0 = raw.u.lo(), u1 = raw.u.hi(), g0 = raw.g.lo(), g1 = raw.g.hi();
-            const float z0 = raw.z.lo(), z1 = raw.z.hi(), r0 = raw.d.lo() + bias[0], r1 = raw.d.hi() + bias[1];
-            const bool live = raw.live;
-            float slope[2] = {0.0f, 0.0f}, dp0 = g0, dp1 = g1, d0 = 0.0f, d1 = 0.0f;
-            if (z) {
-                float s;
-                slope[0] = silu_slope(z0, s);
-                dp0 = g0 * s;
-                slope[1] = silu_slope(z1, s);
-                dp1 = g1 * s;
-            }
-            if (m.row < TT) {
-                d0 = step_size(a, raw.d.lo(), bias[0], live);
-                d1 = step_size(a, raw.d.hi(), bias[1], live);
-                dp0 = live ? dp0 : 0.0f;
-                dp1 = live ? dp1 : 0.0f;
-                *(float4 *)&sh.du[m.row][2 * m.pair] = make_float4(d0, d0 * u0, d1, d1 * u1);
-                if constexpr (!FOLD) *(float2 *)&sh.dp[m.row][2 * m.pair] = make_float2(dp0, dp1);
-                else *(float2 *)&sh.y[m.row][2 * m.pair] = make_float2(dp0, dp1);
-            }
-            const float (*dpt)[kSelCh];
-            if constexpr (FOLD) dpt = sh.y; else dpt = sh.dp;
+        for (long long bl = blocks - 1; bl >= 0; --bl) {
+            const long long s0 = first + bl * kSelKeep;
 #pragma unroll
-            for (int q = 0; q < Raw::NB; ++q) {
-                const int e = threadIdx.x + q * kSelThreads, r = e / (SP / 2), k = e % (SP / 2) * 2;
-                if (r < TT) {
-                    *(float2 *)&sh.B[r][k] = make_float2(raw.B[q].lo(), raw.B[q].hi());
-                    *(float2 *)&sh.C[r][k] = make_float2(raw.C[q].lo(), raw.C[q].hi());
+            for (int k = 0; k < 4; ++k) {
+                const bool live = has && s0 + 4 * k + rv < l.n;
+                const float g = live ? rg[k].get(0) : 0.0f, raw = rd[k].get(0) + bias, uv = live ? ru[k].get(0) : 0.0f;
+                const float dv = step_size(a, rd[k].get(0), bias, live);
+                float dpv = g, slope = 0.0f;
+                if (z) {
+                    float v;
+                    slope = g * silu_slope(rz[k].get(0), v);
+                    dpv = g * v;
+                    sh.slope[4 * k + rv][ch] = slope;
                 }
+                sh.du[4 * k + rv][ch] = make_float2(dv, dv * uv);
+                sh.own[4 * k + rv][ch] = make_float2(uv, !live ? 0.0f : a.softplus ? sigmoid_of(raw) : 1.0f);
+                sh.dp[4 * k + rv][ch] = dpv;
+                dDv = fmaf(dpv, uv, dDv);
             }
-            __syncthreads();
-            if (tl > 0) raw.load(a, p, m, s0 - TT, u, delta, z, dy, Bm, Cm);
-            const int first = wave * R;
-            float dec[R][SR], h[SR], x[SR], sum = 0.0f;
-            if constexpr (!FOLD) {
+            rB.put(sh.B);
+            rC.put(sh.C);
+            float h[SR];
 #pragma unroll
-                for (int j = 0; j < SR; ++j) h[j] = 0.0f;
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float2 v = sh.du[first + r][ch];
-                sum += v.x;
-#pragma unroll
-                for (int j = 0; j < SR; ++j) {
-                    dec[r][j] = __builtin_amdgcn_exp2f(v.x * (Av[j] * kLog2e));
-                    if constexpr (!FOLD) h[j] = fmaf(dec[r][j], h[j], v.y * sh.B[first + r][row * SR + j]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < SR; ++j) x[j] = 0.0f;
-#pragma unroll
-            for (int r = R - 1; r >= 0; --r) {
-                const float g = dpt[first + r][ch];
-#pragma unroll
-                for (int j = 0; j < SR; ++j) x[j] = dec[r][j] * fmaf(sh.C[first + r][row * SR + j], g, x[j]);
-            }
-            // the state before the tile
-            float hs[SR];
-#pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                sh.P[wave][j][lane] = __builtin_amdgcn_exp2f(sum * (Av[j] * kLog2e));
-                if constexpr (FOLD) {
-                    foldX[wave][j][lane] = x[j];
-                } else {
-                    sh.X[wave][j][lane] = x[j];
-                    sh.H[wave][j][lane] = h[j];
-                    long long at;
-                    hs[j] = state_at<SR>(a, p, b * a.kept + s0 / TT, row, ch, j, at) ? saved[at] : 0.0f;
-                }
-            }
-            __syncthreads();
-            if constexpr (FOLD) {
-                if (wave == 0) {
-#pragma unroll
-                    for (int j = 0; j < SR; ++j) {
-                        float v = sh.carry[turn][j][lane];
-                        for (int w = kSelW - 1; w >= 0; --w) {
-                            v = fmaf(sh.P[w][j][lane], v, foldX[w][j][lane]);
-                            Pall[j] *= sh.P[w][j][lane];
-                        }
-                        sh.carry[turn ^ 1][j][lane] = v;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < SR; ++j) {
-                    h[j] = hs[j];
-                    x[j] = sh.carry[turn][j][lane];
-                }
-                for (int w = 0; w < wave; ++w)
-#pragma unroll
-                    for (int j = 0; j < SR; ++j) h[j] = fmaf(sh.P[w][j][lane], h[j], sh.H[w][j][lane]);
-                for (int w = kSelW - 1; w > wave; --w)
-#pragma unroll
-                    for (int j = 0; j < SR; ++j) x[j] = fmaf(sh.P[w][j][lane], x[j], sh.X[w][j][lane]);
-                float hb[R][SR], yp[R], qv[R], wv[R];
+            for (int j = 0; j < SR; ++j) h[j] = sh.start[0][j][lane] = hs[j];
+            wave_sync();
+            if (bl > 0) fetch(s0 - kSelKeep);
+#pragma unroll 1
+            for (int q = 0; q < NR - 1; ++q) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const float v = sh.du[first + r][ch].y;
+                    const float2 v = sh.du[q * R + r][ch];
+                    float Bv[SR];
+                    row_states<SR>(&sh.B[q * R + r][row * SR], Bv);
+#pragma unroll
+                    for (int j = 0; j < SR; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(v.x * A2[j]), h[j], v.y * Bv[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < SR; ++j) sh.start[q + 1][j][lane] = h[j];
+            }
+#pragma unroll 1
+            for (int q = NR - 1; q >= 0; --q, turn ^= 1) {
+                const int at = q * R;
+                float dec[R][SR], hb[R][SR], yp[R], qv[R], wv[R];
+                // the registers are for decays and states: rows are read again on the way back, and not ahead of their position
+                wave_sync();
+#pragma unroll
+                for (int j = 0; j < SR; ++j) h[j] = sh.start[q][j][lane];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float2 v = sh.du[at + r][ch];
+                    float Bv[SR], Cv[SR];
+                    row_states<SR>(&sh.B[at + r][row * SR], Bv);
+                    row_states<SR>(&sh.C[at + r][row * SR], Cv);
                     yp[r] = 0.0f;
 #pragma unroll
                     for (int j = 0; j < SR; ++j) {
+                        dec[r][j] = __builtin_amdgcn_exp2f(v.x * A2[j]);
                         hb[r][j] = h[j];
-                        h[j] = fmaf(dec[r][j], h[j], v * sh.B[first + r][row * SR + j]);
-                        yp[r] = fmaf(sh.C[first + r][row * SR + j], h[j], yp[r]);
+                        h[j] = fmaf(dec[r][j], h[j], v.y * Bv[j]);
+                        yp[r] = fmaf(Cv[j], h[j], yp[r]);
                     }
+                    made(yp[r]);
+                    if (r % 2) __builtin_amdgcn_sched_barrier(0);
                 }
-                sum_rows_of_lanes<R>(yp);
-                put_rows<R>(sh.y, first, row, ch, yp);
+                sum_states<K>(yp);
+                wave_sync();
 #pragma unroll
                 for (int r = R - 1; r >= 0; --r) {
-                    const float2 v = sh.du[first + r][ch];
-                    const float g = dpt[first + r][ch];
-                    float gB[SR], gC[SR];
+                    const float2 v = sh.du[at + r][ch];
+                    const float g = sh.dp[at + r][ch];
+                    float gB[SR], gC[SR], Bv[SR], Cv[SR];
+                    row_states<SR>(&sh.B[at + r][row * SR], Bv);
+                    row_states<SR>(&sh.C[at + r][row * SR], Cv);
                     qv[r] = wv[r] = 0.0f;
 #pragma unroll
                     for (int j = 0; j < SR; ++j) {
-                        const float bv = sh.B[first + r][row * SR + j];
                         const float ah = dec[r][j] * hb[r][j];
-                        const float G = fmaf(sh.C[first + r][row * SR + j], g, x[j]);
-                        const float t = G * ah;
-                        gC[j] = g * fmaf(v.y, bv, ah);
+                        const float G = fmaf(Cv[j], g, x[j]), t = G * ah;
+                        gC[j] = g * fmaf(v.y, Bv[j], ah);
                         gB[j] = G * v.y;
-                        qv[r] = fmaf(G, bv, qv[r]);
-                        wv[r] = fmaf(t, Av[j], wv[r]);
+                        qv[r] = fmaf(G, Bv[j], qv[r]);
+                        wv[r] = fmaf(t, A2[j], wv[r]);
                         dA[j] = fmaf(t, v.x, dA[j]);
                         x[j] = dec[r][j] * G;
                     }
+                    // lanes of a four write the same value
+                    if constexpr (SR >= 4) {
 #pragma unroll
-                    for (int j = 0; j < SR; ++j) {
-                        gB[j] = sum_channels(gB[j]);
-                        gC[j] = sum_channels(gC[j]);
-                    }
-                    if (ch == 0)
-#pragma unroll
-                        for (int j = 0; j < SR; ++j) {
-                            sh.dB[first + r][row * SR + j] = gB[j];
-                            sh.dC[first + r][row * SR + j] = gC[j];
+                        for (int j = 0; j < SR; j += 4) {
+                            sh.out[turn][0][r][row * SR + j + fv] = sum_four(gB[j], gB[j + 1], gB[j + 2], gB[j + 3]);
+                            sh.out[turn][1][r][row * SR + j + fv] = sum_four(gC[j], gC[j + 1], gC[j + 2], gC[j + 3]);
                         }
-                }
-                sum_rows_of_lanes<R>(qv);
-                put_rows<R>(sh.q, first, row, ch, qv);
-                sum_rows_of_lanes<R>(wv);
-                put_rows<R>(sh.w, first, row, ch, wv);
-                if (wave == 0)
-#pragma unroll
-                    for (int j = 0; j < SR; ++j) sh.carry[turn ^ 1][j][lane] = x[j];
-                __syncthreads();
-                const long long s = s0 + m.row;
-                if (m.have && s < p.last) {
-                    const float2 pv = *(const float2 *)&sh.y[m.row][2 * m.pair];
-                    const float2 q = *(const float2 *)&sh.q[m.row][2 * m.pair];
-                    const float2 w = *(const float2 *)&sh.w[m.row][2 * m.pair];
-                    float e0 = fmaf(u0, q.x, w.x), e1 = fmaf(u1, q.y, w.y);
-                    if (a.softplus) {
-                        e0 *= sigmoid_of(r0);
-                        e1 *= sigmoid_of(r1);
-                    }
-                    e0 = live ? e0 : 0.0f;
-                    e1 = live ? e1 : 0.0f;
-                    const long long at = p.row(a, s) * a.I + p.i0 + 2 * m.pair;
-                    Two<T>::store(du + at, m.have, fmaf(d0, q.x, Dv[0] * dp0), fmaf(d1, q.y, Dv[1] * dp1));
-                    Two<T>::store(ddelta + at, m.have, e0, e1);
-                    if (z)
-                        Two<T>::store(dz + at, m.have, live ? g0 * fmaf(Dv[0], u0, pv.x) * slope[0] : 0.0f,
-                                      live ? g1 * fmaf(Dv[1], u1, pv.y) * slope[1] : 0.0f);
-                    if (live) {
-                        dDv[0] = fmaf(dp0, u0, dDv[0]);
-                        dDv[1] = fmaf(dp1, u1, dDv[1]);
-                        dbv[0] += e0;
-                        dbv[1] += e1;
-                    }
-                }
-                for (int e = threadIdx.x; e < TT * SP; e += kSelThreads) {
-                    const int r = e / SP, k = e % SP;
-                    if (s0 + r >= p.last || k >= a.S) continue;
-                    const long long t = p.row(a, s0 + r);
-                    if (a.tiles == 1) {
-                        Store<T>::store(dB, t * a.S + k, sh.dB[r][k]);
-                        Store<T>::store(dC, t * a.S + k, sh.dC[r][k]);
+                    } else if constexpr (SR == 2) {
+                        sh.out[turn][fv >> 1][r][row * SR + (fv & 1)] = sum_four(gB[0], gB[1], gC[0], gC[1]);
                     } else {
-                        const long long at = (tile * a.B * a.T + t) * a.S + k;
-                        dBp[at] = sh.dB[r][k];
-                        dCp[at] = sh.dC[r][k];
+                        sh.out[turn][fv & 1][r][row] = sum_four(gB[0], gC[0], gB[0], gC[0]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < SR; ++j) made(dA[j]);
+                    made(qv[r]);
+                    made(wv[r]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                sum_states<K>(qv);
+                sum_states<K>(wv);
+#pragma unroll
+                for (int m = 0; m < K; ++m) {
+                    const int e = at + 4 * m + rv;
+                    const long long s = s0 + e;
+                    const float2 o = sh.own[e][ch];
+                    const float ed = fmaf(o.x, qv[m], wv[m] * kLn2) * o.y;
+                    dbv += ed;
+                    const float v[3] = {fmaf(sh.du[e][ch].x, qv[m], Dv * sh.dp[e][ch]), ed,
+                                        z ? sh.slope[e][ch] * fmaf(Dv, o.x, yp[m]) : 0.0f};
+                    const bool live = s < l.n;
+                    if (has && s < last) {
+                        const long long to = l.row(a, s) * a.I + ic;
+                        Store<T>::store(du, to, live ? v[0] : 0.0f);
+                        Store<T>::store(ddelta, to, live ? v[1] : 0.0f);
+                        if (z) Store<T>::store(dz, to, live ? v[2] : 0.0f);
                     }
                 }
-            }
-        }
-        __syncthreads();
-        if (wave == 0 && (FOLD || (dh0 && chunk == 0)))
-#pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                long long at;
-                if (!state_at<SR>(a, p, b, row, ch, j, at)) continue;
-                const float v = sh.carry[turn][j][lane];
-                if (FOLD) fold[chunk * states + at] = make_float2(Pall[j], v);
-                else dh0[at] = v;
-            }
-    }
-    if constexpr (!FOLD) {
-        // the waves' parts of dA, the rows' of dD and dbias, in their order
-        __syncthreads();
-        const Place p(a, 0, tile, 0);
-#pragma unroll
-        for (int j = 0; j < SR; ++j) sh.P[wave][j][lane] = dA[j];
-        float4 *mine = (float4 *)&sh.du[0][0];
-        static_assert(sizeof(sh.du) >= sizeof(float4) * 8 * 16, "");
-        // 64 rows of 8 pairs, 16 rows a turn
-        __syncthreads();
-        if (wave == 0)
-#pragma unroll
-            for (int j = 0; j < SR; ++j) {
-                float s = sh.P[0][j][lane];
-                for (int w = 1; w < kSelW; ++w) s += sh.P[w][j][lane];
-                long long at;
-                if (state_at<SR>(a, p, job0, row, ch, j, at)) dAp[at] = s;
-            }
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int t = 0; t < 4; ++t) {
-            __syncthreads();
-            if (threadIdx.x / 128 == (unsigned)t) mine[threadIdx.x & 127] = make_float4(dDv[0], dDv[1], dbv[0], dbv[1]);
-            __syncthreads();
-            if (threadIdx.x < 8)
-                for (int r = 0; r < 16; ++r) {
-                    const float4 v = mine[r * 8 + threadIdx.x];
-                    acc.x += v.x;
-                    acc.y += v.y;
-                    acc.z += v.z;
-                    acc.w += v.w;
+                if (WIDE) __syncthreads(); else wave_sync();
+                const int step = WIDE ? (int)blockDim.x : 64;
+                for (int e = WIDE ? (int)threadIdx.x : lane; e < 2 * R * SP; e += step) {
+                    const int what = e / (R * SP), r = e / SP % R, k = e % SP;
+                    if (k >= a.S || s0 + at + r >= last) continue;
+                    float v = (WIDE ? shared[0] : sh).out[turn][what][r][k];
+                    if (WIDE)
+                        for (int w = 1; w < waves; ++w) v += shared[w].out[turn][what][r][k];
+                    const long long to = l.row(a, s0 + at + r) * a.S + k;
+                    if (!WIDE || wide == 1) Store<T>::store(what ? dC : dB, to, v);
+                    else (what ? dCp : dBp)[group * a.B * a.T * a.S + to] = v;
                 }
-        }
-        const long long i = p.i0 + 2 * threadIdx.x;
-        if (threadIdx.x < 8 && i < a.I) {
-            float *to = dDp + (job0 * a.I + i) * 2;
-            to[0] = acc.x;
-            to[1] = acc.z;
-            if (i + 1 < a.I) {
-                to[2] = acc.y;
-                to[3] = acc.w;
             }
+            wave_sync();
         }
+        if (dh0 && chunk == 0) store_states<SR>(dh0 + at0, have, x);
+    }
+    store_states<SR>(dAp + (job0 * a.I + ic) * a.S + row * SR, have, dA);
+    dDv += __shfl_xor(dDv, 16);
+    dDv += __shfl_xor(dDv, 32);
+    dbv += __shfl_xor(dbv, 16);
+    dbv += __shfl_xor(dbv, 32);
+    if (row == 0 && has) {
+        dDp[(job0 * a.I + i) * 2] = dDv;
+        dDp[(job0 * a.I + i) * 2 + 1] = dbv;
     }
 }
 
@@ -814,21 +950,22 @@ int check_sel(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype)
 {
     if (B < 1 || T < 1 || I < 1 || S < 1) return PLSTM_EINVAL;
     if (dtype != PLSTM_F32 && dtype != PLSTM_BF16) return PLSTM_EINVAL;
-    if (S > kSelMaxS || B > (1LL << 30) || T > (1LL << 31) || I > (1LL << 30)) return PLSTM_EUNSUPPORTED;
+    if (S > kSelMaxS || B > (1LL << 30) || T > (1LL << 31) || I > (1LL << 24)) return PLSTM_EUNSUPPORTED;
     if (B > (1LL << 30) / I || T > (1LL << 38) / (B * I) || B * I > (1LL << 34) / S) return PLSTM_EUNSUPPORTED;
-    // workgroups of a launch
-    if (B * ((I + kSelCh - 1) / kSelCh) > (1LL << 22)) return PLSTM_EUNSUPPORTED;
+    // waves of a launch
+    if (B * ((I + 15) / 16) > (1LL << 22)) return PLSTM_EUNSUPPORTED;
     return PLSTM_OK;
 }
 
-// Workgroups that fill the card, and jobs that a backward call cuts its positions into.
-constexpr long long kSelFill = 512, kSelJobs = 1024;
+// Waves that fill the card, and the fewest positions of a chunk.
+constexpr long long kSelFill = 2048, kSelChunk = 64;
 
 struct SelPlan {
-    SelArgs a;
-    int SR;
-    float2 *fold;
-    float *dBp, *dCp, *dAp, *dDp;
+    SelArgs a;                          // of the forward and the folds
+    int SR, CL, NB;
+    long long tiles;                    // backward: waves of 16 channels across a sequence's
+    int waves;                          // backward: of a workgroup
+    float *H, *sums, *dBp, *dCp, *dAp, *dDp;
     size_t ws;
 };
 
@@ -838,25 +975,40 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     SelPlan p{};
     SelArgs &a = p.a;
     p.SR = sel_sr(S);
-    const long long tt = sel_tile(p.SR);
-    a = SelArgs{B, T, I, S, reverse, softplus, pu ? pu : I, pd ? pd : I, pz ? pz : I, pB ? pB : S, pC ? pC : S, lengths,
-                (I + kSelCh - 1) / kSelCh, (T + tt - 1) / tt, 1, a.chunk, 0};
-    // Few channels and sequences do not fill the card: chunks of at least 4 tiles run at the same time, at the
-    // price of folding all but one first
-    const long long groups = B * a.tiles;
-    long long chunks = groups * 2 <= kSelFill ? kSelFill / groups : 1;
-    if (chunks > a.kept / 4) chunks = a.kept / 4;
-    if (chunks < 1) chunks = 1;
-    a.chunk = (a.kept + chunks - 1) / chunks * tt;
+    p.CL = sel_cl(p.SR);
+    a.B = B; a.T = T; a.I = I; a.S = S;
+    a.reverse = reverse;
+    a.softplus = softplus;
+    a.pu = pu ? pu : I; a.pd = pd ? pd : I; a.pz = pz ? pz : I; a.pB = pB ? pB : S; a.pC = pC ? pC : S;
+    a.lengths = lengths;
+    const long long lanes = (I + p.CL - 1) / p.CL;
+    p.NB = p.CL == 1 || lanes > 8 ? 1 : lanes > 4 ? 2 : 4;
+    // sequences that share a wave are within 32-bit offsets of each other
+    const long long widest = std::max({a.pu, a.pd, a.pz, a.pB, a.pC});
+    if (T > (1LL << 28) / widest / p.NB) p.NB = 1;
+    a.tiles = (lanes + 15) / 16;
+    a.groups = p.NB == 1 ? B * a.tiles : (B + p.NB - 1) / p.NB;
+    a.kept = (T + kSelKeep - 1) / kSelKeep;
+    p.tiles = (I + 15) / 16;
+    const long long waves = backward ? B * p.tiles : a.groups;
+    long long chunks = 2 * waves <= kSelFill ? kSelFill / waves : 1;
+    if (chunks > (T + kSelChunk - 1) / kSelChunk) chunks = (T + kSelChunk - 1) / kSelChunk;
+    a.chunk = (long long)align_up((size_t)((T + chunks - 1) / chunks), kSelKeep);
     a.chunks = (int)((T + a.chunk - 1) / a.chunk);
-    const long long jobs = (kSelJobs + a.tiles - 1) / a.tiles;
-    a.jobs = jobs < B * a.chunks ? jobs : B * a.chunks;
     Carve cv(ws);
-    if (a.chunks > 1) p.fold = cv.take<float2>((size_t)a.chunks * B * I * S);
+    if (a.chunks > 1) {
+        p.H = cv.take<float>((size_t)a.chunks * B * I * S);
+        p.sums = cv.take<float>((size_t)a.chunks * B * I);
+    }
     if (backward) {
-        if (a.tiles > 1) {
-            p.dBp = cv.take<float>((size_t)a.tiles * B * T * S);
-            p.dCp = cv.take<float>((size_t)a.tiles * B * T * S);
+        p.waves = p.tiles == 1 ? 4 : (int)(p.tiles < 4 ? p.tiles : 4);
+        // each of at most 4096 waves takes as many chunks as the others
+        const long long all = B * a.chunks, each = (all * p.tiles + 4095) / 4096;
+        a.jobs = (all + each - 1) / each;
+        const long long groups = (p.tiles + p.waves - 1) / p.waves;
+        if (p.tiles > 1 && groups > 1) {
+            p.dBp = cv.take<float>((size_t)groups * B * T * S);
+            p.dCp = cv.take<float>((size_t)groups * B * T * S);
         }
         p.dAp = cv.take<float>((size_t)a.jobs * I * S);
         p.dDp = cv.take<float>((size_t)a.jobs * I * 2);
@@ -866,121 +1018,142 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     return p;
 }
 
-bool sel_pitch(int64_t B, int64_t T, int64_t n, int64_t pitch)
+// Rows are at most 2^24 elements apart: lanes' offsets within a stage have 32 bits.
+constexpr long long kSelMaxPitch = 1LL << 24;
+bool sel_pitch(int64_t n, int64_t pitch) { return pitch == 0 || (pitch >= n && pitch <= kSelMaxPitch); }
+
+// The tensors of a call.
+struct SelTensors {
+    const void *u, *delta, *A, *Bm, *Cm, *D, *z, *dbias, *h0, *saved, *dy, *dhT;
+    void *y, *hT, *keep, *du, *ddelta, *dA, *dB, *dC, *dD, *dz, *db, *dh0;
+};
+
+unsigned sel_blocks(long long waves) { return (unsigned)((waves + 3) / 4); }
+
+// Folds all chunks but one, and chains them.
+template <typename T, int SR, int NB, bool BACK>
+int sel_chain(const SelPlan &p, const SelTensors &t, hipStream_t st)
 {
-    return pitch == 0 || (pitch >= n && pitch <= (1LL << 42) / (B * T));
+    constexpr int CL = sel_cl(SR);
+    const SelArgs &a = p.a;
+    k_sel_fold<T, SR, CL, NB, BACK><<<sel_blocks(a.groups * (a.chunks - 1)), 256, 0, st>>>(
+        a, (const T *)t.u, (const T *)t.delta, (const float *)t.A, (const T *)(BACK ? t.Cm : t.Bm), BACK ? a.pC : a.pB,
+        (const T *)t.z, (const T *)t.dy, (const float *)t.dbias, p.H, p.sums);
+    PLSTM_LAUNCH_CHECK();
+    const long long cols = a.B * a.I;
+    k_sel_chain<BACK><<<(unsigned)((cols * a.S + 255) / 256), 256, 0, st>>>(
+        cols, a.I, a.S, a.chunks, (const float *)t.A, (const float *)(BACK ? t.dhT : t.h0), p.H, p.sums);
+    PLSTM_LAUNCH_CHECK();
+    return 2;
 }
 
-template <typename T, int SR>
-int sel_forward(const SelPlan &p, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D,
-                const T *z, const float *dbias, const float *h0, T *y, float *hT, float *saved, hipStream_t st)
+template <typename T, int SR, int NB>
+int sel_forward(const SelPlan &p, const SelTensors &t, hipStream_t st)
 {
+    constexpr int CL = sel_cl(SR);
     const SelArgs &a = p.a;
     int launches = 1;
     if (a.chunks > 1) {
-        k_sel_fwd<T, SR, true><<<(unsigned)(a.B * a.tiles * (a.chunks - 1)), kSelThreads, 0, st>>>(
-            a, u, delta, A, Bm, Cm, D, z, dbias, h0, y, hT, saved, p.fold);
-        PLSTM_LAUNCH_CHECK();
-        ++launches;
+        const int n = sel_chain<T, SR, NB, false>(p, t, st);
+        if (n < 0) return n;
+        launches += n;
     }
-    k_sel_fwd<T, SR, false><<<(unsigned)(a.B * a.tiles * a.chunks), kSelThreads, 0, st>>>(
-        a, u, delta, A, Bm, Cm, D, z, dbias, h0, y, hT, saved, p.fold);
+    k_sel_fwd<T, SR, CL, NB><<<sel_blocks(a.groups * a.chunks), 256, 0, st>>>(
+        a, (const T *)t.u, (const T *)t.delta, (const float *)t.A, (const T *)t.Bm, (const T *)t.Cm, (const float *)t.D,
+        (const T *)t.z, (const float *)t.dbias, (const float *)t.h0, (T *)t.y, (float *)t.hT, (float *)t.keep, p.H);
     PLSTM_LAUNCH_CHECK();
     return launches;
 }
 
-template <typename T>
-int sel_forward_any(const SelPlan &p, const void *u, const void *delta, const void *A, const void *Bm, const void *Cm,
-                    const void *D, const void *z, const void *dbias, const void *h0, void *y, void *hT, void *saved,
-                    hipStream_t st)
-{
-    const SelArgs &a = p.a;
-    if (a.T == 1 && !saved) {
-        const int L = a.S <= 4 ? 1 : a.S <= 8 ? 2 : a.S <= 16 ? 4 : a.S <= 32 ? 8 : 16;
-        const unsigned blocks = (unsigned)((a.B * a.I * L + 255) / 256);
-        const auto step = [&](auto l) {
-            k_sel_step<T, decltype(l)::value><<<blocks, 256, 0, st>>>(
-                a, (const T *)u, (const T *)delta, (const float *)A, (const T *)Bm, (const T *)Cm, (const float *)D,
-                (const T *)z, (const float *)dbias, (const float *)h0, (T *)y, (float *)hT);
-        };
-        switch (L) {
-        case 1: step(std::integral_constant<int, 1>()); break;
-        case 2: step(std::integral_constant<int, 2>()); break;
-        case 4: step(std::integral_constant<int, 4>()); break;
-        case 8: step(std::integral_constant<int, 8>()); break;
-        default: step(std::integral_constant<int, 16>()); break;
-        }
-        PLSTM_LAUNCH_CHECK();
-        return 1;
-    }
-    const auto go = [&](auto sr) {
-        return sel_forward<T, decltype(sr)::value>(p, (const T *)u, (const T *)delta, (const float *)A, (const T *)Bm,
-                                                   (const T *)Cm, (const float *)D, (const T *)z, (const float *)dbias,
-                                                   (const float *)h0, (T *)y, (float *)hT, (float *)saved, st);
-    };
-    switch (p.SR) {
-    case 1: return go(std::integral_constant<int, 1>());
-    case 2: return go(std::integral_constant<int, 2>());
-    case 4: return go(std::integral_constant<int, 4>());
-    case 8: return go(std::integral_constant<int, 8>());
-    default: return go(std::integral_constant<int, 16>());
-    }
-}
-
-struct SelGrads {
-    void *du, *ddelta, *dA, *dB, *dC, *dD, *dz, *db, *dh0;
-};
-
-template <typename T, int SR>
-int sel_backward(const SelPlan &p, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D,
-                 const T *z, const float *dbias, const float *saved, const T *dy, const float *dhT, const SelGrads &g,
-                 hipStream_t st)
+template <typename T, int SR, bool WIDE>
+int sel_backward_walk(const SelPlan &p, const SelTensors &t, hipStream_t st)
 {
     SelArgs a = p.a;
-    int launches = 2;
-    if (a.chunks > 1) {
-        SelArgs f = a;
-        f.jobs = a.B * (a.chunks - 1);
-        k_sel_bwd<T, SR, true><<<(unsigned)(f.jobs * a.tiles), kSelThreads, 0, st>>>(
-            f, u, delta, A, Bm, Cm, D, z, dbias, saved, dy, dhT, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
-            nullptr, nullptr, nullptr, p.fold);
-        PLSTM_LAUNCH_CHECK();
-        ++launches;
-    }
-    k_sel_bwd<T, SR, false><<<(unsigned)(a.jobs * a.tiles), kSelThreads, 0, st>>>(
-        a, u, delta, A, Bm, Cm, D, z, dbias, saved, dy, dhT, (T *)g.du, (T *)g.ddelta, (T *)g.dz, (float *)g.dh0, p.dBp,
-        p.dCp, (T *)g.dB, (T *)g.dC, p.dAp, p.dDp, p.fold);
+    a.tiles = p.tiles;
+    const size_t lds = p.waves * sizeof(BackShared<SR>);
+    const void *fn = (const void *)k_sel_bwd<T, SR, WIDE>;
+    if (lds > 65536 && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return PLSTM_EHIP;
+    const long long blocks = WIDE ? (p.tiles + p.waves - 1) / p.waves * a.jobs : (a.jobs + p.waves - 1) / p.waves;
+    k_sel_bwd<T, SR, WIDE><<<(unsigned)blocks, 64 * p.waves, lds, st>>>(
+        a, (const T *)t.u, (const T *)t.delta, (const float *)t.A, (const T *)t.Bm, (const T *)t.Cm, (const float *)t.D,
+        (const T *)t.z, (const float *)t.dbias, (const float *)t.saved, (const T *)t.dy, (const float *)t.dhT, p.H,
+        (T *)t.du, (T *)t.ddelta, (T *)t.dz, (float *)t.dh0, p.dBp, p.dCp, (T *)t.dB, (T *)t.dC, p.dAp, p.dDp);
     PLSTM_LAUNCH_CHECK();
-    if (a.tiles > 1) {
+    return 1;
+}
+
+template <typename T, int SR, int NB>
+int sel_backward(const SelPlan &p, const SelTensors &t, hipStream_t st)
+{
+    const SelArgs &a = p.a;
+    int launches = 0;
+    if (a.chunks > 1) {
+        const int n = sel_chain<T, SR, NB, true>(p, t, st);
+        if (n < 0) return n;
+        launches += n;
+    }
+    const int n = (p.tiles > 1 ? sel_backward_walk<T, SR, true> : sel_backward_walk<T, SR, false>)(p, t, st);
+    if (n < 0) return n;
+    launches += n;
+    if (p.dBp) {
         const long long n = a.B * a.T * a.S;
-        k_sel_rows<T><<<(unsigned)min((n + 255) / 256, 8192LL), 256, 0, st>>>(n, (int)a.tiles, p.dBp, p.dCp, (T *)g.dB,
-                                                                              (T *)g.dC);
+        k_sel_rows<T><<<(unsigned)min((n + 255) / 256, 8192LL), 256, 0, st>>>(
+            n, (int)((p.tiles + p.waves - 1) / p.waves), p.dBp, p.dCp, (T *)t.dB, (T *)t.dC);
         PLSTM_LAUNCH_CHECK();
         ++launches;
     }
     const long long nA = a.I * a.S;
     k_sel_weights<<<(unsigned)((nA + 2 * a.I + 15) / 16), 256, 0, st>>>(nA, a.I, (int)a.jobs, p.dAp, p.dDp,
-                                                                        (float *)g.dA, (float *)g.dD, (float *)g.db);
+                                                                        (float *)t.dA, (float *)t.dD, (float *)t.db);
     PLSTM_LAUNCH_CHECK();
-    return launches;
+    return launches + 1;
 }
 
 template <typename T>
-int sel_backward_any(const SelPlan &p, const void *u, const void *delta, const void *A, const void *Bm, const void *Cm,
-                     const void *D, const void *z, const void *dbias, const void *saved, const void *dy,
-                     const void *dhT, const SelGrads &g, hipStream_t st)
+int sel_step(const SelPlan &p, const SelTensors &t, hipStream_t st)
 {
-    const auto go = [&](auto sr) {
-        return sel_backward<T, decltype(sr)::value>(p, (const T *)u, (const T *)delta, (const float *)A, (const T *)Bm,
-                                                    (const T *)Cm, (const float *)D, (const T *)z, (const float *)dbias,
-                                                    (const float *)saved, (const T *)dy, (const float *)dhT, g, st);
+    const SelArgs &a = p.a;
+    const int L = a.S <= 4 ? 1 : a.S <= 8 ? 2 : a.S <= 16 ? 4 : a.S <= 32 ? 8 : 16;
+    const unsigned blocks = (unsigned)((a.B * a.I * L + 255) / 256);
+    const auto step = [&](auto l) {
+        k_sel_step<T, decltype(l)::value><<<blocks, 256, 0, st>>>(
+            a, (const T *)t.u, (const T *)t.delta, (const float *)t.A, (const T *)t.Bm, (const T *)t.Cm,
+            (const float *)t.D, (const T *)t.z, (const float *)t.dbias, (const float *)t.h0, (T *)t.y, (float *)t.hT);
     };
-    switch (p.SR) {
-    case 1: return go(std::integral_constant<int, 1>());
-    case 2: return go(std::integral_constant<int, 2>());
-    case 4: return go(std::integral_constant<int, 4>());
-    case 8: return go(std::integral_constant<int, 8>());
-    default: return go(std::integral_constant<int, 16>());
+    switch (L) {
+    case 1: step(std::integral_constant<int, 1>()); break;
+    case 2: step(std::integral_constant<int, 2>()); break;
+    case 4: step(std::integral_constant<int, 4>()); break;
+    case 8: step(std::integral_constant<int, 8>()); break;
+    default: step(std::integral_constant<int, 16>()); break;
+    }
+    PLSTM_LAUNCH_CHECK();
+    return 1;
+}
+
+template <typename T, int SR, int NB>
+int sel_run_one(const SelPlan &p, const SelTensors &t, bool backward, hipStream_t st)
+{
+    return backward ? sel_backward<T, SR, NB>(p, t, st) : sel_forward<T, SR, NB>(p, t, st);
+}
+
+template <typename T>
+int sel_run_all(const SelPlan &p, const SelTensors &t, bool backward, hipStream_t st)
+{
+    if (!backward && p.a.T == 1 && !t.keep) return sel_step<T>(p, t, st);
+    switch (p.SR * 8 + p.NB) {
+    case 9: return sel_run_one<T, 1, 1>(p, t, backward, st);
+    case 10: return sel_run_one<T, 1, 2>(p, t, backward, st);
+    case 12: return sel_run_one<T, 1, 4>(p, t, backward, st);
+    case 17: return sel_run_one<T, 2, 1>(p, t, backward, st);
+    case 18: return sel_run_one<T, 2, 2>(p, t, backward, st);
+    case 20: return sel_run_one<T, 2, 4>(p, t, backward, st);
+    case 33: return sel_run_one<T, 4, 1>(p, t, backward, st);
+    case 34: return sel_run_one<T, 4, 2>(p, t, backward, st);
+    case 36: return sel_run_one<T, 4, 4>(p, t, backward, st);
+    case 65: return sel_run_one<T, 8, 1>(p, t, backward, st);
+    default: return sel_run_one<T, 16, 1>(p, t, backward, st);
     }
 }
 
@@ -994,8 +1167,7 @@ extern "C" {
 size_t pyramid_selective_scan_saved_size(int64_t B, int64_t T, int64_t I, int32_t S)
 {
     if (check_sel(B, T, I, S, PLSTM_F32) != PLSTM_OK) return 0;
-    const int64_t tt = sel_tile(sel_sr(S));
-    return align_up((size_t)B * ((T + tt - 1) / tt) * I * S * sizeof(float), 256);
+    return align_up((size_t)B * ((T + kSelKeep - 1) / kSelKeep) * I * S * sizeof(float), 256);
 }
 
 size_t pyramid_selective_scan_workspace_size(int64_t B, int64_t T, int64_t I, int32_t S, int32_t backward)
@@ -1017,8 +1189,8 @@ int pyramid_selective_scan_forward(int64_t B, int64_t T, int64_t I, int32_t S, i
     if (rc != PLSTM_OK) return rc;
     if ((reverse != 0 && reverse != 1) || (softplus != 0 && softplus != 1) || !u || !delta || !A || !Bm || !Cm || !y || !ws)
         return PLSTM_EINVAL;
-    if (!sel_pitch(B, T, I, u_pitch) || !sel_pitch(B, T, I, delta_pitch) || !sel_pitch(B, T, I, z_pitch) ||
-        !sel_pitch(B, T, S, B_pitch) || !sel_pitch(B, T, S, C_pitch))
+    if (!sel_pitch(I, u_pitch) || !sel_pitch(I, delta_pitch) || !sel_pitch(I, z_pitch) ||
+        !sel_pitch(S, B_pitch) || !sel_pitch(S, C_pitch))
         return PLSTM_EINVAL;
     const size_t e = dtype_size(dtype);
     if (!aligned_to(u, e) || !aligned_to(delta, e) || !aligned_to(A, 4) || !aligned_to(Bm, e) || !aligned_to(Cm, e) ||
@@ -1030,8 +1202,11 @@ int pyramid_selective_scan_forward(int64_t B, int64_t T, int64_t I, int32_t S, i
     const SelPlan p = sel_plan(B, T, I, S, reverse, softplus, u_pitch, delta_pitch, z_pitch, B_pitch, C_pitch, lengths,
                                ws, false);
     timing_begin("selective_fwd", st);
-    const int n = (dtype == PLSTM_F32 ? sel_forward_any<float> : sel_forward_any<uint16_t>)(
-        p, u, delta, A, Bm, Cm, D, z, delta_bias, h0, y, hT, saved, st);
+    SelTensors t{u, delta, A, Bm, Cm, D, z, delta_bias, h0};
+    t.y = y;
+    t.hT = hT;
+    t.keep = saved;
+    const int n = (dtype == PLSTM_F32 ? sel_run_all<float> : sel_run_all<uint16_t>)(p, t, false, st);
     if (n < 0) return n;
     timing_end(n, st);
     return PLSTM_OK;
@@ -1052,8 +1227,8 @@ int pyramid_selective_scan_backward(int64_t B, int64_t T, int64_t I, int32_t S, 
     if ((reverse != 0 && reverse != 1) || (softplus != 0 && softplus != 1) || !u || !delta || !A || !Bm || !Cm ||
         !saved || !dy || !du || !ddelta || !dA || !dB || !dC || !z != !dz || !ws)
         return PLSTM_EINVAL;
-    if (!sel_pitch(B, T, I, u_pitch) || !sel_pitch(B, T, I, delta_pitch) || !sel_pitch(B, T, I, z_pitch) ||
-        !sel_pitch(B, T, S, B_pitch) || !sel_pitch(B, T, S, C_pitch))
+    if (!sel_pitch(I, u_pitch) || !sel_pitch(I, delta_pitch) || !sel_pitch(I, z_pitch) ||
+        !sel_pitch(S, B_pitch) || !sel_pitch(S, C_pitch))
         return PLSTM_EINVAL;
     const size_t e = dtype_size(dtype);
     if (!aligned_to(u, e) || !aligned_to(delta, e) || !aligned_to(A, 4) || !aligned_to(Bm, e) || !aligned_to(Cm, e) ||
@@ -1066,10 +1241,10 @@ int pyramid_selective_scan_backward(int64_t B, int64_t T, int64_t I, int32_t S, 
     hipStream_t st = (hipStream_t)stream;
     const SelPlan p = sel_plan(B, T, I, S, reverse, softplus, u_pitch, delta_pitch, z_pitch, B_pitch, C_pitch, lengths,
                                ws, true);
-    const SelGrads g{du, ddelta, dA, dB, dC, dD, dz, ddelta_bias, dh0};
+    const SelTensors t{u, delta, A, Bm, Cm, D, z, delta_bias, nullptr, saved, dy, dhT, nullptr, nullptr, nullptr,
+                       du, ddelta, dA, dB, dC, dD, dz, ddelta_bias, dh0};
     timing_begin("selective_bwd", st);
-    const int n = (dtype == PLSTM_F32 ? sel_backward_any<float> : sel_backward_any<uint16_t>)(
-        p, u, delta, A, Bm, Cm, D, z, delta_bias, saved, dy, dhT, g, st);
+    const int n = (dtype == PLSTM_F32 ? sel_run_all<float> : sel_run_all<uint16_t>)(p, t, true, st);
     if (n < 0) return n;
     timing_end(n, st);
     return PLSTM_OK;

@@ -80,9 +80,9 @@ def test_selective_scan_refusals(lib):
     for bad in ((0, 5, 8, 16), (2, 5, 8, 65), (2, 5, 1 << 40, 16)):
         assert P.pyramid_selective_scan_workspace_size(*bad) == 0 and P.pyramid_selective_scan_saved_size(*bad) == 0
     assert lib.pyramid_selective_scan_workspace_size(2, 5, 8, 16, 2) == 0
-    # a state for each tile of 64, 32 or 16 positions
-    for S, n in ((1, 64), (16, 64), (17, 32), (32, 32), (33, 16), (64, 16)):
-        assert P.pyramid_selective_scan_saved_size(3, 2 * n + 1, 16, S) == 3 * 3 * 16 * S * 4 + -(3 * 3 * 16 * S * 4) % 256
+    # a state for each 16 positions
+    for S in (1, 16, 17, 64):
+        assert P.pyramid_selective_scan_saved_size(3, 33, 16, S) == 3 * 3 * 16 * S * 4 + -(3 * 3 * 16 * S * 4) % 256
 
 
 def gn_fwd(lib, N=2, V=5, C=8, G=4, dtype=0, act=1, eps=1e-5, x=FAKE, gamma=FAKE, beta=FAKE, y=FAKE, stats=None, ws=FAKE, nbytes=BIG):
