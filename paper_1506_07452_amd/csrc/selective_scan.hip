@@ -44,6 +44,10 @@ struct SelArgs {
 
 // One or two elements from any element on, raw.
 template <typename T, int N> struct Few;
+// A value in the storage type, by the conversion instruction.
+__device__ inline void put_one(float *p, float v) { *p = v; }
+__device__ inline void put_one(uint16_t *p, float v) { *p = (uint16_t)pack_bf16(v, v); }
+
 template <typename T> struct Few<T, 1> {
     typedef T V;
     T w;
@@ -52,7 +56,7 @@ template <typename T> struct Few<T, 1> {
     __device__ float get(int) const { return Store<T>::load(&w, 0); }
     __device__ static void store(T *p, int have, const float *v)
     {
-        if (have > 0) Store<T>::store(p, 0, *v);
+        if (have > 0) put_one(p, *v);
     }
 };
 template <> struct Few<float, 2> {
@@ -104,6 +108,14 @@ template <> struct Few<uint16_t, 2> {
 __device__ inline float softplus_of(float v)
 {
     const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), w = 1.0f + e;
+    return fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.0f)) + fmaxf(v, 0.0f);
+}
+
+// And its derivative, sigmoid(v), from the same exponential.
+__device__ inline float softplus_slope(float v, float &slope)
+{
+    const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), w = 1.0f + e;
+    slope = __builtin_amdgcn_rcpf(w) * (v < 0.0f ? e : 1.0f);
     return fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.0f)) + fmaxf(v, 0.0f);
 }
 
@@ -603,17 +615,19 @@ k_sel_chain(long long cols, long long I, int S, int chunks, const float *A, cons
     if (at >= states) return;
     const float A2 = A[col % I * S + (at - col * S)] * kLog2e;
     float h = from ? from[at] : 0.0f;
-    for (int n = 0; n < chunks; n += 8) {
-        float x[8], s[8];
+    constexpr int U = 16;
+    for (int n = 0; n < chunks; n += U) {
+        float x[U], s[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < U; ++e) {
             const int c = BACK ? chunks - 1 - n - e : n + e;
             const bool has = n + e + 1 < chunks;        // the last one passes nothing on
             x[e] = has ? H[c * states + at] : 0.0f;
             s[e] = has ? sums[c * cols + col] : 0.0f;
         }
+        loads_issued();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < U; ++e) {
             if (n + e >= chunks) break;
             H[(BACK ? chunks - 1 - n - e : n + e) * states + at] = h;
             h = fmaf(__builtin_amdgcn_exp2f(s[e] * A2), h, x[e]);
@@ -710,6 +724,10 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
     }
     const float bias = dbias && has ? dbias[i] : 0.0f, Dv = D && has ? D[i] : 0.0f;
     if (!WIDE && job0 >= a.jobs) return;
+    // element (dB or dC, position, state) of a run's sums that a thread takes where there are no more than threads: from the
+    // run's first row, -1 without one
+    const int oe = WIDE ? (int)threadIdx.x : lane, orow = oe / SP % R, ok = oe % SP;
+    const int out_off = oe < 2 * R * SP && ok < a.S ? (a.reverse ? R - 1 - orow : orow) * a.S + ok : -1;
     for (long long job = job0; job < a.B * a.chunks; job += a.jobs) {
         const long long b = job / a.chunks;
         const int chunk = (int)(job - b * a.chunks);
@@ -728,6 +746,9 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
         StateRows<T, SR, kSelKeep, 1> rB, rC;
         rB.init(a, Bm, a.pB, b, lane);
         rC.init(a, Cm, a.pC, b, lane);
+        // dense outputs are where dy is
+        char *const bu = (char *)du + (wg.base - (const char *)dy), *const bd = (char *)ddelta + (wg.base - (const char *)dy);
+        char *const bz = (char *)dz + (wg.base - (const char *)dy);
         const long long whole = whole_until<1, 1>(a, b, last);
         Few<T, 1> ru[4], rd[4], rz[4], rg[4];
         float hs[SR];
@@ -755,12 +776,15 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
         int turn = 0;
         for (long long bl = blocks - 1; bl >= 0; --bl) {
             const long long s0 = first + bl * kSelKeep;
+            const bool all = s0 + kSelKeep <= whole;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const bool live = has && s0 + 4 * k + rv < l.n;
-                const float g = live ? rg[k].get(0) : 0.0f, raw = rd[k].get(0) + bias, uv = live ? ru[k].get(0) : 0.0f;
-                const float dv = step_size(a, rd[k].get(0), bias, live);
-                float dpv = g, slope = 0.0f;
+                const bool live = has && (all || s0 + 4 * k + rv < l.n);
+                const float g = live ? rg[k].get(0) : 0.0f, uv = live ? ru[k].get(0) : 0.0f;
+                float dv = rd[k].get(0) + bias, back = 1.0f, dpv = g, slope = 0.0f;
+                if (a.softplus) dv = softplus_slope(dv, back);
+                dv = live ? dv : 0.0f;
+                back = live ? back : 0.0f;
                 if (z) {
                     float v;
                     slope = g * silu_slope(rz[k].get(0), v);
@@ -768,7 +792,7 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
                     sh.slope[4 * k + rv][ch] = slope;
                 }
                 sh.du[4 * k + rv][ch] = make_float2(dv, dv * uv);
-                sh.own[4 * k + rv][ch] = make_float2(uv, !live ? 0.0f : a.softplus ? sigmoid_of(raw) : 1.0f);
+                sh.own[4 * k + rv][ch] = make_float2(uv, back);
                 sh.dp[4 * k + rv][ch] = dpv;
                 dDv = fmaf(dpv, uv, dDv);
             }
@@ -829,14 +853,15 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
                     qv[r] = wv[r] = 0.0f;
 #pragma unroll
                     for (int j = 0; j < SR; ++j) {
-                        const float ah = dec[r][j] * hb[r][j];
-                        const float G = fmaf(Cv[j], g, x[j]), t = G * ah;
-                        gC[j] = g * fmaf(v.y, Bv[j], ah);
+                        // the gradient that goes on is a G: times the state before, it is that of the exponent
+                        const float G = fmaf(Cv[j], g, x[j]);
+                        gC[j] = g * (r + 1 < R ? hb[r + 1][j] : h[j]);
                         gB[j] = G * v.y;
                         qv[r] = fmaf(G, Bv[j], qv[r]);
+                        x[j] = dec[r][j] * G;
+                        const float t = x[j] * hb[r][j];
                         wv[r] = fmaf(t, A2[j], wv[r]);
                         dA[j] = fmaf(t, v.x, dA[j]);
-                        x[j] = dec[r][j] * G;
                     }
                     // lanes of a four write the same value
                     if constexpr (SR >= 4) {
@@ -865,27 +890,45 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
                     const float2 o = sh.own[e][ch];
                     const float ed = fmaf(o.x, qv[m], wv[m] * kLn2) * o.y;
                     dbv += ed;
-                    const float v[3] = {fmaf(sh.du[e][ch].x, qv[m], Dv * sh.dp[e][ch]), ed,
-                                        z ? sh.slope[e][ch] * fmaf(Dv, o.x, yp[m]) : 0.0f};
-                    const bool live = s < l.n;
-                    if (has && s < last) {
-                        const long long to = l.row(a, s) * a.I + ic;
-                        Store<T>::store(du, to, live ? v[0] : 0.0f);
-                        Store<T>::store(ddelta, to, live ? v[1] : 0.0f);
-                        if (z) Store<T>::store(dz, to, live ? v[2] : 0.0f);
+                    // from dy's place on, where dense outputs are; padding gets zeros
+                    bool write = has, live = true;
+                    long long to = (s0 + at + 4 * m) * wg.step + wg.off;
+                    if (!all) {
+                        live = s < l.n;
+                        write = has && s < last;
+                        to = (const char *)(dy + l.row(a, s) * a.I + ic) - wg.base;
+                    }
+                    if (write) {
+                        put_one((T *)(bu + to), live ? fmaf(sh.du[e][ch].x, qv[m], Dv * sh.dp[e][ch]) : 0.0f);
+                        put_one((T *)(bd + to), live ? ed : 0.0f);
+                        if (z) put_one((T *)(bz + to), live ? sh.slope[e][ch] * fmaf(Dv, o.x, yp[m]) : 0.0f);
                     }
                 }
                 if (WIDE) __syncthreads(); else wave_sync();
-                const int step = WIDE ? (int)blockDim.x : 64;
-                for (int e = WIDE ? (int)threadIdx.x : lane; e < 2 * R * SP; e += step) {
-                    const int what = e / (R * SP), r = e / SP % R, k = e % SP;
-                    if (k >= a.S || s0 + at + r >= last) continue;
-                    float v = (WIDE ? shared[0] : sh).out[turn][what][r][k];
+                const int step = WIDE ? (int)blockDim.x : 64, e0 = WIDE ? (int)threadIdx.x : lane;
+                const auto add_up = [&](int e) {
+                    float v = (&(WIDE ? shared[0] : sh).out[turn][0][0][0])[e];
                     if (WIDE)
-                        for (int w = 1; w < waves; ++w) v += shared[w].out[turn][what][r][k];
-                    const long long to = l.row(a, s0 + at + r) * a.S + k;
-                    if (!WIDE || wide == 1) Store<T>::store(what ? dC : dB, to, v);
-                    else (what ? dCp : dBp)[group * a.B * a.T * a.S + to] = v;
+                        for (int w = 1; w < waves; ++w) v += (&shared[w].out[turn][0][0][0])[e];
+                    return v;
+                };
+                if (all && 2 * R * SP <= step) {
+                    // one element a thread, a scalar place and the thread's own part
+                    if (out_off >= 0) {
+                        const long long row0 = b * a.T + (a.reverse ? l.n - R - (s0 + at) : s0 + at);
+                        const float v = add_up(e0);
+                        if (!WIDE || wide == 1) put_one((e0 < R * SP ? dB : dC) + row0 * a.S + out_off, v);
+                        else ((e0 < R * SP ? dBp : dCp) + group * a.B * a.T * a.S + row0 * a.S)[out_off] = v;
+                    }
+                } else {
+                    for (int e = e0; e < 2 * R * SP; e += step) {
+                        const int what = e / (R * SP), r = e / SP % R, k = e % SP;
+                        if (k >= a.S || s0 + at + r >= last) continue;
+                        const float v = add_up(e);
+                        const long long to = l.row(a, s0 + at + r) * a.S + k;
+                        if (!WIDE || wide == 1) put_one((what ? dC : dB) + to, v);
+                        else (what ? dCp : dBp)[group * a.B * a.T * a.S + to] = v;
+                    }
                 }
             }
             wave_sync();
@@ -920,20 +963,30 @@ k_sel_rows(long long n, int tiles, const float *dBp, const float *dCp, T *dB, T 
     }
 }
 
-// dA [I S], dD and ddelta_bias [I] from the jobs' parts, in 64 bits: 16 lanes an output.
-__global__ void __launch_bounds__(256)
+// dA [I S], dD and ddelta_bias [I] from the jobs' parts, in 64 bits: L lanes an output.
+template <int L>
+__global__ void __launch_bounds__(16 * L)
 k_sel_weights(long long nA, long long I, int jobs, const float *dAp, const float *dDp, float *dA, float *dD, float *db)
 {
-    __shared__ double lds[16][16];
+    __shared__ double lds[L][16];
     const int o = threadIdx.x % 16, lane = threadIdx.x / 16;
     const long long at = (long long)blockIdx.x * 16 + o, nD = 2 * I;
     double s = 0.0;
-    if (at < nA + nD)
-        for (int j = lane; j < jobs; j += 16) s += (double)(at < nA ? dAp[j * nA + at] : dDp[j * nD + (at - nA)]);
+    if (at < nA + nD) {
+        const float *p = at < nA ? dAp + at : dDp + (at - nA);
+        const long long step = at < nA ? nA : nD;
+#pragma unroll 8
+        for (int j = lane; j < jobs; j += L) s += (double)p[j * step];
+    }
     lds[lane][o] = s;
     __syncthreads();
+#pragma unroll
+    for (int n = L / 2; n > 0; n /= 2) {
+        if (lane < n) lds[lane][o] += lds[lane + n][o];
+        __syncthreads();
+    }
     if (lane || at >= nA + nD) return;
-    for (int l = 1; l < 16; ++l) s += lds[l][o];
+    s = lds[0][o];
     if (at < nA) {
         dA[at] = (float)s;
     } else {
@@ -990,8 +1043,7 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     a.groups = p.NB == 1 ? B * a.tiles : (B + p.NB - 1) / p.NB;
     a.kept = (T + kSelKeep - 1) / kSelKeep;
     p.tiles = (I + 15) / 16;
-    const long long waves = backward ? B * p.tiles : a.groups;
-    long long chunks = 2 * waves <= kSelFill ? kSelFill / waves : 1;
+    long long chunks = 2 * a.groups <= kSelFill ? kSelFill / a.groups : 1;
     if (chunks > (T + kSelChunk - 1) / kSelChunk) chunks = (T + kSelChunk - 1) / kSelChunk;
     a.chunk = (long long)align_up((size_t)((T + chunks - 1) / chunks), kSelKeep);
     a.chunks = (int)((T + a.chunk - 1) / a.chunk);
@@ -1104,8 +1156,14 @@ int sel_backward(const SelPlan &p, const SelTensors &t, hipStream_t st)
         ++launches;
     }
     const long long nA = a.I * a.S;
-    k_sel_weights<<<(unsigned)((nA + 2 * a.I + 15) / 16), 256, 0, st>>>(nA, a.I, (int)a.jobs, p.dAp, p.dDp,
-                                                                        (float *)t.dA, (float *)t.dD, (float *)t.db);
+    const unsigned blocks = (unsigned)((nA + 2 * a.I + 15) / 16);
+    const auto weights = [&](auto l) {
+        constexpr int L = decltype(l)::value;
+        k_sel_weights<L><<<blocks, 16 * L, 0, st>>>(nA, a.I, (int)a.jobs, p.dAp, p.dDp, (float *)t.dA, (float *)t.dD,
+                                                    (float *)t.db);
+    };
+    if (a.jobs > 128) weights(std::integral_constant<int, 64>());
+    else weights(std::integral_constant<int, 16>());
     PLSTM_LAUNCH_CHECK();
     return launches + 1;
 }
