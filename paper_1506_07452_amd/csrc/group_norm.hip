@@ -20,7 +20,7 @@ constexpr int kGnMaxC = 16384;
 constexpr int kGnThreads = 256;
 constexpr int kGnSmall = 1024;          // threads of a workgroup that holds a volume
 constexpr int kGnHeldC = 2048;         // channels that the sums of such a workgroup have LDS for
-constexpr int kGnBlocks = 2048;         // workgroups that a call aims at
+constexpr int kGnBlocks = 1024;         // workgroups that a call aims at
 
 struct GnArgs {
     long long N, V;
@@ -132,32 +132,56 @@ k_gn_sums(GnArgs a, const T *x, double *part)
     sum_rows<kGnThreads, N>(a, lds, s2, [&](int o, double s) { if (first + o < a.C) to[(first + o) * 2 + 1] = s; });
 }
 
-// Sum over a workgroup of 256.
-__device__ inline double sum256(double v, double *lds)
+// Sums of two values over a workgroup of 1024, in a fixed order.
+__device__ inline void sum1024(double &x, double &y, double (*lds)[2])
 {
-    v = lanes_sum<64>(v);
+    x = lanes_sum<64>(x);
+    y = lanes_sum<64>(y);
+    if ((threadIdx.x & 63) == 0) {
+        lds[threadIdx.x / 64][0] = x;
+        lds[threadIdx.x / 64][1] = y;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+    x = lanes_sum<16>(lds[threadIdx.x & 15][0]);
+    y = lanes_sum<16>(lds[threadIdx.x & 15][1]);
+}
+
+// A thread's share of the parts of group g of volume n: f(channel, the part's two sums), four at a time so that their loads
+// are under way together.
+template <typename F>
+__device__ inline void over_parts(const GnArgs &a, const double *part, long long n, int g, F f)
+{
+    const int all = a.slabs * a.Cg;
+    const double2 *p = (const double2 *)part + n * a.slabs * a.C + g * a.Cg;
+    for (int k = threadIdx.x; k < all; k += 4096) {
+        double2 v[4];
+        int c[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = min(k + 1024 * u, all - 1), slab = e / a.Cg;
+            c[u] = e - slab * a.Cg;
+            v[u] = p[(long long)slab * a.C + c[u]];
+        }
+        loads_issued();
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (k + 1024 * u < all) f(g * a.Cg + c[u], v[u]);
+    }
 }
 
 // A group a workgroup.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 k_gn_stats(GnArgs a, const double *part, GroupStats *st, float *stats)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[16][2];
     const long long n = blockIdx.x / (unsigned)a.G;
     const int g = (int)(blockIdx.x - n * a.G);
     double s1 = 0.0, s2 = 0.0;
-    for (int k = threadIdx.x; k < a.slabs * a.Cg; k += 256) {
-        const int slab = k / a.Cg, c = g * a.Cg + k - slab * a.Cg;
-        const double *p = part + ((n * a.slabs + slab) * a.C + c) * 2;
-        s1 += p[0];
-        s2 += p[1];
-    }
-    s1 = sum256(s1, lds);
-    s2 = sum256(s2, lds);
+    over_parts(a, part, n, g, [&](int, double2 v) {
+        s1 += v.x;
+        s2 += v.y;
+    });
+    sum1024(s1, s2, lds);
     if (threadIdx.x) return;
     const GroupStats r(s1, s2, (double)a.V * a.Cg, a.eps);
     st[blockIdx.x] = r;
@@ -192,12 +216,13 @@ template <int N> struct GnAffine {
     }
 };
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kGnThreads)
 k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats *st, T *y)
 {
     constexpr int N = Piece<T>::N, U = 4;
-    const long long n = blockIdx.x / (unsigned)a.slabs, slab = blockIdx.x - n * a.slabs;
+    // from the end, whose rows were read last
+    const long long id = gridDim.x - 1 - blockIdx.x, n = id / a.slabs, slab = id - n * a.slabs;
     const GnColumn<T> col(a, blockIdx.y);
     if (!col.have) return;
     GnAffine<N> f;
@@ -208,7 +233,7 @@ k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const long long q = r + u * a.rows;
-            raw[u] = load_piece<T>(x + at + q * a.C, q < end ? col.have : 0);
+            raw[u] = load_last<STREAM>(x + at + q * a.C, q < end ? col.have : 0);
         }
         loads_issued();
 #pragma unroll
@@ -218,7 +243,7 @@ k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats
             float v[N];
             Piece<T>::unpack(raw[u], v);
             f.apply(v, a.act, v);
-            store_piece<T>(y + at + q * a.C, col.have, v);
+            store_out<STREAM>(y + at + q * a.C, col.have, v);
         }
     }
 }
@@ -369,56 +394,56 @@ k_gn_bwd_sums(GnArgs a, const T *x, const T *gamma, const T *beta, const float *
 }
 
 // The first `groups` workgroups: a group's mean of a and of a xh; the others: dgamma and
-// dbeta of 16 channels, 16 lanes each over the parts of all volumes.
+// dbeta of 16 channels, 64 lanes each over the parts of all volumes.
 template <typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 k_gn_bwd_finish(GnArgs a, int groups, const T *gamma, const double *part, float2 *means, float *dgamma, float *dbeta)
 {
-    __shared__ double lds[512];
+    __shared__ double2 lds[64][16];
     if ((int)blockIdx.x < groups) {
         const long long n = blockIdx.x / (unsigned)a.G;
         const int g = (int)(blockIdx.x - n * a.G);
         double s1 = 0.0, s2 = 0.0;
-        for (int k = threadIdx.x; k < a.slabs * a.Cg; k += 256) {
-            const int slab = k / a.Cg, c = g * a.Cg + k - slab * a.Cg;
-            const double *p = part + ((n * a.slabs + slab) * a.C + c) * 2;
+        over_parts(a, part, n, g, [&](int c, double2 v) {
             const double w = (double)Store<T>::load(gamma, c);
-            s1 = fma(w, p[1], s1);
-            s2 = fma(w, p[0], s2);
-        }
-        s1 = sum256(s1, lds);
-        s2 = sum256(s2, lds);
+            s1 = fma(w, v.y, s1);
+            s2 = fma(w, v.x, s2);
+        });
+        sum1024(s1, s2, (double(*)[2])lds);
         const double inv = 1.0 / ((double)a.V * a.Cg);
         if (threadIdx.x == 0) means[blockIdx.x] = make_float2((float)(s1 * inv), (float)(s2 * inv));
         return;
     }
     const int o = threadIdx.x % 16, lane = threadIdx.x / 16, c = ((int)blockIdx.x - groups) * 16 + o;
-    double s1 = 0.0, s2 = 0.0;
-    if (c < a.C)
-        for (long long k = lane; k < a.N * a.slabs; k += 16) {
-            const double *p = part + (k * a.C + c) * 2;
-            s1 += p[0];
-            s2 += p[1];
+    double2 s = make_double2(0.0, 0.0);
+    if (c < a.C) {
+        const double2 *p = (const double2 *)part + c;
+#pragma unroll 8
+        for (long long k = lane; k < a.N * a.slabs; k += 64) {
+            const double2 v = p[k * a.C];
+            s.x += v.x;
+            s.y += v.y;
         }
-    lds[lane * 16 + o] = s1;
-    lds[256 + lane * 16 + o] = s2;
+    }
+    lds[lane][o] = s;
     __syncthreads();
     if (lane || c >= a.C) return;
-    for (int l = 1; l < 16; ++l) {
-        s1 += lds[l * 16 + o];
-        s2 += lds[256 + l * 16 + o];
+    for (int l = 1; l < 64; ++l) {
+        s.x += lds[l][o].x;
+        s.y += lds[l][o].y;
     }
-    dgamma[c] = (float)s1;
-    dbeta[c] = (float)s2;
+    dgamma[c] = (float)s.x;
+    dbeta[c] = (float)s.y;
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kGnThreads)
 k_gn_bwd_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const float *stats, const T *dy,
                const float2 *means, T *dx)
 {
     constexpr int N = Piece<T>::N, U = 2;
-    const long long n = blockIdx.x / (unsigned)a.slabs, slab = blockIdx.x - n * a.slabs;
+    // from the end, whose rows were read last
+    const long long id = gridDim.x - 1 - blockIdx.x, n = id / a.slabs, slab = id - n * a.slabs;
     const GnColumn<T> col(a, blockIdx.y);
     if (!col.have) return;
     GnBack<N> f;
@@ -436,8 +461,8 @@ k_gn_bwd_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const float 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const long long s = r + u * a.rows;
-            rx[u] = load_piece<T>(x + at + s * a.C, s < end ? col.have : 0);
-            rd[u] = load_piece<T>(dy + at + s * a.C, s < end ? col.have : 0);
+            rx[u] = load_last<STREAM>(x + at + s * a.C, s < end ? col.have : 0);
+            rd[u] = load_last<STREAM>(dy + at + s * a.C, s < end ? col.have : 0);
         }
         loads_issued();
 #pragma unroll
@@ -453,7 +478,7 @@ k_gn_bwd_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const float 
                 f.values(j, a.act, v[j], d[j], xh, dv);
                 d[j] = f.rstd[j] * (fmaf(f.gamma[j], dv, -m1[j]) - xh * m2[j]);
             }
-            store_piece<T>(dx + at + s * a.C, col.have, d);
+            store_out<STREAM>(dx + at + s * a.C, col.have, d);
         }
     }
 }
@@ -652,11 +677,13 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
     double *part = cv.take<double>((size_t)a.N * a.slabs * a.C * 2);
     GroupStats *gs = cv.take<GroupStats>((size_t)a.N * a.G);
     const dim3 grid((unsigned)(a.N * a.slabs), p.blocks_y);
+    const bool stream = a.N * a.V * a.C * (long long)sizeof(T) >= kStreamBytes;
     k_gn_sums<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, part);
     PLSTM_LAUNCH_CHECK();
-    k_gn_stats<<<(unsigned)(a.N * a.G), 256, 0, st>>>(a, part, gs, (float *)stats);
+    k_gn_stats<<<(unsigned)(a.N * a.G), 1024, 0, st>>>(a, part, gs, (float *)stats);
     PLSTM_LAUNCH_CHECK();
-    k_gn_apply<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta, gs, (T *)y);
+    (stream ? k_gn_apply<T, true> : k_gn_apply<T, false>)<<<grid, kGnThreads, 0, st>>>(
+        a, (const T *)x, (const T *)gamma, (const T *)beta, gs, (T *)y);
     PLSTM_LAUNCH_CHECK();
     return 3;
 }
@@ -683,21 +710,22 @@ int gn_backward(const GnPlan &p, const void *x, const void *gamma, const void *b
         }
         PLSTM_LAUNCH_CHECK();
         if (a.N == 1) return 1;
-        k_gn_bwd_finish<T><<<weights, 256, 0, st>>>(a, 0, (const T *)gamma, part, means, (float *)dgamma, (float *)dbeta);
+        k_gn_bwd_finish<T><<<weights, 1024, 0, st>>>(a, 0, (const T *)gamma, part, means, (float *)dgamma, (float *)dbeta);
         PLSTM_LAUNCH_CHECK();
         return 2;
     }
     const dim3 grid((unsigned)(a.N * a.slabs), p.blocks_y);
+    const bool stream = a.N * a.V * a.C * (long long)sizeof(T) >= kStreamBytes;
     k_gn_bwd_sums<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta,
                                                   (const float *)stats, (const T *)dy, part);
     PLSTM_LAUNCH_CHECK();
     const int groups = (int)(a.N * a.G);
-    k_gn_bwd_finish<T><<<groups + weights, 256, 0, st>>>(a, groups, (const T *)gamma, part, means, (float *)dgamma,
+    k_gn_bwd_finish<T><<<groups + weights, 1024, 0, st>>>(a, groups, (const T *)gamma, part, means, (float *)dgamma,
                                                          (float *)dbeta);
     PLSTM_LAUNCH_CHECK();
     if (!dx) return 2;
-    k_gn_bwd_apply<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta,
-                                                   (const float *)stats, (const T *)dy, means, (T *)dx);
+    (stream ? k_gn_bwd_apply<T, true> : k_gn_bwd_apply<T, false>)<<<grid, kGnThreads, 0, st>>>(
+        a, (const T *)x, (const T *)gamma, (const T *)beta, (const float *)stats, (const T *)dy, means, (T *)dx);
     PLSTM_LAUNCH_CHECK();
     return 3;
 }

@@ -38,6 +38,26 @@ __device__ inline float silu_slope(float a, float &silu)
     return s * fmaf(a, t, 1.0f);
 }
 
+// Pieces of tensors too large for the caches: read for the last time, or written for a later launch.  Non-temporal accesses
+// leave the caches to what is read twice, and no written lines behind that the next launch waits to have written back.
+constexpr long long kStreamBytes = 64LL << 20;      // of a tensor, from which on it is accessed so
+template <bool STREAM, typename T>
+__device__ inline u32x4 load_last(const T *p, int have)
+{
+    if (STREAM && have >= Piece<T>::N) return __builtin_nontemporal_load((const typename Piece<T>::V *)p);
+    return load_piece<T>(p, have);
+}
+template <bool STREAM, typename T>
+__device__ inline void store_out(T *p, int have, const float *v)
+{
+    if (STREAM && have >= Piece<T>::N) {
+        const typename Piece<T>::V w = Piece<T>::packed(v);
+        __builtin_nontemporal_store(w, (typename Piece<T>::V *)p);
+    } else {
+        store_piece<T>(p, have, v);
+    }
+}
+
 // 4 elements from any element on: 16 bytes of fp32, 8 of bf16; raw bits.
 template <typename T> struct Four;
 template <> struct Four<float> {
