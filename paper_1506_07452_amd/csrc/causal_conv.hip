@@ -70,10 +70,21 @@ __device__ inline Four<T> input_row(const ConvArgs &a, const ConvRun &r, const T
     return v;
 }
 
-template <typename T, int K, int U>
+// One past the inputs that a tap reads moves up.
+template <int K>
+__device__ inline void shift(float (*w)[4])
+{
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[k][c] = w[k + 1][c];
+}
+
+template <typename T, int K, bool STREAM>
 __global__ void __launch_bounds__(kConvThreads)
 k_conv_fwd(ConvArgs a, const T *x, const T *w, const T *bias, const T *state, T *y, T *state_out)
 {
+    constexpr int U = 8;
     const long long at = (long long)blockIdx.x * kConvThreads + threadIdx.x;
     const long long ri = at / a.pieces;
     if (ri >= a.B * a.runs) return;
@@ -88,28 +99,38 @@ k_conv_fwd(ConvArgs a, const T *x, const T *w, const T *bias, const T *state, T 
         const Taps<T, K> f(w, bias, r.i, r.have);
 #pragma unroll
         for (int k = 0; k < K - 1; ++k) first[k].get(win[k + 1]);
-        for (int p = 0; p < live; p += U) {
+        const auto row = [&](const Four<T> &v, T *to) {
+            shift<K>(win);
+            v.get(win[K - 1]);
+            float o[4];
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[u] = input_row<T, K>(a, r, x, state, r.s0 + min(p + u, live - 1));
-            loads_issued();
+            for (int c = 0; c < 4; ++c) {
+                o[c] = f.bias[c];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (p + u >= live) break;
-#pragma unroll
-                for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) win[k][c] = win[k + 1][c];
-                raw[u].get(win[K - 1]);
-                float v[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    v[c] = f.bias[c];
-#pragma unroll
-                    for (int k = 0; k < K; ++k) v[c] = fmaf(f.w[k][c], win[k][c], v[c]);
-                    if (a.act) v[c] = silu_of(v[c]);
-                }
-                Four<T>::store(yb + step_of(r.s0 + p + u, r.n, a.reverse) * a.I, r.have, v);
+                for (int k = 0; k < K; ++k) o[c] = fmaf(f.w[k][c], win[k][c], o[c]);
+                if (a.act) o[c] = silu_of(o[c]);
             }
+            Four<T>::template store<STREAM>(to, r.have, o);
+        };
+        // whole turns of whole pieces where the wave has nothing else: loads that ask nothing
+        int p = 0;
+        const long long s0 = step_of(r.s0, r.n, a.reverse);
+        const T *px = x + (r.b * a.T + s0) * a.px + r.i;
+        T *py = yb + s0 * a.I;
+        const long long sx = a.reverse ? -a.px : a.px, sy = a.reverse ? -a.I : a.I;
+        if (__all(r.have == 4))
+            for (; __all(p + U <= live); p += U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u].load(px + u * sx, 4);
+                loads_issued();
+#pragma unroll
+                for (int u = 0; u < U; ++u) row(raw[u], py + u * sy);
+                px += U * sx;
+                py += U * sy;
+            }
+        for (; p < live; ++p) {
+            raw[0] = input_row<T, K>(a, r, x, state, r.s0 + p);
+            row(raw[0], yb + step_of(r.s0 + p, r.n, a.reverse) * a.I);
         }
     }
     const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -131,11 +152,12 @@ k_conv_fwd(ConvArgs a, const T *x, const T *w, const T *bias, const T *state, T 
 
 // PB pieces across and kConvThreads / PB runs down a workgroup; workgroups walk down the runs
 // with the parts of dw and dbias in registers.
-template <typename T, int K, int U>
+template <typename T, int K, bool STREAM>
 __global__ void __launch_bounds__(kConvThreads)
 k_conv_bwd(ConvArgs a, int PB, const T *x, const T *w, const T *bias, const T *state, const T *dy,
            const float *dstate_out, T *dx, float *dstate, float *part)
 {
+    constexpr int U = 4;
     __shared__ float lds[kConvThreads][4];
     const int across = threadIdx.x % PB, down = threadIdx.x / PB, rows = kConvThreads / PB;
     const long long piece = (long long)blockIdx.x * PB + across;
@@ -148,6 +170,7 @@ k_conv_bwd(ConvArgs a, int PB, const T *x, const T *w, const T *bias, const T *s
     if (piece < a.pieces) {
         const int have = (int)min(a.I - piece * 4, 4LL);
         const Taps<T, K> f(w, bias, piece * 4, have);
+        const bool pieces = __all(have == 4);
         for (long long ri = (long long)blockIdx.y * rows + down; ri < all; ri += (long long)gridDim.y * rows) {
             const ConvRun r(a, ri, piece);
             T *dxb = dx + r.b * a.T * a.I + r.i;
@@ -157,7 +180,7 @@ k_conv_bwd(ConvArgs a, int PB, const T *x, const T *w, const T *bias, const T *s
             // dx of position s needs da of s .. s + K - 1, dstate's those of 0 .. K - 2
             const int end = live > 0 ? live + K - 1 : before ? K - 1 : 0;
             float win[K][4], daw[K][4];     // inputs up to position p, da of p - (K - 1) .. p
-            Four<T> rx[U], rd[U], first[K];
+            Four<T> first[K];
 #pragma unroll
             for (int k = 0; k < K - 1; ++k) {
                 first[k].zero();
@@ -169,72 +192,91 @@ k_conv_bwd(ConvArgs a, int PB, const T *x, const T *w, const T *bias, const T *s
 #pragma unroll
                 for (int c = 0; c < 4; ++c) daw[k + 1][c] = 0.0f;
             }
-            for (int p = 0; p < end; p += U) {
+            // takes in position q of the run (own: it is not the next one's); its da
+            const auto take = [&](const Four<T> &vx, const Four<T> &vd, bool has, bool own) {
+                shift<K>(win);
+                shift<K>(daw);
+                float g[4];
+                vx.get(win[K - 1]);
+                vd.get(g);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    rx[u].zero();
-                    rd[u].zero();
-                    const long long s = r.s0 + p + u;
-                    if (p + u < end && s < r.n) {
-                        rx[u] = input_row<T, K>(a, r, x, state, s);
-                        rd[u].load(dyb + step_of(s, r.n, a.reverse) * a.I, r.have);
+                for (int c = 0; c < 4; ++c) {
+                    float v = f.bias[c], silu;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v = fmaf(f.w[k][c], win[k][c], v);
+                    const float da = !has ? 0.0f : a.act ? g[c] * silu_slope(v, silu) : g[c];
+                    daw[K - 1][c] = da;
+                    if (own) {
+#pragma unroll
+                        for (int k = 0; k < K; ++k) dw[k][c] = fmaf(da, win[k][c], dw[k][c]);
+                        dw[K][c] += da;
                     }
                 }
-                loads_issued();
+            };
+            // the gradient of position q - (K - 1), which has all its da now
+            const auto give = [&](float *v) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int q = p + u;
-                    if (q >= end) break;
-                    float da[4], g[4];
+                for (int c = 0; c < 4; ++c) {
+                    v[c] = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            win[k][c] = win[k + 1][c];
-                            daw[k][c] = daw[k + 1][c];
-                        }
-                    rx[u].get(win[K - 1]);
-                    rd[u].get(g);
-                    const bool has = r.s0 + q < r.n;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v = f.bias[c];
-#pragma unroll
-                        for (int k = 0; k < K; ++k) v = fmaf(f.w[k][c], win[k][c], v);
-                        float silu;
-                        da[c] = !has ? 0.0f : a.act ? g[c] * silu_slope(v, silu) : g[c];
-                        daw[K - 1][c] = da[c];
-                    }
-                    if (q < live) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-#pragma unroll
-                            for (int k = 0; k < K; ++k) dw[k][c] = fmaf(da[c], win[k][c], dw[k][c]);
-                            dw[K][c] += da[c];
-                        }
-                    }
-                    // position o = q - (K - 1) of the run has all its da
-                    const long long o = r.s0 + q - (K - 1);
-                    if (q >= K - 1 ? q - (K - 1) < live : before) {
-                        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int k = 0; k < K; ++k) v[c] = fmaf(f.w[K - 1 - k][c], daw[k][c], v[c]);
+                }
+            };
+            const auto step = [&](int q) {
+                Four<T> vx, vd;
+                vx.zero();
+                vd.zero();
+                const long long s = r.s0 + q;
+                if (s < r.n) {
+                    vx = input_row<T, K>(a, r, x, state, s);
+                    vd.load(dyb + step_of(s, r.n, a.reverse) * a.I, r.have);
+                }
+                take(vx, vd, s < r.n, q < live);
+                const long long o = s - (K - 1);
+                if (q >= K - 1 ? q - (K - 1) < live : before) {
+                    float v[4];
+                    give(v);
+                    const long long j = o + (K - 1) - r.n;      // row of the state after that this input is
+                    if (dstate_out && j >= 0) {
+                        const float *e = dstate_out + (r.b * (K - 1) + j) * a.I + r.i;
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-#pragma unroll
-                            for (int k = 0; k < K; ++k) v[c] = fmaf(f.w[K - 1 - k][c], daw[k][c], v[c]);
-                        const long long j = o + (K - 1) - r.n;      // row of the state after that this input is
-                        if (dstate_out && j >= 0) {
-                            const float *e = dstate_out + (r.b * (K - 1) + j) * a.I + r.i;
-#pragma unroll
-                            for (int c = 0; c < 4; ++c)
-                                if (c < r.have) v[c] += e[c];
-                        }
-                        if (o >= 0)
-                            Four<T>::store(dxb + step_of(o, r.n, a.reverse) * a.I, r.have, v);
-                        else
-                            Four<float>::store(dstate + (r.b * (K - 1) + (K - 1 + o)) * a.I + r.i, r.have, v);
+                            if (c < r.have) v[c] += e[c];
                     }
+                    if (o >= 0)
+                        Four<T>::template store<STREAM>(dxb + step_of(o, r.n, a.reverse) * a.I, r.have, v);
+                    else
+                        Four<float>::store(dstate + (r.b * (K - 1) + (K - 1 + o)) * a.I + r.i, r.have, v);
                 }
-            }
+            };
+            int q = 0;
+            for (; q < min(K - 1, end); ++q) step(q);
+            // whole turns of whole pieces that the wave's sequences have, not their last ones
+            const long long s0 = step_of(r.s0 + q, r.n, a.reverse);
+            const T *px = x + (r.b * a.T + s0) * a.px + r.i, *pd = dyb + s0 * a.I;
+            const long long sx = a.reverse ? -a.px : a.px, sy = a.reverse ? -a.I : a.I;
+            T *po = dxb + (s0 - (a.reverse ? -(K - 1) : K - 1)) * a.I;
+            if (pieces)
+                for (; __all(q + U <= live && r.s0 + q + U + K - 1 <= r.n); q += U) {
+                    Four<T> rx[U], rd[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        rx[u].load(px + u * sx, 4);
+                        rd[u].load(pd + u * sy, 4);
+                    }
+                    loads_issued();
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        float v[4];
+                        take(rx[u], rd[u], true, true);
+                        give(v);
+                        Four<T>::template store<STREAM>(po + u * sy, 4, v);
+                    }
+                    px += U * sx;
+                    pd += U * sy;
+                    po += U * sy;
+                }
+            for (; q < end; ++q) step(q);
             const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int p = live; p < r.count; ++p) Four<T>::store(dxb + (r.s0 + p) * a.I, r.have, none);
         }
@@ -350,16 +392,18 @@ int pyramid_causal_conv_forward(int64_t B, int64_t T, int64_t I, int32_t K, int3
     const dim3 grid((unsigned)((lanes + kConvThreads - 1) / kConvThreads));
     hipStream_t st = (hipStream_t)stream;
     timing_begin("conv_fwd", st);
+    const bool stream_out = B * T * I * (int64_t)e >= kStreamBytes;
+    const auto go = [&](auto t, auto fn) {
+        typedef decltype(t) S;
+        fn<<<grid, kConvThreads, 0, st>>>(a, (const S *)x, (const S *)w, (const S *)bias, (const S *)state, (S *)y,
+                                          (S *)state_out);
+    };
     const auto run = [&](auto k) {
         constexpr int KK = decltype(k)::value;
         if (dtype == PLSTM_F32)
-            k_conv_fwd<float, KK, 4><<<grid, kConvThreads, 0, st>>>(
-                a, (const float *)x, (const float *)w, (const float *)bias, (const float *)state,
-                (float *)y, (float *)state_out);
+            go(0.0f, stream_out ? k_conv_fwd<float, KK, true> : k_conv_fwd<float, KK, false>);
         else
-            k_conv_fwd<uint16_t, KK, 4><<<grid, kConvThreads, 0, st>>>(
-                a, (const uint16_t *)x, (const uint16_t *)w, (const uint16_t *)bias,
-                (const uint16_t *)state, (uint16_t *)y, (uint16_t *)state_out);
+            go((uint16_t)0, stream_out ? k_conv_fwd<uint16_t, KK, true> : k_conv_fwd<uint16_t, KK, false>);
     };
     switch (K) {
     case 1: run(std::integral_constant<int, 1>()); break;
@@ -399,17 +443,18 @@ int pyramid_causal_conv_backward(int64_t B, int64_t T, int64_t I, int32_t K, int
     const dim3 grid((unsigned)((a.pieces + PB - 1) / PB), (unsigned)parts);
     hipStream_t st = (hipStream_t)stream;
     timing_begin("conv_bwd", st);
+    const bool stream_out = B * T * I * (int64_t)e >= kStreamBytes;
+    const auto go = [&](auto t, auto fn) {
+        typedef decltype(t) S;
+        fn<<<grid, kConvThreads, 0, st>>>(a, PB, (const S *)x, (const S *)w, (const S *)bias, (const S *)state,
+                                          (const S *)dy, (const float *)dstate_out, (S *)dx, (float *)dstate, (float *)ws);
+    };
     const auto run = [&](auto k) {
         constexpr int KK = decltype(k)::value;
         if (dtype == PLSTM_F32)
-            k_conv_bwd<float, KK, 2><<<grid, kConvThreads, 0, st>>>(
-                a, PB, (const float *)x, (const float *)w, (const float *)bias, (const float *)state,
-                (const float *)dy, (const float *)dstate_out, (float *)dx, (float *)dstate, (float *)ws);
+            go(0.0f, stream_out ? k_conv_bwd<float, KK, true> : k_conv_bwd<float, KK, false>);
         else
-            k_conv_bwd<uint16_t, KK, 4><<<grid, kConvThreads, 0, st>>>(
-                a, PB, (const uint16_t *)x, (const uint16_t *)w, (const uint16_t *)bias,
-                (const uint16_t *)state, (const uint16_t *)dy, (const float *)dstate_out,
-                (uint16_t *)dx, (float *)dstate, (float *)ws);
+            go((uint16_t)0, stream_out ? k_conv_bwd<uint16_t, KK, true> : k_conv_bwd<uint16_t, KK, false>);
         k_conv_weights<KK><<<(unsigned)((I * (KK + 1) + 15) / 16), 256, 0, st>>>(
             I, parts, (const float *)ws, (float *)dw, (float *)db);
     };

@@ -65,7 +65,8 @@ template <> struct Four<float> {
     __device__ void load(const float *p, int have) { w = load_piece<float>(p, have); }
     __device__ void get(float *v) const { Piece<float>::unpack(w, v); }
     __device__ void zero() { w = u32x4{0, 0, 0, 0}; }
-    __device__ static void store(float *p, int have, const float *v) { store_piece<float>(p, have, v); }
+    template <bool STREAM = false>
+    __device__ static void store(float *p, int have, const float *v) { store_out<STREAM>(p, have, v); }
 };
 template <> struct Four<uint16_t> {
     typedef uint32_t V __attribute__((ext_vector_type(2), aligned(2)));
@@ -90,10 +91,13 @@ template <> struct Four<uint16_t> {
         v[3] = bits_float(w[1] & 0xffff0000u);
     }
     __device__ void zero() { w[0] = w[1] = 0; }
+    template <bool STREAM = false>
     __device__ static void store(uint16_t *p, int have, const float *v)
     {
         if (have >= 4) {
-            *(V *)p = V{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            const V w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            if (STREAM) __builtin_nontemporal_store(w, (V *)p);
+            else *(V *)p = w;
         } else {
 #pragma unroll
             for (int j = 0; j < 3; ++j)
