@@ -15,7 +15,7 @@
 // rounded to fp32; ratios are 64-bit quotients: codes are a well-defined function of the inputs.
 #include <math.h>
 
-#include "rows.h"
+#include "sequence.h"
 #include "timing.h"
 
 namespace plstm {
@@ -81,10 +81,11 @@ __global__ void k_adamw_clock(Clock *c, double b1, double b2, uint32_t seed)
     *c = clock_at(c->t + 1, b1, b2, seed);
 }
 
-template <int E> __device__ inline float code_ratio(uint32_t k)
+// The ratio of code k, its bits at 20 .. 27 of `code`: those of an fp32 number 2^(E - 127) times the
+// ratio, whose subnormal numbers are the linear codes.
+template <int E> __device__ inline float code_ratio(uint32_t code)
 {
-    return k < 8 ? (float)k * bits_float((uint32_t)(127 - E - 2) << 23)
-                 : bits_float((k << 20) + ((uint32_t)(127 - E) << 23));
+    return bits_float(code) * bits_float((uint32_t)(254 - E) << 23);
 }
 
 // Scale of a block from the bits of its largest magnitude (a NaN the largest of all): a block
@@ -92,24 +93,27 @@ template <int E> __device__ inline float code_ratio(uint32_t k)
 struct Narrow {
     double scale, inv;
     float stored;
+    uint32_t keep;                          // of codes: none of a block of zeros or NaNs
     __device__ explicit Narrow(uint32_t top)
     {
+        const bool none = top == 0 || top >= kInfBits;
         stored = top >= kInfBits ? __builtin_nanf("") : bits_float(top);
-        scale = (double)stored;
-        inv = top == 0 || top >= kInfBits ? 0.0 : 1.0 / scale;
+        scale = none ? 0.0 : (double)stored;
+        inv = none ? 0.0 : 1.0 / scale;
+        keep = none ? 0u : 255u;
     }
     // Code of |x| <= scale.  The quotient: a correctly rounded reciprocal, and a step of
     // Markstein's, which makes the correctly rounded quotient.
     template <int E> __device__ uint32_t code(float x, uint32_t random) const
     {
         const double a = fabs((double)x), q = a * inv;
-        const double r = inv == 0.0 ? 0.0 : fma(fma(-q, scale, a), inv, q);
+        const double r = fma(fma(-q, scale, a), inv, q);
         // exponent, three bits of mantissa and 16 more of the ratio, those before code 8 in equal steps
-        const uint32_t hi = (uint32_t)(__builtin_bit_cast(uint64_t, r) >> 33);
+        const uint64_t bits = __builtin_bit_cast(uint64_t, r);
+        const uint32_t hi = (uint32_t)(bits >> 33);
         const uint32_t fine = hi - ((uint32_t)(1023 - E) << 19);
         const uint32_t low = (uint32_t)(r * (double)(1ull << (18 + E)));
-        uint32_t k = ((hi < ((uint32_t)(1024 - E) << 19) ? low : fine) + random) >> 16;
-        return k;
+        return ((hi < ((uint32_t)(1024 - E) << 19) ? low : fine) + random) >> 16 & keep;
     }
 };
 
@@ -123,23 +127,12 @@ __device__ inline float blend(double b, float m, double k, double g)
 }
 
 // Elements 4 lane .. of a block: pointers start at any element (codes at 16 bytes).
-__device__ inline void load4(const float *p, int have, float *v)
+template <typename T>
+__device__ inline void load4(const T *p, int have, float *v)
 {
-    Piece<float>::unpack(load_piece<float>(p, have), v);
-}
-__device__ inline void load4(const uint16_t *p, int have, float *v)
-{
-    typedef uint32_t V __attribute__((ext_vector_type(2), aligned(2)));
-    if (have >= 4) {
-        const V w = *(const V *)p;
-        v[0] = bits_float(w[0] << 16);
-        v[1] = bits_float(w[0] & 0xffff0000u);
-        v[2] = bits_float(w[1] << 16);
-        v[3] = bits_float(w[1] & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = j < have ? bf16_to_f32(p[j]) : 0.0f;
-    }
+    Four<T> w;
+    w.load(p, have);
+    w.get(v);
 }
 __device__ inline uint32_t load4_codes(const uint8_t *p, int have)
 {
@@ -150,10 +143,13 @@ __device__ inline uint32_t load4_codes(const uint8_t *p, int have)
         if (j < have) w |= (uint32_t)p[j] << (8 * j);
     return w;
 }
+template <bool STREAM>
 __device__ inline void store4_codes(uint8_t *p, int have, const uint32_t *k)
 {
     if (have >= 4) {
-        *(uint32_t *)p = k[0] | k[1] << 8 | k[2] << 16 | k[3] << 24;
+        const uint32_t w = k[0] | k[1] << 8 | k[2] << 16 | k[3] << 24;
+        if (STREAM) __builtin_nontemporal_store(w, (uint32_t *)p);
+        else *(uint32_t *)p = w;
     } else {
 #pragma unroll
         for (int j = 0; j < 3; ++j)
@@ -165,14 +161,15 @@ __device__ inline void wide_m(uint32_t w, float scale, float *v)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t k = w >> (8 * j) & 255u;
-        v[j] = bits_float(float_bits(code_ratio<15>(k & 127u) * scale) | (k & 128u) << 24);
+        const uint32_t k = w << (24 - 8 * j);       // the code at the top, its sign in the sign's place
+        const float f = code_ratio<15>(k >> 4 & 0x07f00000u) * scale;
+        v[j] = bits_float((float_bits(f) & 0x7fffffffu) | (k & 0x80000000u));
     }
 }
 __device__ inline void wide_v(uint32_t w, float scale, float *v)
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = code_ratio<31>(w >> (8 * j) & 255u) * scale;
+    for (int j = 0; j < 4; ++j) v[j] = code_ratio<31>((w >> (8 * j) & 255u) << 20) * scale;
 }
 
 // The tensor of a workgroup's tile, and the tile's first element in it.
@@ -187,12 +184,17 @@ __device__ inline int seg_of(const AdamArgs &a, long long &first)
     return lo;
 }
 
-template <int BITS, typename G>
-__global__ void __launch_bounds__(256)
-k_adamw(AdamArgs a)
+// Elements of a lane's four from `at` on that a tensor of n has; WHOLE: the tile is inside it.
+template <bool WHOLE>
+__device__ inline int have_of(long long n, long long at)
 {
-    long long first;
-    const AdamSeg &s = a.seg[seg_of(a, first)];
+    const long long left = n - at;
+    return WHOLE ? 4 : left < 0 ? 0 : left > 4 ? 4 : (int)left;
+}
+
+template <int BITS, typename G, bool ROOT, bool STREAM, bool WHOLE>
+__device__ inline void adamw_tile(const AdamArgs &a, const AdamSeg &s, long long first)
+{
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     const Clock now = a.clock ? *a.clock : a.now;
     const float lr = a.lr_at ? *a.lr_at : a.lr;
@@ -205,8 +207,7 @@ k_adamw(AdamArgs a)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const long long at = first + (2 * wave + u) * kAdamBlock + 4 * lane;
-        const long long left = s.n - at;
-        const int have = left < 0 ? 0 : left > 4 ? 4 : (int)left;
+        const int have = have_of<WHOLE>(s.n, at);
         load4(s.theta + at, have, p[u]);
         load4((const G *)s.grad + at, have, g[u]);
         if constexpr (BITS == 32) {
@@ -216,17 +217,17 @@ k_adamw(AdamArgs a)
             cm[u] = load4_codes((const uint8_t *)s.m + at, have);
             cv[u] = load4_codes((const uint8_t *)s.v + at, have);
             const long long block = (first + (2 * wave + u) * kAdamBlock) / kAdamBlock;
-            const bool any = block * kAdamBlock < s.n;
+            const bool any = WHOLE || block * kAdamBlock < s.n;
             sm[u] = any ? s.mscale[block] : 0.0f;
             sv[u] = any ? s.vscale[block] : 0.0f;
         }
     }
+    loads_issued();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const long long at0 = first + (2 * wave + u) * kAdamBlock, at = at0 + 4 * lane;
-        if (at0 >= s.n) break;
-        const long long left = s.n - at;
-        const int have = left < 0 ? 0 : left > 4 ? 4 : (int)left;
+        if (!WHOLE && at0 >= s.n) break;
+        const int have = have_of<WHOLE>(s.n, at);
         if constexpr (BITS == 8) {
             wide_m(cm[u], sm[u], m[u]);
             wide_v(cv[u], sv[u], v[u]);
@@ -237,29 +238,24 @@ k_adamw(AdamArgs a)
             const double gd = (double)g[u][j] * gs;
             m[u][j] = blend(a.b1, m[u][j], k1, gd);
             v[u][j] = blend(a.b2, v[u][j], k2, gd * gd);
-            const float step = m[u][j] * now.c1 / (sqrtf(v[u][j] * now.c2) + a.eps);
+            // off by 8 steps of fp32 at most; the root's instruction takes subnormal numbers for 0, which only an
+            // eps of their roots' size would show (ROOT)
+            const float root = ROOT ? sqrtf(v[u][j] * now.c2) : __builtin_amdgcn_sqrtf(v[u][j] * now.c2);
+            const float step = m[u][j] * now.c1 * __builtin_amdgcn_rcpf(root + a.eps);
             q[j] = fmaf(-lr, fmaf(s.decay, p[u][j], step), p[u][j]);
         }
-        store_piece<float>(s.theta + at, have, q);
-        if (s.copy) {
-            typedef uint32_t V __attribute__((ext_vector_type(2), aligned(2)));
-            if (have >= 4) {
-                *(V *)(s.copy + at) = V{pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3])};
-            } else {
-#pragma unroll
-                for (int j = 0; j < 3; ++j)
-                    if (j < have) s.copy[at + j] = f32_to_bf16(q[j]);
-            }
-        }
+        store_out<STREAM>(s.theta + at, have, q);
+        if (s.copy) Four<uint16_t>::store<STREAM>(s.copy + at, have, q);
         if constexpr (BITS == 32) {
-            store_piece<float>((float *)s.m + at, have, m[u]);
-            store_piece<float>((float *)s.v + at, have, v[u]);
+            store_out<STREAM>((float *)s.m + at, have, m[u]);
+            store_out<STREAM>((float *)s.v + at, have, v[u]);
         } else {
+            if (!WHOLE)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                m[u][j] = j < have ? m[u][j] : 0.0f;
-                v[u][j] = j < have ? v[u][j] : 0.0f;
-            }
+                for (int j = 0; j < 4; ++j) {
+                    m[u][j] = j < have ? m[u][j] : 0.0f;
+                    v[u][j] = j < have ? v[u][j] : 0.0f;
+                }
             const Narrow nm(lanes_max<64>(top_bits<4>(m[u]))), nv(lanes_max<64>(top_bits<4>(v[u])));
             const uint32_t kb = key ^ mix32((uint32_t)(at0 >> 32));
             uint32_t km[4], kv[4];
@@ -267,12 +263,12 @@ k_adamw(AdamArgs a)
             for (int j = 0; j < 4; ++j) {
                 const uint32_t random = mix32((uint32_t)(at + j) ^ kb);
                 km[j] = nm.code<15>(m[u][j], random & 0xffffu);
-                km[j] |= km[j] && m[u][j] < 0.0f ? 128u : 0u;
+                km[j] |= km[j] ? float_bits(m[u][j]) >> 24 & 128u : 0u;
                 kv[j] = nv.code<31>(v[u][j], random >> 16);
-                kv[j] = kv[j] == 0 && nv.inv != 0.0 && v[u][j] > 0.0f ? 1u : kv[j];
+                kv[j] = max(kv[j], v[u][j] > 0.0f ? nv.keep & 1u : 0u);
             }
-            store4_codes((uint8_t *)s.m + at, have, km);
-            store4_codes((uint8_t *)s.v + at, have, kv);
+            store4_codes<STREAM>((uint8_t *)s.m + at, have, km);
+            store4_codes<STREAM>((uint8_t *)s.v + at, have, kv);
             if (lane == 0) {
                 s.mscale[at0 / kAdamBlock] = nm.stored;
                 s.vscale[at0 / kAdamBlock] = nv.stored;
@@ -281,7 +277,18 @@ k_adamw(AdamArgs a)
     }
 }
 
+template <int BITS, typename G, bool ROOT, bool STREAM>
+__global__ void __launch_bounds__(256)
+k_adamw(AdamArgs a)
+{
+    long long first;
+    const AdamSeg &s = a.seg[seg_of(a, first)];
+    if (first + kAdamTile <= s.n) adamw_tile<BITS, G, ROOT, STREAM, true>(a, s, first);
+    else adamw_tile<BITS, G, ROOT, STREAM, false>(a, s, first);
+}
+
 // The fp32 numbers that 8-bit moments stand for: theta takes m's, copy v's.
+template <bool STREAM>
 __global__ void __launch_bounds__(256)
 k_adamw_moments(AdamArgs a)
 {
@@ -297,8 +304,8 @@ k_adamw_moments(AdamArgs a)
         float m[4], v[4];
         wide_m(load4_codes((const uint8_t *)s.m + at, have), s.mscale[at0 / kAdamBlock], m);
         wide_v(load4_codes((const uint8_t *)s.v + at, have), s.vscale[at0 / kAdamBlock], v);
-        store_piece<float>(s.theta + at, have, m);
-        store_piece<float>((float *)s.copy + at, have, v);
+        store_out<STREAM>(s.theta + at, have, m);
+        store_out<STREAM>((float *)s.copy + at, have, v);
     }
 }
 
@@ -333,6 +340,14 @@ int for_tiles(AdamArgs &a, int32_t count, F segment, const void *fn, hipStream_t
         tiles += t;
     }
     return launches;
+}
+
+// Parameters that the caches do not hold until they are read again.
+bool large(int32_t count, const plstm_adamw_segment *segs)
+{
+    long long n = 0;
+    for (int32_t k = 0; k < count; ++k) n += segs[k].n;
+    return n * 4 >= kStreamBytes;
 }
 
 int check_segments(int32_t count, const plstm_adamw_segment *segs, int32_t bits)
@@ -401,10 +416,17 @@ int pyramid_adamw_step(int32_t count, const plstm_adamw_segment *segs, int32_t b
         k_adamw_clock<<<1, 1, 0, st>>>((Clock *)clock, beta1, beta2, seed);
         PLSTM_LAUNCH_CHECK();
     }
-    const void *fn = bits == 32 ? (grad_dtype == PLSTM_F32 ? (const void *)k_adamw<32, float>
-                                                           : (const void *)k_adamw<32, uint16_t>)
-                                : (grad_dtype == PLSTM_F32 ? (const void *)k_adamw<8, float>
-                                                           : (const void *)k_adamw<8, uint16_t>);
+    const auto pick = [&](auto root, auto stream) {
+        constexpr bool ROOT = decltype(root)::value, STREAM = decltype(stream)::value;
+        if (bits == 32)
+            return grad_dtype == PLSTM_F32 ? (const void *)k_adamw<32, float, ROOT, STREAM>
+                                           : (const void *)k_adamw<32, uint16_t, ROOT, STREAM>;
+        return grad_dtype == PLSTM_F32 ? (const void *)k_adamw<8, float, ROOT, STREAM>
+                                       : (const void *)k_adamw<8, uint16_t, ROOT, STREAM>;
+    };
+    const void *fn = eps < 1e-15               ? pick(std::true_type(), std::false_type())
+                     : large(count, segs)      ? pick(std::false_type(), std::true_type())
+                                               : pick(std::false_type(), std::false_type());
     const int n = for_tiles(a, count, [&](int32_t k) {
         const plstm_adamw_segment &s = segs[k];
         return AdamSeg{s.theta, s.grad, s.m, s.v, s.mscale, s.vscale, (uint16_t *)s.copy, s.n,
@@ -431,7 +453,7 @@ int pyramid_adamw_moments(int32_t count, const plstm_adamw_segment *segs, void *
         const plstm_adamw_segment &s = segs[k];
         return AdamSeg{(float *)m[k], nullptr, s.m, s.v, s.mscale, s.vscale, (uint16_t *)v[k], s.n,
                        0.0f, 0};
-    }, (const void *)k_adamw_moments, st);
+    }, large(count, segs) ? (const void *)k_adamw_moments<true> : (const void *)k_adamw_moments<false>, st);
     if (n < 0) return n;
     timing_end(n, st);
     return PLSTM_OK;
