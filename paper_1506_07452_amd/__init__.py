@@ -591,14 +591,15 @@ def _tensor(name, t, shape, dtype, dev):
     """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("expected a torch.Tensor, got %r" % type(t))
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.get_device() != dev or \
-            not t.is_contiguous():
-        raise ValueError("%s must be %s %s on cuda:%d and contiguous, got %s %s on %s%s" % (
-            name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device,
-            "" if t.is_contiguous() else ", not contiguous"))
-    return t.data_ptr()
+    try:
+        # a host tensor's device number is -1
+        if t.shape == shape and t.dtype == dtype and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError("expected a torch.Tensor, got %r" % type(t)) from None
+    raise ValueError("%s must be %s %s on cuda:%d and contiguous, got %s %s on %s%s" % (
+        name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device,
+        "" if t.is_contiguous() else ", not contiguous"))
 
 
 def _bytes(ws, dev):
@@ -694,12 +695,13 @@ _scan_ws = {}
 
 
 def _shared_ws(x, dev):
-    """256 bytes that calls which need no workspace share: they do not touch them."""
+    """256 bytes that calls which need no workspace share, as _scan_workspace gives one: they do
+    not touch them."""
     shared = _scan_ws.get(dev)
     if shared is None:
         ws = _workspace(256, x.device)
         shared = _scan_ws[dev] = (ws,) + _bytes(ws, dev)
-    return shared[0]
+    return shared
 
 
 def _scan_workspace(ws, x, dev, stream):
@@ -709,8 +711,7 @@ def _scan_workspace(ws, x, dev, stream):
     if ws is None:
         need = pyramid_scan_workspace_size(*x.shape)
         if need <= 256:
-            _shared_ws(x, dev)
-            return _scan_ws[dev]
+            return _shared_ws(x, dev)
         ws = _temporary(need, x.device, stream)
     return (ws,) + _bytes(ws, dev)
 
@@ -794,32 +795,34 @@ def _pitched(name, t, shape, dtype, dev):
     elements of a row next to each other, rows (b, t) at (b T + t) pitch (0: dense)."""
     if t is None:
         return None, 0
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("expected a torch.Tensor, got %r" % type(t))
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.get_device() != dev:
-        raise ValueError("%s must be %s %s on cuda:%d, got %s %s on %s" % (
-            name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device))
-    if t.is_contiguous():
-        return t.data_ptr(), 0
+    try:
+        if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+            raise ValueError("%s must be %s %s on cuda:%d, got %s %s on %s" % (
+                name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device))
+        if t.is_contiguous():
+            return t.data_ptr(), 0
+        sb, st, sn = t.stride()
+    except AttributeError:
+        raise TypeError("expected a torch.Tensor, got %r" % type(t)) from None
     B, T, n = shape
-    sb, st, sn = t.stride()
     pitch = st if T > 1 else sb if B > 1 else n
     if (n > 1 and sn != 1) or pitch < n or (B > 1 and sb != T * pitch):
         raise ValueError("%s must be contiguous or a slice of contiguous rows, got strides %s" % (
-            name, list(t.stride())))
+            name, (sb, st, sn)))
     return t.data_ptr(), pitch
 
 
 def _main_pitched(name, t):
-    """As _main, for a main input [B][T][n] that may be a slice of wider rows."""
+    """Storage type code, device number, pointer and pitch of a main input [B][T][n] that may
+    be a slice of wider rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("expected a torch.Tensor, got %r" % type(t))
     code = _DT.get(t.dtype)
     if code is None or t.dim() != 3:
         raise ValueError("%s must be float32 or bfloat16 with 3 dimensions" % name)
-    if not t.is_cuda:
-        raise ValueError("%s must live on the GPU" % name)
     dev = t.get_device()
+    if dev < 0:
+        raise ValueError("%s must live on the GPU" % name)
     return (code, dev) + _pitched(name, t, t.shape, t.dtype, dev)
 
 
@@ -886,17 +889,20 @@ def _select_saved(saved, B, T, I, S, dev):
     return saved.data_ptr()
 
 
-def _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev):
-    B, T, I = u.shape
+def _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths):
+    """The device and the arguments of a selective scan call up to its lengths."""
+    dt, dev, pu, lu = _main_pitched("u", u)
+    shape, dtype, f32 = u.shape, u.dtype, torch.float32
+    B, T, I = shape
     S = A.shape[-1] if A.dim() == 2 else 0
-    f32 = torch.float32
-    return (B, T, I, S, dt, int(bool(reverse)), int(bool(softplus)),
-            *_pitched("u", u, u.shape, u.dtype, dev),
-            *_pitched("delta", delta, u.shape, u.dtype, dev), _tensor("A", A, (I, S), f32, dev),
-            *_pitched("Bm", Bm, (B, T, S), u.dtype, dev), *_pitched("Cm", Cm, (B, T, S), u.dtype, dev),
-            _tensor("D", D, (I,), f32, dev), *_pitched("z", z, u.shape, u.dtype, dev),
-            _tensor("delta_bias", delta_bias, (I,), f32, dev),
-            _tensor("lengths", lengths, (B,), torch.int32, dev))
+    pd, ld = _pitched("delta", delta, shape, dtype, dev)
+    pB, lB = _pitched("Bm", Bm, (B, T, S), dtype, dev)
+    pC, lC = _pitched("Cm", Cm, (B, T, S), dtype, dev)
+    pz, lz = _pitched("z", z, shape, dtype, dev)
+    return dev, (B, T, I, S, dt, 1 if reverse else 0, 1 if softplus else 0, pu, lu, pd, ld,
+                 _tensor("A", A, (I, S), f32, dev), pB, lB, pC, lC, _tensor("D", D, (I,), f32, dev),
+                 pz, lz, _tensor("delta_bias", delta_bias, (I,), f32, dev),
+                 _tensor("lengths", lengths, (B,), torch.int32, dev))
 
 
 def pyramid_selective_scan_forward(u, delta, A, Bm, Cm, y, D=None, z=None, delta_bias=None,
@@ -910,16 +916,15 @@ def pyramid_selective_scan_forward(u, delta, A, Bm, Cm, y, D=None, z=None, delta
     reverse as in pyramid_scan_forward; h0, hT [B][I][S] fp32 are the state before and
     after (hT may be h0); saved (pyramid_selective_scan_saved_size bytes) keeps what
     the backward needs."""
-    dt, dev, _, _ = _main_pitched("u", u)
-    args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev)
+    dev, args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths)
     B, T, I, S = args[:4]
     if ws is None:
         need = pyramid_selective_scan_workspace_size(B, T, I, S)
-        ws = _shared_ws(u, dev) if need <= 256 else _temporary(need, u.device, stream)
+        ws = None if need <= 256 else _temporary(need, u.device, stream)
     _run("pyramid_selective_scan_forward", dev, stream, *args,
          _tensor("h0", h0, (B, I, S), torch.float32, dev), _tensor("y", y, u.shape, u.dtype, dev),
          _tensor("hT", hT, (B, I, S), torch.float32, dev), _select_saved(saved, B, T, I, S, dev),
-         *_bytes(ws, dev))
+         *(_shared_ws(u, dev)[1:] if ws is None else _bytes(ws, dev)))
 
 
 def pyramid_selective_scan_backward(u, delta, A, Bm, Cm, saved, dy, du, ddelta, dA, dB, dC, D=None,
@@ -929,8 +934,7 @@ def pyramid_selective_scan_backward(u, delta, A, Bm, Cm, saved, dy, du, ddelta, 
     """Gradients of pyramid_selective_scan_forward: du, ddelta (dz, with z) [B][T][I] and
     dB, dC [B][T][S] in u's dtype; dA [I][S], dD and ddelta_bias [I] (or None), dh0 [B][I][S]
     (or None) in fp32, from dy, dhT (or None) and the forward's inputs and saved buffer."""
-    dt, dev, _, _ = _main_pitched("u", u)
-    args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths, dt, dev)
+    dev, args = _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, lengths)
     B, T, I, S = args[:4]
     if ws is None:
         ws = _temporary(pyramid_selective_scan_workspace_size(B, T, I, S, 1), u.device, stream)
@@ -961,7 +965,9 @@ def _volumes(name, x):
 def _group_norm_ws(ws, N, V, C, G, x, dev, stream):
     if ws is None:
         need = pyramid_group_norm_workspace_size(N, V, C, G)
-        ws = _shared_ws(x, dev) if need <= 256 else _temporary(need, x.device, stream)
+        if need <= 256:
+            return _shared_ws(x, dev)[1:]
+        ws = _temporary(need, x.device, stream)
     return _bytes(ws, dev)
 
 

@@ -216,17 +216,62 @@ template <int N> struct GnAffine {
     }
 };
 
-template <typename T, bool STREAM>
+// The statistics of a volume's groups, made by a workgroup of 256 for itself from few parts (C <= 256 channels).
+__device__ inline void few_stats(const GnArgs &a, const double *part, long long n, double2 *sums, GroupStats *st)
+{
+    const int subs = 256 / a.C, sub = (int)threadIdx.x / a.C, c = (int)threadIdx.x - sub * a.C;
+    double2 s = make_double2(0.0, 0.0);
+    if (sub < subs) {
+        const double2 *p = (const double2 *)part + n * a.slabs * a.C + c;
+#pragma unroll 4
+        for (int k = sub; k < a.slabs; k += subs) {
+            const double2 v = p[k * a.C];
+            s.x += v.x;
+            s.y += v.y;
+        }
+        sums[threadIdx.x] = s;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, all = subs * a.Cg;
+    for (int g = threadIdx.x / 64; g < a.G; g += 4) {
+        double x = 0.0, y = 0.0;
+        for (int e = lane; e < all; e += 64) {
+            const double2 v = sums[e / a.Cg * a.C + g * a.Cg + e % a.Cg];
+            x += v.x;
+            y += v.y;
+        }
+        x = lanes_sum<64>(x);
+        y = lanes_sum<64>(y);
+        if (lane == 0) st[g] = GroupStats(x, y, (double)a.V * a.Cg, a.eps);
+    }
+    __syncthreads();
+}
+
+// FEW: from the parts themselves, a launch less (then stats, where wanted, is written here).
+template <typename T, bool STREAM, bool FEW>
 __global__ void __launch_bounds__(kGnThreads)
-k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats *st, T *y)
+k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats *st, T *y, const double *part, float *stats)
 {
     constexpr int N = Piece<T>::N, U = 4;
+    __shared__ double2 sums[FEW ? 256 : 1];
+    __shared__ GroupStats few[FEW ? 256 : 1];
     // from the end, whose rows were read last
     const long long id = gridDim.x - 1 - blockIdx.x, n = id / a.slabs, slab = id - n * a.slabs;
     const GnColumn<T> col(a, blockIdx.y);
+    if constexpr (FEW) {
+        few_stats(a, part, n, sums, few);
+        if (stats && slab == 0)
+            for (int g = threadIdx.x; g < a.G; g += kGnThreads) {
+                stats[2 * (n * a.G + g)] = few[g].mean;
+                stats[2 * (n * a.G + g) + 1] = few[g].rstd;
+            }
+    }
     if (!col.have) return;
     GnAffine<N> f;
-    f.fill(a, col.c, col.have, gamma, beta, [&](int g) { return st[n * a.G + g]; });
+    f.fill(a, col.c, col.have, gamma, beta, [&](int g) {
+        if constexpr (FEW) return few[g];
+        else return st[n * a.G + g];
+    });
     const long long end = min(a.V, (slab + 1) * a.slab), at = n * a.V * a.C + col.c;
     for (long long r = slab * a.slab + col.row; r < end; r += U * a.rows) {
         u32x4 raw[U];
@@ -615,8 +660,9 @@ GnPlan gn_plan(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype, int32_
     a.rows = kGnThreads / a.across;
     p.blocks_y = (a.pieces + a.across - 1) / a.across;
     p.threads = kGnThreads;
-    // slabs of whole turns of four rows a thread
-    const long long turn = 4LL * a.rows, want = kGnBlocks / (N * p.blocks_y) + 1;
+    // slabs of whole turns of four rows a thread, of one where that would leave most of the card idle
+    const long long turn = N * ((V + 4LL * a.rows - 1) / (4LL * a.rows)) * p.blocks_y < 256 ? a.rows : 4LL * a.rows;
+    const long long want = kGnBlocks / (N * p.blocks_y) + 1;
     a.slab = ((V + want - 1) / want + turn - 1) / turn * turn;
     a.slabs = (int)((V + a.slab - 1) / a.slab);
     return p;
@@ -680,12 +726,19 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
     const bool stream = a.N * a.V * a.C * (long long)sizeof(T) >= kStreamBytes;
     k_gn_sums<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, part);
     PLSTM_LAUNCH_CHECK();
-    k_gn_stats<<<(unsigned)(a.N * a.G), 1024, 0, st>>>(a, part, gs, (float *)stats);
+    // few parts are added by every workgroup for itself (a slab's worth of them: up to 64 of at most 256 channels)
+    const bool few = a.slabs <= 64 && a.C <= 256;
+    if (!few) {
+        k_gn_stats<<<(unsigned)(a.N * a.G), 1024, 0, st>>>(a, part, gs, (float *)stats);
+        PLSTM_LAUNCH_CHECK();
+    }
+    const auto apply = few      ? (stream ? k_gn_apply<T, true, true> : k_gn_apply<T, false, true>)
+                       : stream ? k_gn_apply<T, true, false>
+                                : k_gn_apply<T, false, false>;
+    apply<<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta, gs, (T *)y, part,
+                                       few ? (float *)stats : nullptr);
     PLSTM_LAUNCH_CHECK();
-    (stream ? k_gn_apply<T, true> : k_gn_apply<T, false>)<<<grid, kGnThreads, 0, st>>>(
-        a, (const T *)x, (const T *)gamma, (const T *)beta, gs, (T *)y);
-    PLSTM_LAUNCH_CHECK();
-    return 3;
+    return few ? 2 : 3;
 }
 
 template <typename T>
