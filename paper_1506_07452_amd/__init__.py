@@ -1031,15 +1031,18 @@ def _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay):
             segs[k].vscale = _tensor("vscale", vscale[k], (-(-n // 256),), f32, dev)
         if copies is not None:
             segs[k].copy = _tensor("copies", copies[k], p.shape, torch.bfloat16, dev)
+    starts = [s.theta for s in segs if s.n]
+    if len(set(starts)) < len(starts):
+        raise ValueError("a parameter is given twice")
     return segs, bits, dev0
 
 
-def _adamw_grads(segs, params, grads, dev):
+def _adamw_grads(segs, shapes, grads, dev):
     """Puts the gradients into the segments (None: the tensor is left alone); their type."""
-    if len(grads) != len(params):
+    if len(grads) != len(shapes):
         raise ValueError("one gradient (or None) per parameter")
     dtype = None
-    for seg, p, g in zip(segs, params, grads):
+    for seg, shape, g in zip(segs, shapes, grads):
         if g is None:
             seg.n = 0
             continue
@@ -1047,7 +1050,7 @@ def _adamw_grads(segs, params, grads, dev):
             dtype = g.dtype
             if dtype not in _DT:
                 raise ValueError("gradients must be float32 or bfloat16")
-        seg.grad = _tensor("grads", g, p.shape, dtype, dev)
+        seg.grad = _tensor("grads", g, shape, dtype, dev)
         seg.n = g.numel()
     return PLSTM_F32 if dtype is None else _DT[dtype]
 
@@ -1072,7 +1075,7 @@ def pyramid_adamw_step(params, grads, m, v, lr, step, betas=(0.9, 0.999), eps=1e
     None, or int64 [3] on the device whose first element counts the updates (`step` is then
     ignored), for steps in captured graphs.  seed: of the rounding of 8-bit moments."""
     segs, bits, dev = _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay)
-    dtype = _adamw_grads(segs, params, grads, dev)
+    dtype = _adamw_grads(segs, [p.shape for p in params], grads, dev)
     _adamw_run(segs, bits, dtype, dev, stream, lr, betas, eps, step, seed, clock, grad_scale)
 
 
@@ -1120,6 +1123,7 @@ class AdamW:
                                                      self.vscale, self.copies, weight_decay)
         if got != bits:
             raise ValueError("state has moments in %d bits" % got)
+        self._shapes = [p.shape for p in self.params]
         self._t, self._clock = t, None
         if capturable:
             self._clock = torch.tensor([t, 0, 0], dtype=torch.int64, device=self.params[0].device)
@@ -1139,9 +1143,10 @@ class AdamW:
     def step(self, grads, lr=None, grad_scale=None, stream=None):
         """One update from `grads` (one per parameter, None to leave it alone); lr and
         grad_scale as in pyramid_adamw_step."""
-        for seg, p in zip(self._segs, self.params):
-            seg.theta = p.data_ptr()
-        dtype = _adamw_grads(self._segs, self.params, grads, self._dev)
+        for seg, p, shape in zip(self._segs, self.params, self._shapes):
+            if p.data_ptr() != seg.theta:       # the tensor was given other memory
+                seg.theta = _tensor("params", p, shape, torch.float32, self._dev)
+        dtype = _adamw_grads(self._segs, self._shapes, grads, self._dev)
         _adamw_run(self._segs, self.bits, dtype, self._dev, stream, self.lr if lr is None else lr,
                    self.betas, self.eps, self._t + 1, self.seed, self._clock, grad_scale)
         self._t += 1
@@ -1150,9 +1155,13 @@ class AdamW:
         """fp32 (m, v) of each parameter: the moments themselves, or what their codes stand for."""
         if self.bits == 32:
             return list(zip(self.m, self.v))
-        with torch.cuda.device(self._dev):
+        caller = torch.cuda.current_stream(self._dev)
+        side = caller if stream is None else _torch_stream(stream, self.params[0].device)
+        with torch.cuda.stream(side):
             mout, vout = ([torch.empty(p.shape, device=p.device) for p in self.params] for _ in range(2))
-        pyramid_adamw_moments(self.m, self.v, self.mscale, self.vscale, mout, vout, stream)
+            pyramid_adamw_moments(self.m, self.v, self.mscale, self.vscale, mout, vout, side)
+        for out in mout + vout:         # results are the caller's stream's as well
+            out.record_stream(caller)
         return list(zip(mout, vout))
 
 

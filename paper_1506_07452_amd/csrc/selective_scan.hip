@@ -1036,7 +1036,8 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     a.lengths = lengths;
     const long long lanes = (I + p.CL - 1) / p.CL;
     p.NB = p.CL == 1 || lanes > 8 ? 1 : lanes > 4 ? 2 : 4;
-    // sequences that share a wave are within 32-bit offsets of each other
+    // sequences that share a wave are within 32-bit offsets of each other (wide pitches: fewer chunks and jobs, never
+    // more workspace than the dense rows of workspace_size())
     const long long widest = std::max({a.pu, a.pd, a.pz, a.pB, a.pC});
     if (T > (1LL << 28) / widest / p.NB) p.NB = 1;
     a.tiles = (lanes + 15) / 16;
@@ -1255,10 +1256,10 @@ int pyramid_selective_scan_forward(int64_t B, int64_t T, int64_t I, int32_t S, i
         !aligned_to(D, 4) || !aligned_to(z, e) || !aligned_to(delta_bias, 4) || !aligned_to(lengths, 4) ||
         !aligned_to(h0, 4) || !aligned_to(y, e) || !aligned_to(hT, 4) || !aligned_to(saved, 16) || !aligned_to(ws, 16))
         return PLSTM_EINVAL;
-    if (ws_bytes < pyramid_selective_scan_workspace_size(B, T, I, S, 0)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const SelPlan p = sel_plan(B, T, I, S, reverse, softplus, u_pitch, delta_pitch, z_pitch, B_pitch, C_pitch, lengths,
                                ws, false);
+    if (ws_bytes < p.ws) return PLSTM_EWORKSPACE;
     timing_begin("selective_fwd", st);
     SelTensors t{u, delta, A, Bm, Cm, D, z, delta_bias, h0};
     t.y = y;
@@ -1295,10 +1296,10 @@ int pyramid_selective_scan_backward(int64_t B, int64_t T, int64_t I, int32_t S, 
         !aligned_to(ddelta, e) || !aligned_to(dA, 4) || !aligned_to(dB, e) || !aligned_to(dC, e) || !aligned_to(dD, 4) ||
         !aligned_to(dz, e) || !aligned_to(ddelta_bias, 4) || !aligned_to(dh0, 4) || !aligned_to(ws, 16))
         return PLSTM_EINVAL;
-    if (ws_bytes < pyramid_selective_scan_workspace_size(B, T, I, S, 1)) return PLSTM_EWORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const SelPlan p = sel_plan(B, T, I, S, reverse, softplus, u_pitch, delta_pitch, z_pitch, B_pitch, C_pitch, lengths,
                                ws, true);
+    if (ws_bytes < p.ws) return PLSTM_EWORKSPACE;
     const SelTensors t{u, delta, A, Bm, Cm, D, z, delta_bias, nullptr, saved, dy, dhT, nullptr, nullptr, nullptr,
                        du, ddelta, dA, dB, dC, dD, dz, ddelta_bias, dh0};
     timing_begin("selective_bwd", st);

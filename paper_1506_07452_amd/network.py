@@ -18,14 +18,17 @@ from typing import List, Optional, Tuple
 import torch
 
 from . import (_torch_stream, checkpoint8_empty, plstm_shape, pyramid_checkpoint8_pack,
+               pyramid_causal_conv_backward, pyramid_causal_conv_forward,
                pyramid_checkpoint8_unpack, pyramid_fc_tanh_backward, pyramid_fc_tanh_forward,
+               pyramid_group_norm_backward, pyramid_group_norm_forward,
                pyramid_head_forward, pyramid_head_forward_supported,
                pyramid_head_train, pyramid_head_workspace_size, pyramid_layer_norm_backward,
                pyramid_layer_norm_forward, pyramid_lstm_backward,
                pyramid_lstm_forward, pyramid_lstm_saved_size, pyramid_lstm_workspace_size,
                pyramid_lstm2d_backward, pyramid_lstm2d_forward, pyramid_lstm2d_saved_size,
                pyramid_scan_backward, pyramid_scan_forward, pyramid_scan_saved_size,
-               pyramid_softmax_ce, shape2d_for, shape_for)
+               pyramid_selective_scan_backward, pyramid_selective_scan_forward,
+               pyramid_selective_scan_saved_size, pyramid_softmax_ce, shape2d_for, shape_for)
 
 
 @dataclass
@@ -228,6 +231,94 @@ def _on_its_stream(fn):
     return call
 
 
+def _lines(x, axis):
+    """[lines][T][n]: a volume's [N][D][H][W][n] lines along `axis` ("zyx": all its voxels in
+    raster order); a copy for "z" and "y"."""
+    if x is None:
+        return None
+    if x.dim() != 5 or axis not in ("z", "y", "x", "zyx"):
+        raise ValueError("x must be [N][D][H][W][C] and axis one of z, y, x, zyx")
+    if axis == "zyx":
+        return x.reshape(x.shape[0], -1, x.shape[-1])
+    if axis != "x":
+        x = x.movedim({"z": 1, "y": 2}[axis], 3).contiguous()
+    return x.reshape(-1, x.shape[3], x.shape[4])
+
+
+def _unlines(t, shape, axis):
+    """The volume [N][D][H][W][n] of _lines' output for a volume of `shape`."""
+    N, D, H, W = shape[:4]
+    if axis == "z":
+        return t.view(N, H, W, D, -1).movedim(3, 1).contiguous()
+    if axis == "y":
+        return t.view(N, D, W, H, -1).movedim(3, 2).contiguous()
+    return t.view(N, D, H, W, -1)
+
+
+@_on_its_stream
+def group_norm_forward(x, gamma, beta, groups: int, act: str = "none", eps: float = 1e-5,
+                       training: bool = False, ws=None, stream=None):
+    """Group norm over the voxels of each volume x [N][...][C] with an activation ("none" or
+    "silu"); returns (y, kept): kept is None for inference, else what
+    group_norm_backward needs."""
+    y = torch.empty_like(x)
+    stats = None
+    if training:
+        stats = torch.empty((x.shape[0], groups, 2), dtype=torch.float32, device=x.device)
+    pyramid_group_norm_forward(x, gamma, beta, y, groups, act, stats, eps, ws, stream)
+    return y, (x, stats, groups, act) if training else None
+
+
+@_on_its_stream
+def group_norm_backward(dy, kept, gamma, beta, want_dx: bool = True, ws=None, stream=None):
+    """(dx or None, dgamma, dbeta) of group_norm_forward."""
+    x, stats, groups, act = kept
+    dx = torch.empty_like(x) if want_dx else None
+    dgamma, dbeta = (torch.empty(x.shape[-1], dtype=torch.float32, device=x.device) for _ in range(2))
+    pyramid_group_norm_backward(x, gamma, beta, stats, dy, dx, dgamma, dbeta, groups, act, ws, stream)
+    return dx, dgamma, dbeta
+
+
+@_on_its_stream
+def selective_forward(u, delta, z, Bm, Cm, p, axis: str, reverse: bool = False, training: bool = False,
+                      ws=None, stream=None):
+    """Selective sweep of a volume: a causal convolution with SiLU of u, then a selective scan of it gated
+    by z, along the lines of `axis` ("z", "y" or "x", "zyx": all voxels in raster order;
+    from the far side with `reverse`).  u, delta, z [N][D][H][W][I], Bm, Cm [N][D][H][W][S]; p: a dict
+    of conv_w [I][K], conv_b [I] in their dtype and A [I][S], D, delta_bias [I] fp32.
+    Returns (y, kept): kept is None for inference, else what selective_backward needs."""
+    shape = u.shape
+    u, delta, z, Bm, Cm = (_lines(t, axis) for t in (u, delta, z, Bm, Cm))
+    v, y = torch.empty_like(u), torch.empty_like(u)
+    pyramid_causal_conv_forward(u, p["conv_w"], p["conv_b"], v, act="silu", reverse=reverse, stream=stream)
+    saved = None
+    if training:
+        saved = torch.empty(pyramid_selective_scan_saved_size(*u.shape, p["A"].shape[1]), dtype=torch.uint8,
+                            device=u.device)
+    pyramid_selective_scan_forward(v, delta, p["A"], Bm, Cm, y, p["D"], z, p["delta_bias"], True, reverse,
+                                   saved=saved, ws=ws, stream=stream)
+    return _unlines(y, shape, axis), (u, v, delta, z, Bm, Cm, saved, axis, reverse) if training else None
+
+
+@_on_its_stream
+def selective_backward(dy, kept, p, ws=None, stream=None):
+    """Gradients of selective_forward: a dict of u, delta, z, Bm, Cm (volumes) and conv_w,
+    conv_b, A, D, delta_bias (fp32)."""
+    u, v, delta, z, Bm, Cm, saved, axis, reverse = kept
+    shape, dy = dy.shape, _lines(dy, axis)
+    g = {k: torch.empty_like(t) for k, t in (("v", v), ("delta", delta), ("z", z), ("Bm", Bm), ("Cm", Cm), ("u", u))}
+    for k in ("conv_w", "conv_b", "A", "D", "delta_bias"):
+        g[k] = torch.empty_like(p[k], dtype=torch.float32)
+    pyramid_selective_scan_backward(v, delta, p["A"], Bm, Cm, saved, dy, g["v"], g["delta"], g["A"], g["Bm"],
+                                    g["Cm"], p["D"], z, p["delta_bias"], True, g["D"], g["z"], g["delta_bias"],
+                                    reverse, ws=ws, stream=stream)
+    pyramid_causal_conv_backward(u, p["conv_w"], p["conv_b"], g.pop("v"), g["u"], g["conv_w"], g["conv_b"],
+                                 act="silu", reverse=reverse, stream=stream)
+    for k in ("u", "delta", "z", "Bm", "Cm"):
+        g[k] = _unlines(g[k], shape, axis)
+    return g
+
+
 @_on_its_stream
 def network_forward(x, layers: List[LayerW], fcs: List[Tuple[torch.Tensor, torch.Tensor]],
                     head: Tuple[torch.Tensor, torch.Tensor], labels: Optional[torch.Tensor] = None,
@@ -423,7 +514,7 @@ def _train_step_unfused(x, layers, fcs, head, labels, ws=None, stream=None, loss
 
 
 def network_parameters(layers, fcs, head, norms=None):
-    """Every parameter tensor of a network, in the order of
+    """Every parameter tensor of a network, for RMSprop or AdamW, in the order of
     `network_gradients`: per layer (wx, wh, b), per hidden FC (w, b), head, per
     norm (gamma, beta)."""
     out = []
