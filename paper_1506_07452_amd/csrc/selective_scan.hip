@@ -698,7 +698,7 @@ struct alignas(16) BackShared {
 // the same chunk and add up their dB and dC; else each has the only 16 channels of a sequence of its own.
 // dBp, dCp [group of channels][b][t][S] (one group: dB and dC themselves); dAp [job][I][S], dDp [job][I][2].
 template <typename T, int SR, bool WIDE>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, SR <= 8 ? 2 : 1)
 k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D, const T *z,
           const float *dbias, const float *saved, const T *dy, const float *dhT, const float *behind, T *du, T *ddelta,
           T *dz, float *dh0, float *dBp, float *dCp, T *dB, T *dC, float *dAp, float *dDp)
