@@ -518,7 +518,7 @@ int pyramid_checkpoint8_unpack(int64_t n, int32_t dtype, const void *q, const vo
  *   state_out   : NULL, or [B][K - 1][I]: the last K - 1 inputs of each sequence
  *                 (of the state, where it is shorter), overwritten; may be
  *                 `state` itself, so single steps (T = 1) carry it in place.
- * B, T, I >= 1, 1 <= K <= 8, B I <= 2^30, T <= 2^31, B T I <= 2^38. */
+ * B, T, I >= 1, 1 <= K <= 8, B I <= 2^30, T <= 2^31, B T I <= 2^38, B T x_pitch <= 2^40. */
 size_t pyramid_causal_conv_workspace_size(int64_t B, int64_t T, int64_t I, int32_t K);
 int pyramid_causal_conv_forward(int64_t B, int64_t T, int64_t I, int32_t K, int32_t dtype,
                                 int32_t act, int32_t reverse, const void *x, int64_t x_pitch,
@@ -597,7 +597,7 @@ int pyramid_selective_scan_backward(int64_t B, int64_t T, int64_t I, int32_t S, 
  *   stats       : NULL, or fp32 [N][G][2], overwritten with (mean, rstd) for the
  *                 backward, whose (x - mean) is that of the rounded mean.
  *   ws          : at least pyramid_group_norm_workspace_size() bytes.
- * 1 <= C <= 16384, G divides C, N <= 2^22, V <= 2^36, N V C <= 2^38. */
+ * 1 <= C <= 16384, G divides C, N <= 2^22, N G <= 2^30, V <= 2^36, N V C <= 2^38. */
 size_t pyramid_group_norm_workspace_size(int64_t N, int64_t V, int32_t C, int32_t G);
 int pyramid_group_norm_forward(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype, int32_t act,
                                float eps, const void *x, const void *gamma, const void *beta, void *y,

@@ -7,6 +7,8 @@
 //   dw[k] = sum_s da_s x_{s - (K - 1) + k},  dbias = sum_s da_s
 // A lane has 4 channels and walks a run of positions with the last K inputs in registers,
 // so x is read once (and K - 1 rows more a run); everything is bound by bytes.
+#include <algorithm>
+
 #include "sequence.h"
 #include "timing.h"
 
@@ -15,7 +17,7 @@ namespace {
 
 constexpr int kConvMaxK = 8;
 constexpr int kConvThreads = 256;
-constexpr int kConvMaxParts = 512;          // workgroups down the positions, each with a part of dw and dbias
+constexpr int kConvParts = 512, kConvMaxParts = 65535;     // workgroups down the positions, each with a part of dw and dbias
 
 struct ConvArgs {
     long long B, T, I, px;                  // px: elements from one row of x to the next
@@ -354,7 +356,8 @@ int conv_parts(const ConvArgs &a)
 {
     const long long rows = kConvThreads / conv_across(a);
     const long long need = (a.B * a.runs + rows - 1) / rows;
-    return (int)(need < kConvMaxParts ? need : kConvMaxParts);
+    // two runs a lane from some point on: what it adds up in 32 bits stays short (the parts are added in 64)
+    return (int)(need <= kConvParts ? need : std::min<long long>(std::max<long long>(need / 2, kConvParts), kConvMaxParts));
 }
 
 bool conv_pitch(int64_t B, int64_t T, int64_t I, int64_t px)

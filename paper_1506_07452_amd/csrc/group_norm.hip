@@ -396,9 +396,9 @@ k_gn_bwd_sums(GnArgs a, const T *x, const T *gamma, const T *beta, const float *
     const long long n = blockIdx.x / (unsigned)a.slabs, slab = blockIdx.x - n * a.slabs;
     const GnColumn<T> col(a, blockIdx.y);
     const long long end = min(a.V, (slab + 1) * a.slab), at = n * a.V * a.C + col.c;
-    float p[N], q[N];
+    double ps[N], qs[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) p[j] = q[j] = 0.0f;
+    for (int j = 0; j < N; ++j) ps[j] = qs[j] = 0.0;
     if (col.have) {
         GnBack<N> f;
         f.fill(a, n, col.c, col.have, gamma, beta, stats);
@@ -411,6 +411,9 @@ k_gn_bwd_sums(GnArgs a, const T *x, const T *gamma, const T *beta, const float *
                 rd[u] = load_piece<T>(dy + at + s * a.C, s < end ? col.have : 0);
             }
             loads_issued();
+            float p[N], q[N];           // of a turn in 32 bits, of turns in 64
+#pragma unroll
+            for (int j = 0; j < N; ++j) p[j] = q[j] = 0.0f;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (r + u * a.rows >= end) break;
@@ -425,17 +428,17 @@ k_gn_bwd_sums(GnArgs a, const T *x, const T *gamma, const T *beta, const float *
                     q[j] += dv;
                 }
             }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                ps[j] += (double)p[j];
+                qs[j] += (double)q[j];
+            }
         }
     }
-    double s[N];
     const int first = blockIdx.y * a.across * N;
     double *to = part + (long long)blockIdx.x * a.C * 2;
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = (double)p[j];
-    sum_rows<kGnThreads, N>(a, lds, s, [&](int o, double t) { if (first + o < a.C) to[(first + o) * 2] = t; });
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = (double)q[j];
-    sum_rows<kGnThreads, N>(a, lds, s, [&](int o, double t) { if (first + o < a.C) to[(first + o) * 2 + 1] = t; });
+    sum_rows<kGnThreads, N>(a, lds, ps, [&](int o, double t) { if (first + o < a.C) to[(first + o) * 2] = t; });
+    sum_rows<kGnThreads, N>(a, lds, qs, [&](int o, double t) { if (first + o < a.C) to[(first + o) * 2 + 1] = t; });
 }
 
 // The first `groups` workgroups: a group's mean of a and of a xh; the others: dgamma and
@@ -624,6 +627,7 @@ int check_gn(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype)
     if (N < 1 || V < 1 || C < 1 || G < 1 || C % G) return PLSTM_EINVAL;
     if (dtype != PLSTM_F32 && dtype != PLSTM_BF16) return PLSTM_EINVAL;
     if (C > kGnMaxC || N > (1LL << 22) || V > (1LL << 36) || N * V > (1LL << 38) / C) return PLSTM_EUNSUPPORTED;
+    if (N * G > (1LL << 30)) return PLSTM_EUNSUPPORTED;         // workgroups of a launch
     return PLSTM_OK;
 }
 

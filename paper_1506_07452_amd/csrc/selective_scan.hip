@@ -630,7 +630,9 @@ k_sel_chain(long long cols, long long I, int S, int chunks, const float *A, cons
         for (int e = 0; e < U; ++e) {
             if (n + e >= chunks) break;
             H[(BACK ? chunks - 1 - n - e : n + e) * states + at] = h;
-            h = fmaf(__builtin_amdgcn_exp2f(s[e] * A2), h, x[e]);
+            // whole powers of 2 apart: the product may be a number where a chunk's growth alone is none
+            const float p = fminf(fmaxf(s[e] * A2, -1e6f), 1e6f), whole = rintf(p);
+            h = ldexpf(h * __builtin_amdgcn_exp2f(p - whole), (int)whole) + x[e];
         }
     }
 }
@@ -715,12 +717,15 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
     const bool has = i < a.I;
     const long long ic = has ? i : 0;
     const int have = states_have<SR>(a, row, has);
+    // sums over the steps: of a block in 32 bits, of blocks in 64
     float A2[SR], dA[SR], dDv = 0.0f, dbv = 0.0f;
+    double dAs[SR], dDs = 0.0, dbs = 0.0;
     load_states<SR>(A + ic * a.S + row * SR, have, A2);
 #pragma unroll
     for (int j = 0; j < SR; ++j) {
         A2[j] *= kLog2e;
         dA[j] = 0.0f;
+        dAs[j] = 0.0;
     }
     const float bias = dbias && has ? dbias[i] : 0.0f, Dv = D && has ? D[i] : 0.0f;
     if (!WIDE && job0 >= a.jobs) return;
@@ -932,17 +937,27 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
                 }
             }
             wave_sync();
+#pragma unroll
+            for (int j = 0; j < SR; ++j) {
+                dAs[j] += (double)dA[j];
+                dA[j] = 0.0f;
+            }
+            dDs += (double)dDv;
+            dbs += (double)dbv;
+            dDv = dbv = 0.0f;
         }
         if (dh0 && chunk == 0) store_states<SR>(dh0 + at0, have, x);
     }
+#pragma unroll
+    for (int j = 0; j < SR; ++j) dA[j] = (float)dAs[j];
     store_states<SR>(dAp + (job0 * a.I + ic) * a.S + row * SR, have, dA);
-    dDv += __shfl_xor(dDv, 16);
-    dDv += __shfl_xor(dDv, 32);
-    dbv += __shfl_xor(dbv, 16);
-    dbv += __shfl_xor(dbv, 32);
+    dDs += __shfl_xor(dDs, 16);
+    dDs += __shfl_xor(dDs, 32);
+    dbs += __shfl_xor(dbs, 16);
+    dbs += __shfl_xor(dbs, 32);
     if (row == 0 && has) {
-        dDp[(job0 * a.I + i) * 2] = dDv;
-        dDp[(job0 * a.I + i) * 2 + 1] = dbv;
+        dDp[(job0 * a.I + i) * 2] = (float)dDs;
+        dDp[(job0 * a.I + i) * 2 + 1] = (float)dbs;
     }
 }
 

@@ -265,3 +265,11 @@ def test_adamw_form():
         new, _, m, v = R.adamw(ours, g * t, m, v, t, 1e-2, (0.9, 0.99), 1e-6, 0.02)
         ours = new.float()
     assert (ours - want.detach()).abs().max() <= 1e-6
+
+
+def test_group_norm_of_more_groups_than_a_launch(lib):
+    """A workgroup for each group: there are no more than a launch has."""
+    many = dict(N=1 << 20, V=2, C=2048, G=2048)
+    assert gn_fwd(lib, **many) == -2 and gn_bwd(lib, **many) == -2
+    assert P.pyramid_group_norm_workspace_size(1 << 20, 2, 2048, 2048) == 0
+    assert P.pyramid_group_norm_workspace_size(1 << 20, 2, 2048, 1024) > 0

@@ -556,3 +556,35 @@ def test_giant_update():
             rc, rs = R.narrow(x, E, half)
             assert torch.equal(codes[at:at + e].cpu(), rc)
             assert torch.equal(scales[at // 256:at // 256 + rs.numel()].cpu(), rs)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+def test_growing_states(reverse):
+    """States that grow by exp(96) within a chunk, from 0 and from 1e-30: products that a chunk's growth alone would leave the
+    range of."""
+    B, T, I, S = 1, 192, 3, 4
+    u, Bm, Cm = (rand(k, (B, T, I if k == 1 else S), F32) for k in (1, 2, 3))
+    first = slice(64, None) if reverse else slice(0, 128)
+    u[:, first] = 0.0                   # nothing grows but h0 and what goes back to it
+    delta = torch.full((B, T, I), 0.01)
+    grow = slice(128, None) if reverse else slice(0, 64)
+    delta[:, grow] = 1.5
+    A = torch.ones((I, S))
+    h0 = torch.full((B, I, S), 1e-30)
+    h0[:, 1] = 0.0
+    dy = rand(4, (B, T, I), F32, 1e-30)
+    ref = R.Select(u, delta, A, Bm, Cm, reverse=reverse, h0=h0)
+    grads = ref.backward(dy)
+    dev = [t.to(DEV) for t in (u, delta, A, Bm, Cm)]
+    y, hT = Out((B, T, I), F32), Out((B, I, S), F32)
+    saved = torch.empty(P.pyramid_selective_scan_saved_size(B, T, I, S), dtype=torch.uint8, device=DEV)
+    say("growing states", reverse)
+    P.pyramid_selective_scan_forward(*dev, y.t, reverse=reverse, h0=h0.to(DEV), hT=hT.t, saved=saved)
+    o = dict(du=Out((B, T, I), F32), ddelta=Out((B, T, I), F32), dA=Out((I, S), F32), dB=Out((B, T, S), F32), dC=Out((B, T, S), F32),
+             dh0=Out((B, I, S), F32))
+    P.pyramid_selective_scan_backward(*dev, saved, dy.to(DEV), reverse=reverse, **{k: v.t for k, v in o.items()})
+    near("y", y.get(), ref.y, rounded(ref.y, ref.ey, F32))
+    near("hT", hT.get(), ref.hT, ref.ehT)
+    assert ref.hT.abs().max() < 1e20 and all(torch.isfinite(v).all() for v, _ in grads.values())
+    for k, out in o.items():
+        near(k, out.get(), grads[k][0], rounded(*grads[k], F32))
