@@ -1025,8 +1025,10 @@ int check_sel(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype)
     return PLSTM_OK;
 }
 
-// Waves that fill the card, and the fewest positions of a chunk.
-constexpr long long kSelFill = 2048, kSelChunk = 64;
+// Waves that fill the card, and the fewest positions of a chunk.  bf16, forward (and backward): 1 x 16384 x 1024 144 us with 4096 waves, 150
+// with 2048, 185 with 1024; 2 x 4096 x 2048 499, 515, 593 (3072 leave a part of the card idle: 547).  1 x 1024 x 512 in chunks of
+// 32 positions 66 us, of 64 90, of 128 147, of 16 65.
+constexpr long long kSelFill = 4096, kSelChunk = 32;
 
 struct SelPlan {
     SelArgs a;                          // of the forward and the folds
@@ -1051,8 +1053,7 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     a.lengths = lengths;
     const long long lanes = (I + p.CL - 1) / p.CL;
     p.NB = p.CL == 1 || lanes > 8 ? 1 : lanes > 4 ? 2 : 4;
-    // sequences that share a wave are within 32-bit offsets of each other (wide pitches: fewer chunks and jobs, never
-    // more workspace than the dense rows of workspace_size())
+    // sequences that share a wave are within 32-bit offsets of each other
     const long long widest = std::max({a.pu, a.pd, a.pz, a.pB, a.pC});
     if (T > (1LL << 28) / widest / p.NB) p.NB = 1;
     a.tiles = (lanes + 15) / 16;
@@ -1247,7 +1248,11 @@ size_t pyramid_selective_scan_saved_size(int64_t B, int64_t T, int64_t I, int32_
 size_t pyramid_selective_scan_workspace_size(int64_t B, int64_t T, int64_t I, int32_t S, int32_t backward)
 {
     if (check_sel(B, T, I, S, PLSTM_F32) != PLSTM_OK || (backward != 0 && backward != 1)) return 0;
-    return sel_plan(B, T, I, S, 0, 0, 0, 0, 0, 0, 0, nullptr, nullptr, backward != 0).ws;
+    // of rows as near and as far apart as they may be: whether sequences share waves decides the chunks
+    size_t most = 0;
+    for (long long pitch : {0LL, kSelMaxPitch})
+        most = std::max(most, sel_plan(B, T, I, S, 0, 0, pitch, pitch, 0, 0, 0, nullptr, nullptr, backward != 0).ws);
+    return most;
 }
 
 int pyramid_selective_scan_forward(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype,

@@ -588,3 +588,27 @@ def test_growing_states(reverse):
     assert ref.hT.abs().max() < 1e20 and all(torch.isfinite(v).all() for v, _ in grads.values())
     for k, out in o.items():
         near(k, out.get(), grads[k][0], rounded(*grads[k], F32))
+
+
+def test_far_rows_of_long_sequences():
+    """Sequences that would share waves but for the pitch of their rows, in other chunks then, with the workspace that is
+    asked for: forward and backward."""
+    B, T, I, S, far = 5, 44000, 3, 1, 1600
+    u, delta, dy = rand(1, (B, T, I), F32), rand(2, (B, T, I), F32).abs() * 0.1, rand(3, (B, T, I), F32)
+    Bm, Cm = rand(4, (B, T, S), F32), rand(5, (B, T, S), F32)
+    A = -torch.exp(rand(6, (I, S), F32, 0.5))
+    ref = R.Select(u, delta, A, Bm, Cm)
+    grads = ref.backward(dy)
+    rows = torch.empty((B, T, far), device=DEV)
+    ud = rows[..., 100:100 + I]
+    ud.copy_(u)
+    dev = [t.to(DEV) for t in (delta, A, Bm, Cm)]
+    say("far rows of long sequences")
+    ws = [torch.empty(P.pyramid_selective_scan_workspace_size(B, T, I, S, k), dtype=torch.uint8, device=DEV) for k in (0, 1)]
+    y, saved = Out((B, T, I), F32), torch.empty(P.pyramid_selective_scan_saved_size(B, T, I, S), dtype=torch.uint8, device=DEV)
+    P.pyramid_selective_scan_forward(ud, *dev, y.t, saved=saved, ws=ws[0])
+    o = dict(du=Out((B, T, I), F32), ddelta=Out((B, T, I), F32), dA=Out((I, S), F32), dB=Out((B, T, S), F32), dC=Out((B, T, S), F32))
+    P.pyramid_selective_scan_backward(ud, *dev, saved, dy.to(DEV), ws=ws[1], **{k: v.t for k, v in o.items()})
+    near("y", y.get(), ref.y, rounded(ref.y, ref.ey, F32))
+    for k, out in o.items():
+        near(k, out.get(), grads[k][0], rounded(*grads[k], F32))
