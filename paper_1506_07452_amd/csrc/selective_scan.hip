@@ -12,6 +12,11 @@
 // over the states comes out in, and passes to the other rows through LDS.
 // Few channels and long sequences do not fill the card: a sequence is then cut into chunks whose
 // folds (last state = exp(A sum d) h + H) are made first and chained by a small launch.
+// Bound by the issue of vector instructions, not by bytes: a state and position take an exponential (the time of 3.2 products),
+// 4 products in the forward, 3 in a fold; the backward 29 instructions (11 for the formulas, half of the states again, 5.5 for
+// the sums over channels, 3 a state for what belongs to an element).  16 states, bf16, 2 x 4096 x 2048: forward 76 us (its bytes
+// 26), folds 51 and 59, backward 289 (bytes 46), the vector units busy 80 to 87%.  The whole MR volume along x (11520 x 240 x 16
+// fp32), no folds: forward 231 us, at the rate of its bytes; backward 738.
 #include <algorithm>
 
 #include "sequence.h"
@@ -26,7 +31,8 @@ constexpr int kSelStage = 8;            // positions that a forward wave stages 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 inline int sel_sr(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
-// Channels of a lane in the forward and the folds.
+// Channels of a lane in the forward and the folds: two share the rows of B and C that a lane reads (2 x 4096 x 2048 515 us, with one
+// 550; 1 x 16384 x 1024 150, 163; sequences too short to fill the card lose by it, 1 x 1024 x 512 90, 78).
 __host__ __device__ constexpr int sel_cl(int SR) { return SR <= 4 ? 2 : 1; }
 
 struct SelArgs {
@@ -681,7 +687,8 @@ k_sel_step(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, c
     }
 }
 
-// Positions of a run of the backward, whose decays and states a lane has in registers.
+// Positions of a run of the backward, whose decays and states a lane has in registers: half of the states are made twice with 8
+// of them, three quarters with 4 (2 x 4096 x 2048, 16 states: 310 us, 355).
 __host__ __device__ constexpr int sel_run(int SR) { return SR <= 4 ? 8 : 4; }
 
 template <int SR>
@@ -699,6 +706,7 @@ struct alignas(16) BackShared {
 // then run by run, from the last on, the states in it and back.  WIDE: the waves of a workgroup have neighbouring channels of
 // the same chunk and add up their dB and dC; else each has the only 16 channels of a sequence of its own.
 // dBp, dCp [group of channels][b][t][S] (one group: dB and dC themselves); dAp [job][I][S], dDp [job][I][2].
+// Two waves a SIMD; 16 states a lane have the registers of one (64 states, 2 x 2048 x 2048 bf16: 785 us, with two and spills 1202).
 template <typename T, int SR, bool WIDE>
 __global__ void __launch_bounds__(256, SR <= 8 ? 2 : 1)
 k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, const T *Cm, const float *D, const T *z,
@@ -1052,6 +1060,7 @@ SelPlan sel_plan(int64_t B, int64_t T, int64_t I, int32_t S, int32_t reverse, in
     a.pu = pu ? pu : I; a.pd = pd ? pd : I; a.pz = pz ? pz : I; a.pB = pB ? pB : S; a.pC = pC ? pC : S;
     a.lengths = lengths;
     const long long lanes = (I + p.CL - 1) / p.CL;
+    // few channels: sequences share a wave (11520 x 240 x 16 forward and backward 981 us, one a wave 1073)
     p.NB = p.CL == 1 || lanes > 8 ? 1 : lanes > 4 ? 2 : 4;
     // sequences that share a wave are within 32-bit offsets of each other
     const long long widest = std::max({a.pu, a.pd, a.pz, a.pB, a.pC});
@@ -1179,6 +1188,7 @@ int sel_backward(const SelPlan &p, const SelTensors &t, hipStream_t st)
         k_sel_weights<L><<<blocks, 16 * L, 0, st>>>(nA, a.I, (int)a.jobs, p.dAp, p.dDp, (float *)t.dA, (float *)t.dD,
                                                     (float *)t.db);
     };
+    // 3840 parts of 16 x 16 outputs: 64 lanes each 14.6 us, 16 lanes 19.0; 64 parts of 2048 x 16: 8.8, 5.0
     if (a.jobs > 128) weights(std::integral_constant<int, 64>());
     else weights(std::integral_constant<int, 16>());
     PLSTM_LAUNCH_CHECK();

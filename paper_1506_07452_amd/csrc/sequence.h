@@ -39,7 +39,9 @@ __device__ inline float silu_slope(float a, float &silu)
 }
 
 // Pieces of tensors too large for the caches: read for the last time, or written for a later launch.  Non-temporal accesses
-// leave the caches to what is read twice, and no written lines behind that the next launch waits to have written back.
+// leave the caches to what is read twice, and no written lines behind that the next launch waits to have written back: group norm of
+// 1 x 2764800 x 16 fp32 248 us, without 297, of 8 x 262144 x 64 bf16 388, 454; the convolution of 2 x 8192 x 2048 92, 96;
+// AdamW of 66 million elements 329, 345.  Smaller ones make no difference here and may be in a cache for their reader.
 constexpr long long kStreamBytes = 64LL << 20;      // of a tensor, from which on it is accessed so
 template <bool STREAM, typename T>
 __device__ inline u32x4 load_last(const T *p, int have)
