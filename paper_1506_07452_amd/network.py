@@ -247,6 +247,8 @@ def _lines(x, axis):
 
 def _unlines(t, shape, axis):
     """The volume [N][D][H][W][n] of _lines' output for a volume of `shape`."""
+    if t is None:
+        return None
     N, D, H, W = shape[:4]
     if axis == "z":
         return t.view(N, H, W, D, -1).movedim(3, 1).contiguous()
@@ -283,7 +285,7 @@ def group_norm_backward(dy, kept, gamma, beta, want_dx: bool = True, ws=None, st
 def selective_forward(u, delta, z, Bm, Cm, p, axis: str, reverse: bool = False, training: bool = False,
                       ws=None, stream=None):
     """Selective sweep of a volume: a causal convolution with SiLU of u, then a selective scan of it gated
-    by z, along the lines of `axis` ("z", "y" or "x", "zyx": all voxels in raster order;
+    by z (or None), along the lines of `axis` ("z", "y" or "x", "zyx": all voxels in raster order;
     from the far side with `reverse`).  u, delta, z [N][D][H][W][I], Bm, Cm [N][D][H][W][S]; p: a dict
     of conv_w [I][K], conv_b [I] in their dtype and A [I][S], D, delta_bias [I] fp32.
     Returns (y, kept): kept is None for inference, else what selective_backward needs."""
@@ -302,11 +304,12 @@ def selective_forward(u, delta, z, Bm, Cm, p, axis: str, reverse: bool = False, 
 
 @_on_its_stream
 def selective_backward(dy, kept, p, ws=None, stream=None):
-    """Gradients of selective_forward: a dict of u, delta, z, Bm, Cm (volumes) and conv_w,
-    conv_b, A, D, delta_bias (fp32)."""
+    """Gradients of selective_forward: a dict of u, delta, z (None without it), Bm, Cm (volumes)
+    and conv_w, conv_b, A, D, delta_bias (fp32)."""
     u, v, delta, z, Bm, Cm, saved, axis, reverse = kept
     shape, dy = dy.shape, _lines(dy, axis)
-    g = {k: torch.empty_like(t) for k, t in (("v", v), ("delta", delta), ("z", z), ("Bm", Bm), ("Cm", Cm), ("u", u))}
+    g = {k: None if t is None else torch.empty_like(t)
+         for k, t in (("v", v), ("delta", delta), ("z", z), ("Bm", Bm), ("Cm", Cm), ("u", u))}
     for k in ("conv_w", "conv_b", "A", "D", "delta_bias"):
         g[k] = torch.empty_like(p[k], dtype=torch.float32)
     pyramid_selective_scan_backward(v, delta, p["A"], Bm, Cm, saved, dy, g["v"], g["delta"], g["A"], g["Bm"],

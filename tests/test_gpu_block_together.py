@@ -612,3 +612,78 @@ def test_far_rows_of_long_sequences():
     near("y", y.get(), ref.y, rounded(ref.y, ref.ey, F32))
     for k, out in o.items():
         near(k, out.get(), grads[k][0], rounded(*grads[k], F32))
+
+
+@DTYPES
+@pytest.mark.parametrize("axis", ["z", "y", "x", "zyx"])
+def test_sweep_without_a_gate(axis, dtype):
+    """A volume's selective sweep without z is the operators on its lines, forward and backward."""
+    N, D, H, W, I, S = 2, 3, 4, 37, 10, 6
+    u, delta = rand(1, (N, D, H, W, I), dtype).to(DEV), rand(2, (N, D, H, W, I), dtype, 0.5, -2.0).to(DEV)
+    Bm, Cm = (rand(k, (N, D, H, W, S), dtype).to(DEV) for k in (3, 4))
+    dy = rand(5, (N, D, H, W, I), dtype).to(DEV)
+    p = dict(conv_w=rand(6, (I, 3), dtype, 0.5).to(DEV), conv_b=rand(7, (I,), dtype).to(DEV), A=-torch.exp(rand(8, (I, S), F32)).to(DEV),
+             D=rand(9, (I,), F32).to(DEV), delta_bias=rand(10, (I,), F32).to(DEV))
+    say("sweep without a gate", axis, dtype)
+    y, kept = net.selective_forward(u, delta, None, Bm, Cm, p, axis, True, training=True)
+    g = net.selective_backward(dy, kept, p)
+    assert g["z"] is None
+    order = {"z": (0, 2, 3, 1, 4), "y": (0, 1, 3, 2, 4), "x": (0, 1, 2, 3, 4), "zyx": (0, 1, 2, 3, 4)}[axis]
+    back = [order.index(k) for k in range(5)]
+    T = {"z": D, "y": H, "x": W, "zyx": D * H * W}[axis]
+
+    def lines(t):
+        return t.permute(order).reshape(-1, T, t.shape[-1]).contiguous()
+
+    def volume(t):
+        return t.view([(N, D, H, W)[k] for k in order[:4]] + [t.shape[-1]]).permute(back)
+
+    ul, dl, Bl, Cl = (lines(t) for t in (u, delta, Bm, Cm))
+    v, yl = torch.empty_like(ul), torch.empty_like(ul)
+    P.pyramid_causal_conv_forward(ul, p["conv_w"], p["conv_b"], v, act="silu", reverse=True)
+    saved = torch.empty(P.pyramid_selective_scan_saved_size(*ul.shape, S), dtype=torch.uint8, device=DEV)
+    P.pyramid_selective_scan_forward(v, dl, p["A"], Bl, Cl, yl, p["D"], None, p["delta_bias"], True, True, saved=saved)
+    assert torch.equal(volume(yl), y)
+    dv, dd, dB, dC = (torch.empty_like(t) for t in (ul, dl, Bl, Cl))
+    dA, dD, db = (torch.empty_like(p[k]) for k in ("A", "D", "delta_bias"))
+    P.pyramid_selective_scan_backward(v, dl, p["A"], Bl, Cl, saved, lines(dy), dv, dd, dA, dB, dC, p["D"], None, p["delta_bias"], True,
+                                      dD, None, db, True)
+    for k, t in (("delta", dd), ("Bm", dB), ("Cm", dC)):
+        assert torch.equal(volume(t), g[k]), k
+    for k, t in (("A", dA), ("D", dD), ("delta_bias", db)):
+        assert torch.equal(t, g[k]), k
+
+
+@DTYPES
+def test_large_workgroups_in_a_graph(dtype):
+    """Kernels that ask for more LDS than a launch has by itself (many states, a held volume of many channels), captured
+    before they have run elsewhere in other forms, replayed."""
+    B, T, I, S = 2, 100, 40, 40
+    u, delta, dy = rand(1, (B, T, I), dtype).to(DEV), rand(2, (B, T, I), dtype, 0.5, -2.0).to(DEV), rand(3, (B, T, I), dtype).to(DEV)
+    Bm, Cm = (rand(k, (B, T, S), dtype).to(DEV) for k in (4, 5))
+    A = -torch.exp(rand(6, (I, S), F32)).to(DEV)
+    x, gamma = rand(7, (3, 2, 2048), dtype).to(DEV), rand(8, (2048,), dtype, 0.2, 1.0).to(DEV)
+
+    def go():
+        y, saved = torch.empty_like(u), torch.empty(P.pyramid_selective_scan_saved_size(B, T, I, S), dtype=torch.uint8, device=DEV)
+        P.pyramid_selective_scan_forward(u, delta, A, Bm, Cm, y, softplus=True, saved=saved)
+        g = [torch.empty_like(t) for t in (u, delta, A, Bm, Cm)]
+        P.pyramid_selective_scan_backward(u, delta, A, Bm, Cm, saved, dy, *g, softplus=True)
+        z, stats, dx = torch.empty_like(x), torch.empty((3, 16, 2), device=DEV), torch.empty_like(x)
+        dg, db = torch.empty(2048, device=DEV), torch.empty(2048, device=DEV)
+        P.pyramid_group_norm_forward(x, gamma, gamma, z, 16, "silu", stats)
+        P.pyramid_group_norm_backward(x, gamma, gamma, stats, z, dx, dg, db, 16, "silu")
+        return [y] + g + [z, dx, dg, db]
+
+    say("large workgroups in a graph", dtype)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = go()
+    for _ in range(3):
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        want = go()
+        torch.cuda.synchronize()
+        same(got, want)
