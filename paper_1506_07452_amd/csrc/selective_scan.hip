@@ -1034,7 +1034,7 @@ int check_sel(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype)
 }
 
 // Waves that fill the card, and the fewest positions of a chunk.  bf16, forward (and backward): 1 x 16384 x 1024 144 us with 4096 waves, 150
-// with 2048, 185 with 1024; 2 x 4096 x 2048 499, 515, 593 (3072 leave a part of the card idle: 547).  1 x 1024 x 512 in chunks of
+// with 2048, 185 with 1024; 2 x 4096 x 2048 499, 515, 593.  1 x 1024 x 512 in chunks of
 // 32 positions 66 us, of 64 90, of 128 147, of 16 65.
 constexpr long long kSelFill = 4096, kSelChunk = 32;
 
