@@ -7,6 +7,8 @@ HIP kernels); gradients flow through the same entry points in reverse.
 Beyond Fig. 3 a layer's output may be normed over its channels before its FC
 (`norms`), and a training step may hold what the layers keep for their
 backward in 8 bits (`checkpoint8`).
+Group norm and selective sweeps along the lines of a volume, the blocks of state
+space models over volumes, stand beside them.
 """
 from __future__ import annotations
 

@@ -12,6 +12,7 @@ from tests import block_ref as R
 from tests.gpu_util import DEV, TOL, host, normwise, say
 from tests.seq_ref import rounded
 from tests.test_gpu_block import poisoned, sliced
+from tests.test_gpu_network_norm import case
 from tests.test_gpu_sequence import BF16, DTYPES, F32, Out, near, rand
 from tests.test_gpu_streams import beside_busy_stream, same
 
@@ -687,3 +688,25 @@ def test_large_workgroups_in_a_graph(dtype):
         want = go()
         torch.cuda.synchronize()
         same(got, want)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_network_updates(bits):
+    """A normed network's parameters and gradients through AdamW, decay for the weights only."""
+    d, _ = case([16, 32], True, 61, (1, 0))
+    params = net.network_parameters(d["layers"], d["fcs"], d["head"], d["norms"])
+    decay = [0.05 if p.dim() > 1 else 0.0 for p in params]
+    opt = P.AdamW(params, lr=1e-3, weight_decay=decay, bits=bits, seed=4)
+    m, v = ([torch.zeros(p.shape) for p in params] for _ in range(2))
+    say("network updates", bits)
+    for t in (1, 2):
+        grads = net.network_gradients(net.network_train_step(d["x"], d["layers"], d["fcs"], d["head"], d["labels"], norms=d["norms"]))
+        before = [p.cpu() for p in params]
+        opt.step(grads)
+        for k, (p, g) in enumerate(zip(params, grads)):
+            new, bound, m[k], v[k] = R.adamw(before[k], g.cpu(), m[k], v[k], t, 1e-3, (0.9, 0.999), 1e-8, decay[k])
+            near("p", p.cpu(), new, bound + 2.0 ** -23 * 1e-3 * 4)
+        if bits == 8:
+            m, v = ([x[j].cpu() for x in opt.moments()] for j in (0, 1))
+        else:
+            assert all(torch.equal(a.cpu(), b) for a, b in zip(opt.m + opt.v, m + v))
