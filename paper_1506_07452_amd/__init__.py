@@ -1146,7 +1146,7 @@ class AdamW:
         for seg, p, shape in zip(self._segs, self.params, self._shapes):
             if p.data_ptr() != seg.theta:       # the tensor was given other memory
                 seg.theta = _tensor("params", p, shape, torch.float32, self._dev)
-        dtype = _adamw_grads(self._segs, self._shapes, grads, self._dev)
+        dtype = _adamw_grads(self._segs, self._shapes, list(grads), self._dev)
         _adamw_run(self._segs, self.bits, dtype, self._dev, stream, self.lr if lr is None else lr,
                    self.betas, self.eps, self._t + 1, self.seed, self._clock, grad_scale)
         self._t += 1
