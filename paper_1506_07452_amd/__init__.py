@@ -1051,7 +1051,7 @@ def _adamw_grads(segs, shapes, grads, dev):
             if dtype not in _DT:
                 raise ValueError("gradients must be float32 or bfloat16")
         seg.grad = _tensor("grads", g, shape, dtype, dev)
-        seg.n = g.numel()
+        seg.n = shape.numel()
     return PLSTM_F32 if dtype is None else _DT[dtype]
 
 
@@ -1124,6 +1124,7 @@ class AdamW:
         if got != bits:
             raise ValueError("state has moments in %d bits" % got)
         self._shapes = [p.shape for p in self.params]
+        self._rows, self._at = list(self._segs), [p.data_ptr() for p in self.params]
         self._t, self._clock = t, None
         if capturable:
             self._clock = torch.tensor([t, 0, 0], dtype=torch.int64, device=self.params[0].device)
@@ -1143,10 +1144,10 @@ class AdamW:
     def step(self, grads, lr=None, grad_scale=None, stream=None):
         """One update from `grads` (one per parameter, None to leave it alone); lr and
         grad_scale as in pyramid_adamw_step."""
-        for seg, p, shape in zip(self._segs, self.params, self._shapes):
-            if p.data_ptr() != seg.theta:       # the tensor was given other memory
-                seg.theta = _tensor("params", p, shape, torch.float32, self._dev)
-        dtype = _adamw_grads(self._segs, self._shapes, list(grads), self._dev)
+        for k, p in enumerate(self.params):
+            if p.data_ptr() != self._at[k]:     # the tensor was given other memory
+                self._rows[k].theta = self._at[k] = _tensor("params", p, self._shapes[k], torch.float32, self._dev)
+        dtype = _adamw_grads(self._rows, self._shapes, list(grads), self._dev)
         _adamw_run(self._segs, self.bits, dtype, self._dev, stream, self.lr if lr is None else lr,
                    self.betas, self.eps, self._t + 1, self.seed, self._clock, grad_scale)
         self._t += 1
