@@ -823,6 +823,8 @@ def _main_pitched(name, t):
     dev = t.get_device()
     if dev < 0:
         raise ValueError("%s must live on the GPU" % name)
+    if t.is_contiguous():
+        return code, dev, t.data_ptr(), 0
     return (code, dev) + _pitched(name, t, t.shape, t.dtype, dev)
 
 
@@ -963,12 +965,14 @@ def _volumes(name, x):
 
 
 def _group_norm_ws(ws, N, V, C, G, x, dev, stream):
+    """`ws`, or one made with torch (the caller holds it until its call is under way), its pointer and its bytes."""
     if ws is None:
         need = pyramid_group_norm_workspace_size(N, V, C, G)
         if need <= 256:
-            return _shared_ws(x, dev)[1:]
+            return _shared_ws(x, dev)
         ws = _temporary(need, x.device, stream)
-    return _bytes(ws, dev)
+        return ws, ws.data_ptr(), need
+    return (ws,) + _bytes(ws, dev)
 
 
 def pyramid_group_norm_forward(x, gamma, beta, y, groups, act="none", stats=None, eps=1e-5, ws=None,
@@ -977,11 +981,12 @@ def pyramid_group_norm_forward(x, gamma, beta, y, groups, act="none", stats=None
     [N][...][C], times gamma plus beta [C], act ("none" or "silu") of it into y; one dtype.
     stats [N][groups][2] fp32 takes (mean, rstd) for the backward."""
     dt, px, dev, N, V, C = _volumes("x", x)
+    ws, pw, bw = _group_norm_ws(ws, N, V, C, groups, x, dev, stream)
     _run("pyramid_group_norm_forward", dev, stream, N, V, C, groups, dt, _act(act), eps, px,
          _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
          _tensor("y", y, x.shape, x.dtype, dev),
          _tensor("stats", stats, (N, groups, 2), torch.float32, dev),
-         *_group_norm_ws(ws, N, V, C, groups, x, dev, stream))
+         pw, bw)
 
 
 def pyramid_group_norm_backward(x, gamma, beta, stats, dy, dx, dgamma, dbeta, groups, act="none",
@@ -989,13 +994,14 @@ def pyramid_group_norm_backward(x, gamma, beta, stats, dy, dx, dgamma, dbeta, gr
     """Gradients of pyramid_group_norm_forward: dx (or None) of x's shape, dgamma and dbeta [C]
     fp32, from dy, the forward's inputs and its stats."""
     dt, px, dev, N, V, C = _volumes("x", x)
+    ws, pw, bw = _group_norm_ws(ws, N, V, C, groups, x, dev, stream)
     _run("pyramid_group_norm_backward", dev, stream, N, V, C, groups, dt, _act(act), px,
          _tensor("gamma", gamma, (C,), x.dtype, dev), _tensor("beta", beta, (C,), x.dtype, dev),
          _tensor("stats", stats, (N, groups, 2), torch.float32, dev),
          _tensor("dy", dy, x.shape, x.dtype, dev), _tensor("dx", dx, x.shape, x.dtype, dev),
          _tensor("dgamma", dgamma, (C,), torch.float32, dev),
          _tensor("dbeta", dbeta, (C,), torch.float32, dev),
-         *_group_norm_ws(ws, N, V, C, groups, x, dev, stream))
+         pw, bw)
 
 
 def pyramid_adamw_scales(n: int) -> int:

@@ -3,6 +3,8 @@ them against 64-bit automatic differentiation, in captured graphs, on other stre
 the current one, two calls at once, and past 2^31 and 2^32 elements."""
 from __future__ import annotations
 
+import weakref
+
 import pytest
 import torch
 
@@ -710,3 +712,27 @@ def test_network_updates(bits):
             m, v = ([x[j].cpu() for x in opt.moments()] for j in (0, 1))
         else:
             assert all(torch.equal(a.cpu(), b) for a, b in zip(opt.m + opt.v, m + v))
+
+
+@pytest.mark.parametrize("name", ["conv_backward", "scan_forward", "scan_backward", "norm_forward", "norm_backward"])
+def test_workspace_lives_through_the_call(name, monkeypatch):
+    """A workspace that the binding makes is not given back before its call has been made."""
+    call, _ = entry_points(F32)[name]
+    made, seen, run = [], [], P._run
+    temporary = P._temporary
+
+    def tracked(*args):
+        ws = temporary(*args)
+        made.append(weakref.ref(ws))
+        return ws
+
+    def watched(*args):
+        seen.extend(ref() is not None for ref in made)
+        run(*args)
+
+    monkeypatch.setattr(P, "_temporary", tracked)
+    monkeypatch.setattr(P, "_run", watched)
+    say("workspace through the call", name)
+    call(None)
+    torch.cuda.synchronize()
+    assert seen == [True]
