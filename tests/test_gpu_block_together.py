@@ -736,3 +736,36 @@ def test_workspace_lives_through_the_call(name, monkeypatch):
     call(None)
     torch.cuda.synchronize()
     assert seen == [True]
+
+
+@DTYPES
+@pytest.mark.parametrize("T", [2, 5, 100, 700])
+def test_conv_state_in_place_of_runs(T, dtype):
+    """The state after in the place of the one before, where a sequence has several runs and where it is shorter than the taps."""
+    B, I, K = 3, 21, 8
+    x, w, b = rand(1, (B, T, I), dtype).to(DEV), rand(2, (I, K), dtype, 0.5).to(DEV), rand(3, (I,), dtype).to(DEV)
+    lengths = torch.tensor([T, 0, T // 2], dtype=torch.int32, device=DEV)
+    before = rand(4, (B, K - 1, I), dtype).to(DEV)
+    after, y, there = torch.empty_like(before), torch.empty_like(x), torch.empty_like(x)
+    say("convolution's state in place", T, dtype)
+    for reverse in (False, True):
+        how = dict(act="silu", reverse=reverse, lengths=lengths)
+        P.pyramid_causal_conv_forward(x, w, b, y, state=before, state_out=after, **how)
+        state = before.clone()
+        P.pyramid_causal_conv_forward(x, w, b, there, state=state, state_out=state, **how)
+        assert torch.equal(there, y) and torch.equal(state, after)
+
+
+def test_counted_updates_without_gradients():
+    """A counted update of tensors of which some, or all, have no gradient: the count goes on, those tensors stay."""
+    p = [rand(k, (300,), F32).to(DEV) for k in (1, 2)]
+    g = rand(3, (300,), F32).to(DEV)
+    kept = [t.clone() for t in p]
+    opt = P.AdamW(p, lr=1e-2, capturable=True)
+    opt.step([None, None])
+    opt.step([None, g])
+    say("counted updates")
+    assert opt.t == 2 and torch.equal(p[0], kept[0])
+    new, bound, m, v = R.adamw(kept[1].cpu(), g.cpu(), torch.zeros(300), torch.zeros(300), 2, 1e-2, (0.9, 0.999), 1e-8, 0.01)
+    near("p", p[1].cpu(), new, bound + 2.0 ** -23 * 1e-2 * 4)
+    assert torch.equal(opt.m[1].cpu(), m) and torch.equal(opt.v[1].cpu(), v) and not opt.m[0].any()
