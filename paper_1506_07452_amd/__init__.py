@@ -1008,6 +1008,9 @@ def pyramid_adamw_scales(n: int) -> int:
     return int(load().pyramid_adamw_scales(n))
 
 
+_data_ptr = torch.Tensor.data_ptr
+
+
 def _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay):
     """Segments of an AdamW call without its gradients, the bits of its moments and its device."""
     count = len(params)
@@ -1056,8 +1059,11 @@ def _adamw_grads(segs, shapes, grads, dev):
             dtype = g.dtype
             if dtype not in _DT:
                 raise ValueError("gradients must be float32 or bfloat16")
-        seg.grad = _tensor("grads", g, shape, dtype, dev)
-        seg.n = shape.numel()
+        # _tensor's questions without its call (12 tensors 1 us of 13)
+        seg.grad = (g.data_ptr() if g.shape == shape and g.dtype == dtype and g.get_device() == dev and g.is_contiguous()
+                    else _tensor("grads", g, shape, dtype, dev))
+        if not seg.n:                   # left alone before
+            seg.n = shape.numel()
     return PLSTM_F32 if dtype is None else _DT[dtype]
 
 
@@ -1066,8 +1072,8 @@ def _adamw_run(segs, bits, grad_dtype, dev, stream, lr, betas, eps, step, seed, 
     if isinstance(lr, torch.Tensor):
         lr, lr_dev = 0.0, _tensor("lr", lr, (1,), torch.float32, dev)
     _run("pyramid_adamw_step", dev, stream, len(segs), segs, bits, grad_dtype, lr, betas[0], betas[1],
-         eps, step, seed & 0xffffffff, _tensor("clock", clock, (3,), torch.int64, dev), lr_dev,
-         _tensor("grad_scale", grad_scale, (1,), torch.float32, dev))
+         eps, step, seed & 0xffffffff, None if clock is None else _tensor("clock", clock, (3,), torch.int64, dev), lr_dev,
+         None if grad_scale is None else _tensor("grad_scale", grad_scale, (1,), torch.float32, dev))
 
 
 def pyramid_adamw_step(params, grads, m, v, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
@@ -1103,7 +1109,10 @@ class AdamW:
     bits or in 8 (`bits`), zero at first or taken from `state` (what state() gives).
     copies: bf16 tensors (or None each) that take the updated parameters.
     weight_decay: a number or one per tensor.  capturable=True keeps the number of updates on
-    the device, so that a step captured in a graph goes on counting when it is replayed."""
+    the device, so that a step captured in a graph goes on counting when it is replayed.
+    An update works on the memory that params and copies have when it is called (a captured one on
+    that of its capture).  The moments' memory, m and v (with 8 bits their codes, and the scales mscale and
+    vscale), is the optimiser's from first to last: to go on from others, give them as `state`."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32,
                  copies=None, seed=0, state=None, capturable=False):
@@ -1112,28 +1121,57 @@ class AdamW:
         self.params = list(params)
         self.lr, self.betas, self.eps, self.seed, self.bits = lr, betas, eps, seed, bits
         self.copies = None if copies is None else list(copies)
-        self.mscale = self.vscale = None
+        ms = vs = None
         if state is None:
             dt = torch.float32 if bits == 32 else torch.uint8
-            self.m, self.v = ([torch.zeros_like(p, dtype=dt, memory_format=torch.contiguous_format)
-                               for p in self.params] for _ in range(2))
+            m, v = ([torch.zeros_like(p, dtype=dt, memory_format=torch.contiguous_format)
+                     for p in self.params] for _ in range(2))
             if bits == 8:
-                self.mscale, self.vscale = ([torch.zeros(-(-p.numel() // 256), device=p.device)
-                                             for p in self.params] for _ in range(2))
+                ms, vs = ([torch.zeros(-(-p.numel() // 256), device=p.device)
+                           for p in self.params] for _ in range(2))
             t = 0
         else:
-            self.m, self.v, t = list(state["m"]), list(state["v"]), int(state["t"])
+            m, v, t = state["m"], state["v"], int(state["t"])
             if bits == 8:
-                self.mscale, self.vscale = list(state["mscale"]), list(state["vscale"])
-        self._segs, got, self._dev = _adamw_segments(self.params, self.m, self.v, self.mscale,
-                                                     self.vscale, self.copies, weight_decay)
-        if got != bits:
-            raise ValueError("state has moments in %d bits" % got)
-        self._shapes = [p.shape for p in self.params]
-        self._rows, self._at = list(self._segs), [p.data_ptr() for p in self.params]
+                ms, vs = state["mscale"], state["vscale"]
+        # tensors of its own over their memory: a caller's may be given other memory
+        self._m, self._v, self._ms, self._vs = (None if ts is None else [t.detach() for t in ts] for ts in (m, v, ms, vs))
+        self._shown = {}
+        self._decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else weight_decay
+        self._renew()
         self._t, self._clock = t, None
         if capturable:
             self._clock = torch.tensor([t, 0, 0], dtype=torch.int64, device=self.params[0].device)
+
+    def _addresses(self):
+        """Where the caller's tensors are that an update writes (0: a copy that is None)."""
+        at = list(map(_data_ptr, self.params))
+        if self.copies is not None:
+            at += [0 if c is None else c.data_ptr() for c in self.copies]
+        return at
+
+    def _renew(self):
+        """Segments of the tensors that are there now."""
+        segs, bits, dev = _adamw_segments(self.params, self._m, self._v, self._ms, self._vs, self.copies, self._decay)
+        if bits != self.bits:
+            raise ValueError("state has moments in %d bits" % bits)
+        self._segs, self._rows, self._dev = segs, list(segs), dev
+        self._shapes, self._at = [p.shape for p in self.params], self._addresses()
+
+    def _show(self, name):
+        """Tensors for others over the moments or scales: new ones where one of them was given other memory."""
+        shown = self._shown.get(name)
+        if shown is None or list(map(_data_ptr, shown[0])) != shown[1]:
+            held = getattr(self, name)
+            if held is None:
+                return None
+            shown = self._shown[name] = tuple(t.detach() for t in held), list(map(_data_ptr, held))
+        return shown[0]
+
+    m = property(lambda self: self._show("_m"))
+    v = property(lambda self: self._show("_v"))
+    mscale = property(lambda self: self._show("_ms"))
+    vscale = property(lambda self: self._show("_vs"))
 
     @property
     def t(self):
@@ -1141,18 +1179,17 @@ class AdamW:
         return self._t if self._clock is None else int(self._clock[0])
 
     def state(self):
-        """The moments, their scales and the number of updates: the tensors themselves."""
-        out = {"m": self.m, "v": self.v, "t": self.t}
+        """The moments, their scales and the number of updates: tensors of the memory itself."""
+        out = {"m": list(self.m), "v": list(self.v), "t": self.t}
         if self.bits == 8:
-            out.update(mscale=self.mscale, vscale=self.vscale)
+            out.update(mscale=list(self.mscale), vscale=list(self.vscale))
         return out
 
     def step(self, grads, lr=None, grad_scale=None, stream=None):
         """One update from `grads` (one per parameter, None to leave it alone); lr and
         grad_scale as in pyramid_adamw_step."""
-        for k, p in enumerate(self.params):
-            if p.data_ptr() != self._at[k]:     # the tensor was given other memory
-                self._rows[k].theta = self._at[k] = _tensor("params", p, self._shapes[k], torch.float32, self._dev)
+        if self._addresses() != self._at:       # a tensor was given other memory, or replaced
+            self._renew()
         dtype = _adamw_grads(self._rows, self._shapes, list(grads), self._dev)
         _adamw_run(self._segs, self.bits, dtype, self._dev, stream, self.lr if lr is None else lr,
                    self.betas, self.eps, self._t + 1, self.seed, self._clock, grad_scale)
@@ -1166,7 +1203,7 @@ class AdamW:
         side = caller if stream is None else _torch_stream(stream, self.params[0].device)
         with torch.cuda.stream(side):
             mout, vout = ([torch.empty(p.shape, device=p.device) for p in self.params] for _ in range(2))
-            pyramid_adamw_moments(self.m, self.v, self.mscale, self.vscale, mout, vout, side)
+            pyramid_adamw_moments(self._m, self._v, self._ms, self._vs, mout, vout, side)
         for out in mout + vout:         # results are the caller's stream's as well
             out.record_stream(caller)
         return list(zip(mout, vout))

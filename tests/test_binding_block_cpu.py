@@ -1,0 +1,124 @@
+"""What the binding of the block operators passes on and refuses, on the CPU: the questions that need a device
+are answered by stand-ins, calls are recorded and not made."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_1506_07452_amd as P
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Host tensors stand for a device's; calls of entry points end up in the list."""
+    made = []
+
+    def main(name, t, dims):
+        assert t.is_contiguous()
+        return P._DT[t.dtype], t.data_ptr(), 0
+
+    def tensor(name, t, shape, dtype, dev):
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError(name)
+        return t.data_ptr()
+
+    def run(name, dev, stream, *args):
+        row = {"name": name, "args": args}
+        if name.startswith("pyramid_adamw"):
+            row["segs"] = [{f: getattr(s, f) for f, _ in P.plstm_adamw_segment._fields_} for s in args[1]]
+        made.append(row)
+
+    monkeypatch.setattr(P, "_main", main)
+    monkeypatch.setattr(P, "_tensor", tensor)
+    monkeypatch.setattr(P, "_run", run)
+    return made
+
+
+SIZES = (300, 17, 256)
+
+
+def optimiser(bits=8, copies=True, **kw):
+    params = [torch.zeros(n) for n in SIZES]
+    return P.AdamW(params, bits=bits, copies=[torch.zeros(n, dtype=BF16) if k != 1 else None for k, n in enumerate(SIZES)] if copies else None,
+                   **kw), [torch.ones(n) for n in SIZES]
+
+
+def addresses(opt):
+    """What an update has to work on: the tensors that the optimiser shows."""
+    rows = []
+    for k, p in enumerate(opt.params):
+        row = dict(theta=p, m=opt.m[k], v=opt.v[k])
+        if opt.bits == 8:
+            row.update(mscale=opt.mscale[k], vscale=opt.vscale[k])
+        if opt.copies is not None and opt.copies[k] is not None:
+            row["copy"] = opt.copies[k]
+        rows.append({f: t.data_ptr() for f, t in row.items()})
+    return rows
+
+
+def follows(opt, grads, calls):
+    calls.clear()
+    opt.step(grads)
+    for row, seg in zip(addresses(opt), calls[0]["segs"]):
+        assert {f: seg[f] for f in row} == row
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_update_follows_its_tensors(bits, calls):
+    """An update works on the parameters and copies that are there now, whichever of them was given other memory or replaced."""
+    opt, grads = optimiser(bits)
+    follows(opt, grads, calls)
+    held = []           # the memory of before stays taken: other memory has other addresses
+    for tensors in (opt.params, opt.copies):
+        held.append(tensors[0].data)
+        tensors[0].data = tensors[0].data.clone()
+        follows(opt, grads, calls)
+        held.append(tensors[2])
+        tensors[2] = tensors[2].clone()
+        follows(opt, grads, calls)
+    opt.copies[1] = torch.zeros(17, dtype=BF16)
+    follows(opt, grads, calls)
+    opt.copies[0] = None
+    follows(opt, grads, calls)
+    assert calls[0]["segs"][0]["copy"] is None
+    # what does not fit is refused
+    t = opt.t
+    for tensors in (opt.params, opt.copies):
+        kept = tensors[2]
+        tensors[2] = torch.zeros(5, dtype=kept.dtype)
+        with pytest.raises(ValueError):
+            opt.step(grads)
+        tensors[2] = kept
+    assert opt.t == t
+    follows(opt, grads, calls)
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_stay_where_they_are(bits, given, calls):
+    """The moments' memory is held by the optimiser: tensors that show it, the caller's own among them, can be given
+    other memory, and lists changed, without the update's going anywhere else."""
+    opt, grads = optimiser(bits, copies=False)
+    names = ["m", "v"] + (["mscale", "vscale"] if bits == 8 else [])
+    state = opt.state()
+    if given:
+        opt = P.AdamW(opt.params, bits=bits, state=state)
+    before = addresses(opt)
+    for name in names:
+        held = state[name][0].data
+        state[name][0].data = torch.zeros_like(held)        # a shown tensor, or the one that was given
+        state[name][1] = torch.zeros_like(state[name][1])
+        getattr(opt, name)[0].data = torch.zeros_like(held)
+        with pytest.raises(AttributeError):
+            setattr(opt, name, list(getattr(opt, name)))
+        with pytest.raises(TypeError):
+            getattr(opt, name)[0] = torch.zeros_like(held)
+    follows(opt, grads, calls)
+    assert addresses(opt) == before
+    for name in names:
+        getattr(opt, name)[1].fill_(3)
+        assert (opt.state()[name][1] == 3).all()
