@@ -1040,10 +1040,17 @@ def _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay):
             segs[k].vscale = _tensor("vscale", vscale[k], (-(-n // 256),), f32, dev)
         if copies is not None:
             segs[k].copy = _tensor("copies", copies[k], p.shape, torch.bfloat16, dev)
-    starts = [s.theta for s in segs if s.n]
-    if len(set(starts)) < len(starts):
-        raise ValueError("a parameter is given twice")
+    _apart([(at, n * e) for s in segs for at, n, e in (
+        (s.theta, s.n, 4), (s.m, s.n, bits // 8), (s.v, s.n, bits // 8), (s.copy, s.n, 2),
+        (s.mscale, -(-s.n // 256), 4), (s.vscale, -(-s.n // 256), 4))])
     return segs, bits, dev0
+
+
+def _apart(places):
+    """Refuses memory (address and bytes) that is written under two names: lanes would race for it."""
+    places = sorted((at, at + n) for at, n in places if at and n)
+    if any(a[1] > b[0] for a, b in zip(places, places[1:])):
+        raise ValueError("parameters, moments, scales and copies must not overlap (is one given twice?)")
 
 
 def _adamw_grads(segs, shapes, grads, dev):
@@ -1097,10 +1104,13 @@ def pyramid_adamw_moments(m, v, mscale, vscale, mout, vout, stream=None):
     if bits != 8:
         raise ValueError("m and v must be 8-bit codes")
     count = len(mout)
+    if len(vout) != count:
+        raise ValueError("mout and vout must have the same length")
     pm, pv = (ctypes.c_void_p * count)(), (ctypes.c_void_p * count)()
     for k in range(count):
         pm[k] = segs[k].theta
         pv[k] = _tensor("vout", vout[k], mout[k].shape, torch.float32, dev)
+    _apart([(at, 4 * s.n) for k, s in enumerate(segs) for at in (pm[k], pv[k])])
     _run("pyramid_adamw_moments", dev, stream, count, segs, pm, pv)
 
 

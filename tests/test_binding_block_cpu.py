@@ -122,3 +122,47 @@ def test_moments_stay_where_they_are(bits, given, calls):
     for name in names:
         getattr(opt, name)[1].fill_(3)
         assert (opt.state()[name][1] == 3).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_updated_memory_is_apart(bits, calls):
+    """What an update writes is refused where two of its tensors share memory, in part or whole."""
+    moment = dict(dtype=F32 if bits == 32 else torch.uint8)
+    whole, rest = torch.zeros(600), torch.zeros(200)
+    codes = torch.zeros(2048, **moment)
+    halves = torch.zeros(600, dtype=BF16)
+    scales = torch.zeros(8)
+
+    def make(params=(whole[:300], whole[300:]), m=(codes[:300], codes[512:812]), v=(codes[1024:1324], codes[1536:1836]),
+             copies=(halves[:300], halves[300:]), ms=(scales[:2], scales[2:4]), vs=(scales[4:6], scales[6:])):
+        state = dict(m=list(m), v=list(v), t=3, mscale=list(ms), vscale=list(vs))
+        return P.AdamW(params, bits=bits, state=state, copies=copies)
+
+    opt = make()                # neighbours touch
+    opt.step([rest.new_ones(300)] * 2)
+    for bad in (dict(params=(whole[:300], whole[299:599])), dict(params=(whole[:300], whole[:300])), dict(params=(whole[:300], whole[100:400])),
+                dict(m=(codes[:300], codes[299:599])), dict(v=(codes[1024:1324], codes[200:500])), dict(copies=(halves[:300], halves[200:500])),
+                dict(copies=(halves[:300], halves[:300])), dict(copies=(halves[:300], whole.view(BF16)[900:1200]))):
+        with pytest.raises(ValueError):
+            make(**bad)
+    if bits == 8:
+        for bad in (dict(ms=(scales[:2], scales[1:3])), dict(vs=(scales[1:3], scales[6:])), dict(vs=(scales[4:6], scales[5:7]))):
+            with pytest.raises(ValueError):
+                make(**bad)
+    # also where memory comes to overlap later
+    opt.copies[1].data = halves[299:599]
+    with pytest.raises(ValueError):
+        opt.step([rest.new_ones(300)] * 2)
+    one = dict(m=[codes[:200]], v=[codes[512:712]], mscale=[scales[:1]], vscale=[scales[1:2]])
+    if bits == 8:
+        calls.clear()
+        P.pyramid_adamw_moments(**one, mout=[rest], vout=[torch.zeros(200)])
+        assert len(calls) == 1
+        for out in (dict(mout=[rest], vout=[rest]), dict(mout=[whole[:200]], vout=[whole[100:300]]), dict(mout=[rest], vout=[])):
+            with pytest.raises(ValueError):
+                P.pyramid_adamw_moments(**one, **out)
+        assert len(calls) == 1
+    with pytest.raises(ValueError):
+        P.pyramid_adamw_step([whole[:300], whole[200:500]], [whole.new_ones(300)] * 2, [codes[:300], codes[512:812]],
+                             [codes[1024:1324], codes[1536:1836]], 1e-3, 1, mscale=[scales[:2], scales[2:4]],
+                             vscale=[scales[4:6], scales[6:]])
