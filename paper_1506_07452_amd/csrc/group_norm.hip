@@ -12,6 +12,8 @@
 // A held volume: 64 x 64 x 32 bf16 forward and backward 30 us, by slabs 34; 300 x 256 x 32 31, 41.
 // Sums of x and x^2 are 64-bit: squares of fp32 are exact, so the variance of values at
 // 1000 times their spread still has 10 digits, and the order of the sums does not show.
+#include <algorithm>
+
 #include "sequence.h"
 #include "timing.h"
 
@@ -25,6 +27,8 @@ constexpr int kGnHeldC = 2048;         // channels that the sums of such a workg
 // Workgroups that a call aims at: 1 x 2764800 x 16 fp32 245 us with 768, 249 with 1024, 253 with 2048, 324 with 256;
 // 8 x 262144 x 64 bf16 386, 389, 414, 622 (512: 243 and 393).
 constexpr int kGnBlocks = 768;
+// Workgroups of 1024 of a launch, which has fewer than 2^32 work items: volumes and groups past them are in launches of their own.
+constexpr unsigned kGnLaunch = 1u << 21;
 
 struct GnArgs {
     long long N, V;
@@ -173,13 +177,14 @@ __device__ inline void over_parts(const GnArgs &a, const double *part, long long
     }
 }
 
-// A group a workgroup.
+// A group a workgroup, from group `first` of all on.
 __global__ void __launch_bounds__(1024)
-k_gn_stats(GnArgs a, const double *part, GroupStats *st, float *stats)
+k_gn_stats(GnArgs a, unsigned first, const double *part, GroupStats *st, float *stats)
 {
     __shared__ double lds[16][2];
-    const long long n = blockIdx.x / (unsigned)a.G;
-    const int g = (int)(blockIdx.x - n * a.G);
+    const unsigned at = first + blockIdx.x;
+    const long long n = at / (unsigned)a.G;
+    const int g = (int)(at - n * a.G);
     double s1 = 0.0, s2 = 0.0;
     over_parts(a, part, n, g, [&](int, double2 v) {
         s1 += v.x;
@@ -188,10 +193,10 @@ k_gn_stats(GnArgs a, const double *part, GroupStats *st, float *stats)
     sum1024(s1, s2, lds);
     if (threadIdx.x) return;
     const GroupStats r(s1, s2, (double)a.V * a.Cg, a.eps);
-    st[blockIdx.x] = r;
+    st[at] = r;
     if (stats) {
-        stats[2 * (long long)blockIdx.x] = r.mean;
-        stats[2 * (long long)blockIdx.x + 1] = r.rstd;
+        stats[2 * (long long)at] = r.mean;
+        stats[2 * (long long)at + 1] = r.rstd;
     }
 }
 
@@ -297,16 +302,16 @@ k_gn_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const GroupStats
     }
 }
 
-// A volume in the registers of a workgroup, K rows a thread.
+// A volume in the registers of a workgroup, K rows a thread; from volume `first` on.
 template <typename T, int NT, int K>
 __global__ void __launch_bounds__(NT)
-k_gn_small_fwd(GnArgs a, const T *x, const T *gamma, const T *beta, T *y, float *stats)
+k_gn_small_fwd(GnArgs a, unsigned first, const T *x, const T *gamma, const T *beta, T *y, float *stats)
 {
     constexpr int N = Piece<T>::N;
     extern __shared__ double dyn[];
     double *lds = dyn, *ch = dyn + sum_rows_lds<NT, N>(a.across);       // ch [C][2]
     GroupStats *st = (GroupStats *)(ch + 2 * a.C);
-    const long long n = blockIdx.x;
+    const long long n = first + blockIdx.x;
     const GnColumn<T> col(a, 0);
     const long long at = n * a.V * a.C + col.c;
     u32x4 raw[K];
@@ -445,16 +450,17 @@ k_gn_bwd_sums(GnArgs a, const T *x, const T *gamma, const T *beta, const float *
     sum_rows<kGnThreads, N>(a, lds, qs, [&](int o, double t) { if (first + o < a.C) to[(first + o) * 2 + 1] = t; });
 }
 
-// The first `groups` workgroups: a group's mean of a and of a xh; the others: dgamma and
-// dbeta of 16 channels, 64 lanes each over the parts of all volumes.
+// The first `groups` workgroups: a group's mean of a and of a xh, from group `first` of all on; the others: dgamma
+// and dbeta of 16 channels, 64 lanes each over the parts of all volumes.
 template <typename T>
 __global__ void __launch_bounds__(1024)
-k_gn_bwd_finish(GnArgs a, int groups, const T *gamma, const double *part, float2 *means, float *dgamma, float *dbeta)
+k_gn_bwd_finish(GnArgs a, unsigned first, int groups, const T *gamma, const double *part, float2 *means, float *dgamma, float *dbeta)
 {
     __shared__ double2 lds[64][16];
     if ((int)blockIdx.x < groups) {
-        const long long n = blockIdx.x / (unsigned)a.G;
-        const int g = (int)(blockIdx.x - n * a.G);
+        const unsigned at = first + blockIdx.x;
+        const long long n = at / (unsigned)a.G;
+        const int g = (int)(at - n * a.G);
         double s1 = 0.0, s2 = 0.0;
         over_parts(a, part, n, g, [&](int c, double2 v) {
             const double w = (double)Store<T>::load(gamma, c);
@@ -463,7 +469,7 @@ k_gn_bwd_finish(GnArgs a, int groups, const T *gamma, const double *part, float2
         });
         sum1024(s1, s2, (double(*)[2])lds);
         const double inv = 1.0 / ((double)a.V * a.Cg);
-        if (threadIdx.x == 0) means[blockIdx.x] = make_float2((float)(s1 * inv), (float)(s2 * inv));
+        if (threadIdx.x == 0) means[at] = make_float2((float)(s1 * inv), (float)(s2 * inv));
         return;
     }
     const int o = threadIdx.x % 16, lane = threadIdx.x / 16, c = ((int)blockIdx.x - groups) * 16 + o;
@@ -535,17 +541,17 @@ k_gn_bwd_apply(GnArgs a, const T *x, const T *gamma, const T *beta, const float 
     }
 }
 
-// A volume in the registers of a workgroup; part [n][C][2] as of one slab.
+// A volume in the registers of a workgroup, from volume `first` on; part [n][C][2] as of one slab.
 template <typename T, int NT, int K>
 __global__ void __launch_bounds__(NT)
-k_gn_small_bwd(GnArgs a, const T *x, const T *gamma, const T *beta, const float *stats, const T *dy, T *dx,
+k_gn_small_bwd(GnArgs a, unsigned first, const T *x, const T *gamma, const T *beta, const float *stats, const T *dy, T *dx,
                double *part, float *dgamma, float *dbeta)
 {
     constexpr int N = Piece<T>::N;
     extern __shared__ double dyn[];
     float *lds = (float *)dyn, *ch = lds + sum_rows_lds<NT, N>(a.across);       // ch [C][2]
     float2 *means = (float2 *)(ch + 2 * a.C);
-    const long long n = blockIdx.x;
+    const long long n = first + blockIdx.x;
     const GnColumn<T> col(a, 0);
     const long long at = n * a.V * a.C + col.c;
     u32x4 rx[K], rd[K];
@@ -631,7 +637,7 @@ int check_gn(int64_t N, int64_t V, int32_t C, int32_t G, int32_t dtype)
     if (N < 1 || V < 1 || C < 1 || G < 1 || C % G) return PLSTM_EINVAL;
     if (dtype != PLSTM_F32 && dtype != PLSTM_BF16) return PLSTM_EINVAL;
     if (C > kGnMaxC || N > (1LL << 22) || V > (1LL << 36) || N * V > (1LL << 38) / C) return PLSTM_EUNSUPPORTED;
-    if (N * G > (1LL << 30)) return PLSTM_EUNSUPPORTED;         // workgroups of a launch
+    if (N * G > (1LL << 30)) return PLSTM_EUNSUPPORTED;
     return PLSTM_OK;
 }
 
@@ -682,29 +688,43 @@ constexpr int gn_held(int dtype, bool backward)
     return (dtype == PLSTM_F32 ? 16 : 8) / (backward ? 2 : 1);
 }
 
+// Runs launch(first, workgroups) over `all` of them; returns the number of launches.
+template <typename F>
+int gn_launches(long long all, F launch)
+{
+    int n = 0;
+    for (long long first = 0; first < all; first += kGnLaunch, ++n)
+        launch((unsigned)first, (unsigned)std::min<long long>(all - first, kGnLaunch));
+    return n;
+}
+
 template <typename T, int NT, int K>
-void launch_small_fwd(const GnPlan &p, const void *x, const void *gamma, const void *beta, void *y, void *stats,
+int launch_small_fwd(const GnPlan &p, const void *x, const void *gamma, const void *beta, void *y, void *stats,
                       hipStream_t st)
 {
     const size_t lds = sizeof(double) * (sum_rows_lds<NT, Piece<T>::N>(p.a.across) + 2 * p.a.C) + sizeof(GroupStats) * p.a.G;
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)k_gn_small_fwd<T, NT, K>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)lds);
-    k_gn_small_fwd<T, NT, K><<<(unsigned)p.a.N, NT, lds, st>>>(p.a, (const T *)x, (const T *)gamma, (const T *)beta,
-                                                               (T *)y, (float *)stats);
+    return gn_launches(p.a.N, [&](unsigned first, unsigned n) {
+        k_gn_small_fwd<T, NT, K><<<n, NT, lds, st>>>(p.a, first, (const T *)x, (const T *)gamma, (const T *)beta,
+                                                     (T *)y, (float *)stats);
+    });
 }
 
 template <typename T, int NT, int K>
-void launch_small_bwd(const GnPlan &p, const void *x, const void *gamma, const void *beta, const void *stats,
+int launch_small_bwd(const GnPlan &p, const void *x, const void *gamma, const void *beta, const void *stats,
                       const void *dy, void *dx, double *part, void *dgamma, void *dbeta, hipStream_t st)
 {
     const size_t lds = sizeof(float) * (sum_rows_lds<NT, Piece<T>::N>(p.a.across) + 2 * p.a.C) + sizeof(float2) * p.a.G;
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)k_gn_small_bwd<T, NT, K>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)lds);
-    k_gn_small_bwd<T, NT, K><<<(unsigned)p.a.N, NT, lds, st>>>(p.a, (const T *)x, (const T *)gamma, (const T *)beta,
-                                                               (const float *)stats, (const T *)dy, (T *)dx, part,
-                                                               (float *)dgamma, (float *)dbeta);
+    return gn_launches(p.a.N, [&](unsigned first, unsigned n) {
+        k_gn_small_bwd<T, NT, K><<<n, NT, lds, st>>>(p.a, first, (const T *)x, (const T *)gamma, (const T *)beta,
+                                                     (const float *)stats, (const T *)dy, (T *)dx, part,
+                                                     (float *)dgamma, (float *)dbeta);
+    });
 }
 
 template <typename T>
@@ -713,7 +733,8 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
 {
     const GnArgs &a = p.a;
     if (p.held) {
-        const auto go = [&](auto fn) { fn(p, x, gamma, beta, y, stats, st); };
+        int n = 0;
+        const auto go = [&](auto fn) { n = fn(p, x, gamma, beta, y, stats, st); };
         if (p.threads == kGnThreads) {
             if (p.held == 1) go(launch_small_fwd<T, kGnThreads, 1>);
             else if (p.held == 2) go(launch_small_fwd<T, kGnThreads, 2>);
@@ -725,7 +746,7 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
             else if constexpr (sizeof(T) == 4) go(launch_small_fwd<T, kGnSmall, 16>);
         }
         PLSTM_LAUNCH_CHECK();
-        return 1;
+        return n;
     }
     Carve cv(ws);
     double *part = cv.take<double>((size_t)a.N * a.slabs * a.C * 2);
@@ -737,8 +758,11 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
     // few parts are added by every workgroup for itself (a slab's worth of them: up to 64 of at most 256 channels): 1 x 4096 x 32
     // 13.5 us a call, with a launch between 15.8
     const bool few = a.slabs <= 64 && a.C <= 256;
+    int launches = 2;
     if (!few) {
-        k_gn_stats<<<(unsigned)(a.N * a.G), 1024, 0, st>>>(a, part, gs, (float *)stats);
+        launches += gn_launches(a.N * a.G, [&](unsigned first, unsigned n) {
+            k_gn_stats<<<n, 1024, 0, st>>>(a, first, part, gs, (float *)stats);
+        });
         PLSTM_LAUNCH_CHECK();
     }
     const auto apply = few      ? (stream ? k_gn_apply<T, true, true> : k_gn_apply<T, false, true>)
@@ -747,7 +771,7 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
     apply<<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta, gs, (T *)y, part,
                                        few ? (float *)stats : nullptr);
     PLSTM_LAUNCH_CHECK();
-    return few ? 2 : 3;
+    return launches;
 }
 
 template <typename T>
@@ -760,7 +784,8 @@ int gn_backward(const GnPlan &p, const void *x, const void *gamma, const void *b
     float2 *means = cv.take<float2>((size_t)a.N * a.G);
     const int weights = (a.C + 15) / 16;
     if (p.held) {
-        const auto go = [&](auto fn) { fn(p, x, gamma, beta, stats, dy, dx, part, dgamma, dbeta, st); };
+        int n = 0;
+        const auto go = [&](auto fn) { n = fn(p, x, gamma, beta, stats, dy, dx, part, dgamma, dbeta, st); };
         if (p.threads == kGnThreads) {
             if (p.held == 1) go(launch_small_bwd<T, kGnThreads, 1>);
             else if (p.held == 2) go(launch_small_bwd<T, kGnThreads, 2>);
@@ -771,25 +796,28 @@ int gn_backward(const GnPlan &p, const void *x, const void *gamma, const void *b
             else if constexpr (sizeof(T) == 4) go(launch_small_bwd<T, kGnSmall, 8>);
         }
         PLSTM_LAUNCH_CHECK();
-        if (a.N == 1) return 1;
-        k_gn_bwd_finish<T><<<weights, 1024, 0, st>>>(a, 0, (const T *)gamma, part, means, (float *)dgamma, (float *)dbeta);
+        if (a.N == 1) return n;
+        k_gn_bwd_finish<T><<<weights, 1024, 0, st>>>(a, 0, 0, (const T *)gamma, part, means, (float *)dgamma,
+                                                     (float *)dbeta);
         PLSTM_LAUNCH_CHECK();
-        return 2;
+        return n + 1;
     }
     const dim3 grid((unsigned)(a.N * a.slabs), p.blocks_y);
     const bool stream = a.N * a.V * a.C * (long long)sizeof(T) >= kStreamBytes;
     k_gn_bwd_sums<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta,
                                                   (const float *)stats, (const T *)dy, part);
     PLSTM_LAUNCH_CHECK();
-    const int groups = (int)(a.N * a.G);
-    k_gn_bwd_finish<T><<<groups + weights, 1024, 0, st>>>(a, groups, (const T *)gamma, part, means, (float *)dgamma,
-                                                         (float *)dbeta);
+    const int launches = 1 + gn_launches(a.N * a.G, [&](unsigned first, unsigned n) {
+        // the weights with the last ones
+        k_gn_bwd_finish<T><<<n + (first + n == a.N * a.G ? weights : 0), 1024, 0, st>>>(
+            a, first, (int)n, (const T *)gamma, part, means, (float *)dgamma, (float *)dbeta);
+    });
     PLSTM_LAUNCH_CHECK();
-    if (!dx) return 2;
+    if (!dx) return launches;
     (stream ? k_gn_bwd_apply<T, true> : k_gn_bwd_apply<T, false>)<<<grid, kGnThreads, 0, st>>>(
         a, (const T *)x, (const T *)gamma, (const T *)beta, (const float *)stats, (const T *)dy, means, (T *)dx);
     PLSTM_LAUNCH_CHECK();
-    return 3;
+    return launches + 1;
 }
 
 }  // namespace

@@ -6,8 +6,11 @@ import pytest
 import torch
 
 import paper_1506_07452_amd as P
+from tests import block_ref as R
 from tests.gpu_util import DEV, say
-from tests.test_gpu_sequence import BF16, F32, rand
+from tests.seq_ref import rounded
+from tests.test_gpu_block import gn_case
+from tests.test_gpu_sequence import BF16, F32, near, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +40,37 @@ def test_update_of_tensors_with_other_memory(bits):
     assert all(torch.equal(a, b) for a, b in zip(plain.m + plain.v, moved.m + moved.v))
     # all but the first update's went to memory of the update before
     assert all(torch.equal(a, b) for a, b in before)
+
+
+# ------------------------------------------------- more work than a launch takes
+
+@pytest.mark.parametrize("N,G", [(1024, 4096), (1025, 4096), (513, 4100)])
+def test_group_norm_of_groups_past_a_launch(N, G):
+    """More groups than a launch of workgroups of 1024 has (fewer than 2^32 work items), a channel each: the last of them are
+    in another launch, which the weights' gradients go with."""
+    say("group norm of groups past a launch", N, G)
+    gn_case(N, (2,), G, G, F32, seed=N)
+
+
+def test_group_norm_of_volumes_past_a_launch():
+    """As many volumes as there may be, each held by a workgroup of 1024."""
+    N, V, period = 1 << 22, 1025, 64
+    say("group norm of volumes past a launch")
+    base, dbase = rand(1, (period, V, 1), BF16, 0.8, 0.3), rand(2, (period, V, 1), BF16, 0.3)
+    gamma, beta = rand(3, (1,), BF16, 0.2, 1.0), rand(4, (1,), BF16, 0.3)
+    x, dy = (b.to(DEV).repeat(N // period, 1, 1) for b in (base, dbase))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    stats, dg, db = torch.empty((N, 1, 2), device=DEV), torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+    P.pyramid_group_norm_forward(x, gamma.to(DEV), beta.to(DEV), y, 1, act="silu", stats=stats)
+    P.pyramid_group_norm_backward(x, gamma.to(DEV), beta.to(DEV), stats, dy, dx, dg, db, 1, act="silu")
+    torch.cuda.synchronize()
+    for t in (y, dx, stats):
+        rows = t.view(N // period, -1)
+        assert all(bool((part == rows[0]).all()) for part in rows.split(1 << 13))
+    (ry, ey), _, kept = R.group_norm(base, gamma, beta, 1, "silu", 1e-5)
+    near("y", y[:period].cpu(), ry, rounded(ry, ey, BF16))
+    (rx, ex), (rg, eg), (rb, eb) = R.group_norm_backward(kept, base, gamma, beta, dbase, 1, "silu")
+    near("dx", dx[:period].cpu(), rx, rounded(rx, ex, BF16))
+    times = N // period
+    near("dgamma", dg.cpu(), rg * times, rounded(rg * times, eg * times, F32))
+    near("dbeta", db.cpu(), rb * times, rounded(rb * times, eb * times, F32))
