@@ -302,15 +302,15 @@ k_conv_bwd(ConvArgs a, int PB, const T *x, const T *w, const T *bias, const T *s
     }
 }
 
-// dw [I][K] and dbias [I] from the parts, added in 64 bits: 16 lanes an output, each
+// dw [I][K] and dbias [I] from the parts, from workgroup `first` of all on, added in 64 bits: 16 lanes an output, each
 // every 16th part, then in the lanes' order.
 template <int K>
 __global__ void __launch_bounds__(256)
-k_conv_weights(long long I, int parts, const float *part, float *dw, float *db)
+k_conv_weights(unsigned first, long long I, int parts, const float *part, float *dw, float *db)
 {
     __shared__ double lds[16][16];
     const int o = threadIdx.x % 16, lane = threadIdx.x / 16;
-    const long long at = (long long)blockIdx.x * 16 + o, all = I * (K + 1);
+    const long long at = (long long)(first + blockIdx.x) * 16 + o, all = I * (K + 1);
     double s = 0.0;
     if (at < all)
         for (int p = lane; p < parts; p += 16) s += (double)part[(long long)p * all + at];
@@ -462,21 +462,23 @@ int pyramid_causal_conv_backward(int64_t B, int64_t T, int64_t I, int32_t K, int
             go(0.0f, stream_out ? k_conv_bwd<float, KK, true> : k_conv_bwd<float, KK, false>);
         else
             go((uint16_t)0, stream_out ? k_conv_bwd<uint16_t, KK, true> : k_conv_bwd<uint16_t, KK, false>);
-        k_conv_weights<KK><<<(unsigned)((I * (KK + 1) + 15) / 16), 256, 0, st>>>(
-            I, parts, (const float *)ws, (float *)dw, (float *)db);
+        return in_launches<256>((I * (KK + 1) + 15) / 16, [&](unsigned first, unsigned n) {
+            k_conv_weights<KK><<<n, 256, 0, st>>>(first, I, parts, (const float *)ws, (float *)dw, (float *)db);
+        });
     };
+    int launches = 0;
     switch (K) {
-    case 1: run(std::integral_constant<int, 1>()); break;
-    case 2: run(std::integral_constant<int, 2>()); break;
-    case 3: run(std::integral_constant<int, 3>()); break;
-    case 4: run(std::integral_constant<int, 4>()); break;
-    case 5: run(std::integral_constant<int, 5>()); break;
-    case 6: run(std::integral_constant<int, 6>()); break;
-    case 7: run(std::integral_constant<int, 7>()); break;
-    default: run(std::integral_constant<int, 8>()); break;
+    case 1: launches = run(std::integral_constant<int, 1>()); break;
+    case 2: launches = run(std::integral_constant<int, 2>()); break;
+    case 3: launches = run(std::integral_constant<int, 3>()); break;
+    case 4: launches = run(std::integral_constant<int, 4>()); break;
+    case 5: launches = run(std::integral_constant<int, 5>()); break;
+    case 6: launches = run(std::integral_constant<int, 6>()); break;
+    case 7: launches = run(std::integral_constant<int, 7>()); break;
+    default: launches = run(std::integral_constant<int, 8>()); break;
     }
     PLSTM_LAUNCH_CHECK();
-    timing_end(2, st);
+    timing_end(1 + launches, st);
     return PLSTM_OK;
 }
 

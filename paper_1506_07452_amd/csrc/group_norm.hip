@@ -12,8 +12,6 @@
 // A held volume: 64 x 64 x 32 bf16 forward and backward 30 us, by slabs 34; 300 x 256 x 32 31, 41.
 // Sums of x and x^2 are 64-bit: squares of fp32 are exact, so the variance of values at
 // 1000 times their spread still has 10 digits, and the order of the sums does not show.
-#include <algorithm>
-
 #include "sequence.h"
 #include "timing.h"
 
@@ -27,8 +25,6 @@ constexpr int kGnHeldC = 2048;         // channels that the sums of such a workg
 // Workgroups that a call aims at: 1 x 2764800 x 16 fp32 245 us with 768, 249 with 1024, 253 with 2048, 324 with 256;
 // 8 x 262144 x 64 bf16 386, 389, 414, 622 (512: 243 and 393).
 constexpr int kGnBlocks = 768;
-// Workgroups of 1024 of a launch, which has fewer than 2^32 work items: volumes and groups past them are in launches of their own.
-constexpr unsigned kGnLaunch = 1u << 21;
 
 struct GnArgs {
     long long N, V;
@@ -688,16 +684,6 @@ constexpr int gn_held(int dtype, bool backward)
     return (dtype == PLSTM_F32 ? 16 : 8) / (backward ? 2 : 1);
 }
 
-// Runs launch(first, workgroups) over `all` of them; returns the number of launches.
-template <typename F>
-int gn_launches(long long all, F launch)
-{
-    int n = 0;
-    for (long long first = 0; first < all; first += kGnLaunch, ++n)
-        launch((unsigned)first, (unsigned)std::min<long long>(all - first, kGnLaunch));
-    return n;
-}
-
 template <typename T, int NT, int K>
 int launch_small_fwd(const GnPlan &p, const void *x, const void *gamma, const void *beta, void *y, void *stats,
                       hipStream_t st)
@@ -706,7 +692,7 @@ int launch_small_fwd(const GnPlan &p, const void *x, const void *gamma, const vo
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)k_gn_small_fwd<T, NT, K>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)lds);
-    return gn_launches(p.a.N, [&](unsigned first, unsigned n) {
+    return in_launches<NT>(p.a.N, [&](unsigned first, unsigned n) {
         k_gn_small_fwd<T, NT, K><<<n, NT, lds, st>>>(p.a, first, (const T *)x, (const T *)gamma, (const T *)beta,
                                                      (T *)y, (float *)stats);
     });
@@ -720,7 +706,7 @@ int launch_small_bwd(const GnPlan &p, const void *x, const void *gamma, const vo
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)k_gn_small_bwd<T, NT, K>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)lds);
-    return gn_launches(p.a.N, [&](unsigned first, unsigned n) {
+    return in_launches<NT>(p.a.N, [&](unsigned first, unsigned n) {
         k_gn_small_bwd<T, NT, K><<<n, NT, lds, st>>>(p.a, first, (const T *)x, (const T *)gamma, (const T *)beta,
                                                      (const float *)stats, (const T *)dy, (T *)dx, part,
                                                      (float *)dgamma, (float *)dbeta);
@@ -760,7 +746,7 @@ int gn_forward(const GnPlan &p, const void *x, const void *gamma, const void *be
     const bool few = a.slabs <= 64 && a.C <= 256;
     int launches = 2;
     if (!few) {
-        launches += gn_launches(a.N * a.G, [&](unsigned first, unsigned n) {
+        launches += in_launches<1024>(a.N * a.G, [&](unsigned first, unsigned n) {
             k_gn_stats<<<n, 1024, 0, st>>>(a, first, part, gs, (float *)stats);
         });
         PLSTM_LAUNCH_CHECK();
@@ -807,7 +793,7 @@ int gn_backward(const GnPlan &p, const void *x, const void *gamma, const void *b
     k_gn_bwd_sums<T><<<grid, kGnThreads, 0, st>>>(a, (const T *)x, (const T *)gamma, (const T *)beta,
                                                   (const float *)stats, (const T *)dy, part);
     PLSTM_LAUNCH_CHECK();
-    const int launches = 1 + gn_launches(a.N * a.G, [&](unsigned first, unsigned n) {
+    const int launches = 1 + in_launches<1024>(a.N * a.G, [&](unsigned first, unsigned n) {
         // the weights with the last ones
         k_gn_bwd_finish<T><<<n + (first + n == a.N * a.G ? weights : 0), 1024, 0, st>>>(
             a, first, (int)n, (const T *)gamma, part, means, (float *)dgamma, (float *)dbeta);

@@ -986,14 +986,14 @@ k_sel_rows(long long n, int tiles, const float *dBp, const float *dCp, T *dB, T 
     }
 }
 
-// dA [I S], dD and ddelta_bias [I] from the jobs' parts, in 64 bits: L lanes an output.
+// dA [I S], dD and ddelta_bias [I] from the jobs' parts, from workgroup `first` of all on, in 64 bits: L lanes an output.
 template <int L>
 __global__ void __launch_bounds__(16 * L)
-k_sel_weights(long long nA, long long I, int jobs, const float *dAp, const float *dDp, float *dA, float *dD, float *db)
+k_sel_weights(unsigned first, long long nA, long long I, int jobs, const float *dAp, const float *dDp, float *dA, float *dD, float *db)
 {
     __shared__ double lds[L][16];
     const int o = threadIdx.x % 16, lane = threadIdx.x / 16;
-    const long long at = (long long)blockIdx.x * 16 + o, nD = 2 * I;
+    const long long at = (long long)(first + blockIdx.x) * 16 + o, nD = 2 * I;
     double s = 0.0;
     if (at < nA + nD) {
         const float *p = at < nA ? dAp + at : dDp + (at - nA);
@@ -1182,17 +1182,18 @@ int sel_backward(const SelPlan &p, const SelTensors &t, hipStream_t st)
         ++launches;
     }
     const long long nA = a.I * a.S;
-    const unsigned blocks = (unsigned)((nA + 2 * a.I + 15) / 16);
     const auto weights = [&](auto l) {
         constexpr int L = decltype(l)::value;
-        k_sel_weights<L><<<blocks, 16 * L, 0, st>>>(nA, a.I, (int)a.jobs, p.dAp, p.dDp, (float *)t.dA, (float *)t.dD,
-                                                    (float *)t.db);
+        launches += in_launches<16 * L>((nA + 2 * a.I + 15) / 16, [&](unsigned first, unsigned n) {
+            k_sel_weights<L><<<n, 16 * L, 0, st>>>(first, nA, a.I, (int)a.jobs, p.dAp, p.dDp, (float *)t.dA, (float *)t.dD,
+                                                   (float *)t.db);
+        });
     };
     // 3840 parts of 16 x 16 outputs: 64 lanes each 14.6 us, 16 lanes 19.0; 64 parts of 2048 x 16: 8.8, 5.0
     if (a.jobs > 128) weights(std::integral_constant<int, 64>());
     else weights(std::integral_constant<int, 16>());
     PLSTM_LAUNCH_CHECK();
-    return launches + 1;
+    return launches;
 }
 
 template <typename T>

@@ -38,6 +38,18 @@ __device__ inline float silu_slope(float a, float &silu)
     return s * fmaf(a, t, 1.0f);
 }
 
+// A launch has fewer than 2^32 work items.  Calls launch(first, workgroups) for pieces of at most half of that of `all` workgroups of
+// THREADS; returns the number of launches.
+template <int THREADS, typename F>
+inline int in_launches(long long all, F launch)
+{
+    constexpr long long most = (1LL << 31) / THREADS;
+    int n = 0;
+    for (long long first = 0; first < all; first += most, ++n)
+        launch((unsigned)first, (unsigned)(all - first < most ? all - first : most));
+    return n;
+}
+
 // Pieces of tensors too large for the caches: read for the last time, or written for a later launch.  Non-temporal accesses
 // leave the caches to what is read twice, and no written lines behind that the next launch waits to have written back: group norm of
 // 1 x 2764800 x 16 fp32 248 us, without 297, of 8 x 262144 x 64 bf16 388, 454; the convolution of 2 x 8192 x 2048 92, 96;

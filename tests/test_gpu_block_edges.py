@@ -74,3 +74,57 @@ def test_group_norm_of_volumes_past_a_launch():
     times = N // period
     near("dgamma", dg.cpu(), rg * times, rounded(rg * times, eg * times, F32))
     near("dbeta", db.cpu(), rb * times, rounded(rb * times, eb * times, F32))
+
+
+def test_conv_weights_past_a_launch():
+    """So many channels that the sums of the weights' gradients have outputs in a second launch."""
+    K, n = 4, 300
+    I = (1 << 28) // (K + 1) + 5000
+    say("convolution weights past a launch", I)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+
+    def some(*shape, dtype=BF16):
+        return torch.empty(shape, dtype=dtype, device=DEV).normal_(generator=gen)
+    x, w, b, state, dy, dst = some(1, 1, I), some(I, K), some(I), some(1, K - 1, I), some(1, 1, I), some(1, K - 1, I, dtype=F32)
+    dx, dw, db, before = torch.empty_like(x), torch.empty((I, K), device=DEV), torch.empty(I, device=DEV), torch.empty_like(dst)
+    P.pyramid_causal_conv_backward(x, w, b, dy, dx, dw, db, act="silu", state=state, dstate_out=dst, dstate=before)
+    # the first, those around the launches' border, the last
+    for at in (0, (1 << 31) // 16 // (K + 1) - n // 2, I - n):
+        c = slice(at, at + n)
+        part = [t[..., c].cpu() for t in (x, b, state, dy, dst)]
+        _, _, kept = R.conv_forward(part[0], w[c].cpu(), part[1], "silu", False, None, part[2])
+        gx, gw, gb, gs = R.conv_backward(kept, w[c].cpu(), part[3], "silu", False, part[4])
+        near("dx", dx[..., c].cpu(), gx[0], rounded(*gx, BF16))
+        near("dw", dw[c].cpu(), *gw)
+        near("db", db[c].cpu(), *gb)
+        near("dstate", before[..., c].cpu(), *gs)
+
+
+def test_scan_weights_past_a_launch():
+    """The most channels of a scan: the sums of the weights' gradients have outputs in a second launch."""
+    I, S, n = 1 << 24, 16, 200
+    say("scan weights past a launch")
+    gen = torch.Generator(device=DEV).manual_seed(2)
+
+    def some(*shape, dtype=BF16):
+        return torch.empty(shape, dtype=dtype, device=DEV).normal_(generator=gen)
+    u, delta, dy = some(1, 1, I), some(1, 1, I), some(1, 1, I)
+    Bm, Cm, h0, dhT = some(1, 1, S), some(1, 1, S), some(1, I, S, dtype=F32), some(1, I, S, dtype=F32)
+    A, D, bias = some(I, S, dtype=F32).mul_(0.5).exp_().neg_(), some(I, dtype=F32), some(I, dtype=F32)
+    saved = torch.empty(P.pyramid_selective_scan_saved_size(1, 1, I, S), dtype=torch.uint8, device=DEV)
+    how = dict(D=D, delta_bias=bias, softplus=True)
+    P.pyramid_selective_scan_forward(u, delta, A, Bm, Cm, torch.empty_like(u), h0=h0, saved=saved, **how)
+    du, ddelta, dA, dB, dC = (torch.empty_like(t) for t in (u, delta, A, Bm, Cm))
+    dD, dbias, dh0 = torch.empty_like(D), torch.empty_like(D), torch.empty_like(h0)
+    P.pyramid_selective_scan_backward(u, delta, A, Bm, Cm, saved, dy, du, ddelta, dA, dB, dC, dD=dD, ddelta_bias=dbias, dhT=dhT, dh0=dh0,
+                                      **how)
+    # dA first, then dD and ddelta_bias: around the launches' border and in the last of all
+    for at in (0, (1 << 31) // 16 // S - n // 2, I - n):
+        c = slice(at, at + n)
+        ref = R.Select(u[..., c].cpu(), delta[..., c].cpu(), A[c].cpu(), Bm.cpu(), Cm.cpu(), D[c].cpu(), None, bias[c].cpu(), True,
+                       h0=h0[:, c].cpu())
+        want = ref.backward(dy[..., c].cpu(), dhT[:, c].cpu())
+        for name, got in (("dA", dA[c]), ("dD", dD[c]), ("ddelta_bias", dbias[c]), ("dh0", dh0[:, c])):
+            near(name, got.cpu(), *want[name])
+        for name, got in (("du", du), ("ddelta", ddelta)):
+            near(name, got[..., c].cpu(), want[name][0], rounded(*want[name], BF16))
