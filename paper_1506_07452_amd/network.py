@@ -289,7 +289,8 @@ def selective_forward(u, delta, z, Bm, Cm, p, axis: str, reverse: bool = False, 
     """Selective sweep of a volume: a causal convolution with SiLU of u, then a selective scan of it gated
     by z (or None), along the lines of `axis` ("z", "y" or "x", "zyx": all voxels in raster order;
     from the far side with `reverse`).  u, delta, z [N][D][H][W][I], Bm, Cm [N][D][H][W][S]; p: a dict
-    of conv_w [I][K], conv_b [I] in their dtype and A [I][S], D, delta_bias [I] fp32.
+    of conv_w [I][K], conv_b [I] in their dtype and A [I][S], D, delta_bias [I] fp32 (conv_b, D and
+    delta_bias may be None: zeros).
     Returns (y, kept): kept is None for inference, else what selective_backward needs."""
     shape = u.shape
     u, delta, z, Bm, Cm = (_lines(t, axis) for t in (u, delta, z, Bm, Cm))
@@ -306,14 +307,14 @@ def selective_forward(u, delta, z, Bm, Cm, p, axis: str, reverse: bool = False, 
 
 @_on_its_stream
 def selective_backward(dy, kept, p, ws=None, stream=None):
-    """Gradients of selective_forward: a dict of u, delta, z (None without it), Bm, Cm (volumes)
-    and conv_w, conv_b, A, D, delta_bias (fp32)."""
+    """Gradients of selective_forward: a dict of u, delta, z, Bm, Cm (volumes) and conv_w, conv_b,
+    A, D, delta_bias (fp32); None for what was None."""
     u, v, delta, z, Bm, Cm, saved, axis, reverse = kept
     shape, dy = dy.shape, _lines(dy, axis)
     g = {k: None if t is None else torch.empty_like(t)
          for k, t in (("v", v), ("delta", delta), ("z", z), ("Bm", Bm), ("Cm", Cm), ("u", u))}
     for k in ("conv_w", "conv_b", "A", "D", "delta_bias"):
-        g[k] = torch.empty_like(p[k], dtype=torch.float32)
+        g[k] = None if p[k] is None else torch.empty_like(p[k], dtype=torch.float32)
     pyramid_selective_scan_backward(v, delta, p["A"], Bm, Cm, saved, dy, g["v"], g["delta"], g["A"], g["Bm"],
                                     g["Cm"], p["D"], z, p["delta_bias"], True, g["D"], g["z"], g["delta_bias"],
                                     reverse, ws=ws, stream=stream)

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_1506_07452_amd as P
+from paper_1506_07452_amd import network as net
 from tests import block_ref as R
 from tests.gpu_util import DEV, say
 from tests.seq_ref import rounded
@@ -128,3 +129,25 @@ def test_scan_weights_past_a_launch():
             near(name, got.cpu(), *want[name])
         for name, got in (("du", du), ("ddelta", ddelta)):
             near(name, got[..., c].cpu(), want[name][0], rounded(*want[name], BF16))
+
+
+# ---------------------------------------------------- arguments that are left out
+
+@pytest.mark.parametrize("left_out", [("conv_b",), ("D",), ("delta_bias",), ("conv_b", "D", "delta_bias")])
+def test_sweep_without_biases(left_out):
+    """A selective sweep's conv_b, D and delta_bias may be None: zeros, without a gradient."""
+    say("sweep without", left_out)
+    shape, I, S = (2, 3, 4, 9), 6, 4
+    u, delta, z, dy = (rand(k, shape + (I,), F32, 0.5).to(DEV) for k in range(4))
+    Bm, Cm = (rand(4 + k, shape + (S,), F32).to(DEV) for k in range(2))
+    p = {"conv_w": rand(6, (I, 4), F32, 0.5), "conv_b": rand(7, (I,), F32, 0.2), "A": -torch.exp(rand(8, (I, S), F32, 0.5)),
+         "D": rand(9, (I,), F32), "delta_bias": rand(10, (I,), F32, 0.5)}
+    p = {k: torch.zeros_like(t).to(DEV) if k in left_out else t.to(DEV) for k, t in p.items()}
+    y, kept = net.selective_forward(u, delta, z, Bm, Cm, p, "x", training=True)
+    want = net.selective_backward(dy, kept, p)
+    none = {k: None if k in left_out else t for k, t in p.items()}
+    got_y, kept = net.selective_forward(u, delta, z, Bm, Cm, none, "x", training=True)
+    got = net.selective_backward(dy, kept, none)
+    assert torch.equal(y, got_y) and set(got) == set(want)
+    for k, g in got.items():
+        assert g is None if k in left_out else torch.equal(g, want[k]), k
