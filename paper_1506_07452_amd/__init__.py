@@ -587,6 +587,12 @@ def _main(name, t, dims):
     return code, t.data_ptr(), t.get_device()
 
 
+def _torch_tensor(t):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("expected a torch.Tensor, got %r" % type(t))
+    return t
+
+
 def _tensor(name, t, shape, dtype, dev):
     """Pointer of a tensor that has to have this shape, type and device (None: NULL)."""
     if t is None:
@@ -595,8 +601,9 @@ def _tensor(name, t, shape, dtype, dev):
         # a host tensor's device number is -1
         if t.shape == shape and t.dtype == dtype and t.get_device() == dev and t.is_contiguous():
             return t.data_ptr()
-    except AttributeError:
-        raise TypeError("expected a torch.Tensor, got %r" % type(t)) from None
+    except (AttributeError, TypeError):     # an array of another library: its type is not comparable
+        pass
+    _torch_tensor(t)
     raise ValueError("%s must be %s %s on cuda:%d and contiguous, got %s %s on %s%s" % (
         name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device,
         "" if t.is_contiguous() else ", not contiguous"))
@@ -795,15 +802,13 @@ def _pitched(name, t, shape, dtype, dev):
     elements of a row next to each other, rows (b, t) at (b T + t) pitch (0: dense)."""
     if t is None:
         return None, 0
-    try:
-        if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
-            raise ValueError("%s must be %s %s on cuda:%d, got %s %s on %s" % (
-                name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device))
-        if t.is_contiguous():
-            return t.data_ptr(), 0
-        sb, st, sn = t.stride()
-    except AttributeError:
-        raise TypeError("expected a torch.Tensor, got %r" % type(t)) from None
+    _torch_tensor(t)
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError("%s must be %s %s on cuda:%d, got %s %s on %s" % (
+            name, dtype, list(shape), dev, t.dtype, list(t.shape), t.device))
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    sb, st, sn = t.stride()
     B, T, n = shape
     pitch = st if T > 1 else sb if B > 1 else n
     if (n > 1 and sn != 1) or pitch < n or (B > 1 and sb != T * pitch):
@@ -842,7 +847,7 @@ def pyramid_causal_conv_forward(x, w, bias, y, act="none", reverse=False, length
     pyramid_scan_forward."""
     dt, dev, px, pitch = _main_pitched("x", x)
     B, T, I = x.shape
-    K = w.shape[-1] if w.dim() == 2 else 0
+    K = w.shape[-1] if _torch_tensor(w).dim() == 2 else 0
     _run("pyramid_causal_conv_forward", dev, stream, B, T, I, K, dt, _act(act), int(bool(reverse)),
          px, pitch, _tensor("w", w, (I, K), x.dtype, dev), _tensor("bias", bias, (I,), x.dtype, dev),
          _tensor("lengths", lengths, (B,), torch.int32, dev),
@@ -858,7 +863,7 @@ def pyramid_causal_conv_backward(x, w, bias, dy, dx, dw, db, act="none", reverse
     forward's inputs."""
     dt, dev, px, pitch = _main_pitched("x", x)
     B, T, I = x.shape
-    K = w.shape[-1] if w.dim() == 2 else 0
+    K = w.shape[-1] if _torch_tensor(w).dim() == 2 else 0
     if ws is None:
         ws = _temporary(pyramid_causal_conv_workspace_size(B, T, I, K), x.device, stream)
     _run("pyramid_causal_conv_backward", dev, stream, B, T, I, K, dt, _act(act), int(bool(reverse)),
@@ -896,7 +901,7 @@ def _select_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus, reverse, len
     dt, dev, pu, lu = _main_pitched("u", u)
     shape, dtype, f32 = u.shape, u.dtype, torch.float32
     B, T, I = shape
-    S = A.shape[-1] if A.dim() == 2 else 0
+    S = A.shape[-1] if _torch_tensor(A).dim() == 2 else 0
     pd, ld = _pitched("delta", delta, shape, dtype, dev)
     pB, lB = _pitched("Bm", Bm, (B, T, S), dtype, dev)
     pC, lC = _pitched("Cm", Cm, (B, T, S), dtype, dev)
@@ -1016,7 +1021,7 @@ def _adamw_segments(params, m, v, mscale, vscale, copies, weight_decay):
     count = len(params)
     if count < 1 or not len(m) == len(v) == count or (copies is not None and len(copies) != count):
         raise ValueError("params, m, v (and copies) must have the same length, at least 1")
-    if m[0].dtype not in (torch.float32, torch.uint8):
+    if _torch_tensor(m[0]).dtype not in (torch.float32, torch.uint8):
         raise ValueError("moments must be float32 or (8-bit codes) uint8")
     bits = 32 if m[0].dtype == torch.float32 else 8
     if bits == 8 and (mscale is None or vscale is None or not len(mscale) == len(vscale) == count):
@@ -1058,19 +1063,25 @@ def _adamw_grads(segs, shapes, grads, dev):
     if len(grads) != len(shapes):
         raise ValueError("one gradient (or None) per parameter")
     dtype = None
-    for seg, shape, g in zip(segs, shapes, grads):
-        if g is None:
-            seg.n = 0
-            continue
-        if dtype is None:
-            dtype = g.dtype
-            if dtype not in _DT:
-                raise ValueError("gradients must be float32 or bfloat16")
-        # _tensor's questions without its call (12 tensors 1 us of 13)
-        seg.grad = (g.data_ptr() if g.shape == shape and g.dtype == dtype and g.get_device() == dev and g.is_contiguous()
-                    else _tensor("grads", g, shape, dtype, dev))
-        if not seg.n:                   # left alone before
-            seg.n = shape.numel()
+    try:
+        for seg, shape, g in zip(segs, shapes, grads):
+            if g is None:
+                seg.n = 0
+                continue
+            if dtype is None:
+                dtype = g.dtype
+                if dtype not in _DT:
+                    raise ValueError("gradients must be float32 or bfloat16")
+            # _tensor's questions without its call (12 tensors 1 us of 13)
+            if g.shape == shape and g.dtype == dtype and g.get_device() == dev and g.is_contiguous():
+                seg.grad = g.data_ptr()
+            else:
+                seg.grad = _tensor("grads", g, shape, dtype, dev)
+            if not seg.n:               # left alone before
+                seg.n = shape.numel()
+    except (AttributeError, TypeError, ValueError):
+        _torch_tensor(g)
+        raise
     return PLSTM_F32 if dtype is None else _DT[dtype]
 
 
@@ -1208,7 +1219,7 @@ class AdamW:
     def moments(self, stream=None):
         """fp32 (m, v) of each parameter: the moments themselves, or what their codes stand for."""
         if self.bits == 32:
-            return list(zip(self.m, self.v))
+            return list(zip(self._show("_m"), self._show("_v")))
         caller = torch.cuda.current_stream(self._dev)
         side = caller if stream is None else _torch_stream(stream, self.params[0].device)
         with torch.cuda.stream(side):

@@ -2,6 +2,7 @@
 are answered by stand-ins, calls are recorded and not made."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
@@ -166,3 +167,40 @@ def test_updated_memory_is_apart(bits, calls):
         P.pyramid_adamw_step([whole[:300], whole[200:500]], [whole.new_ones(300)] * 2, [codes[:300], codes[512:812]],
                              [codes[1024:1324], codes[1536:1836]], 1e-3, 1, mscale=[scales[:2], scales[2:4]],
                              vscale=[scales[4:6], scales[6:]])
+
+
+# a tensor's attributes, not a tensor's type
+FOREIGN = [np.zeros((2, 4), np.float32), [0.0], "ab", 3]
+
+
+@pytest.mark.parametrize("t", FOREIGN, ids=lambda t: type(t).__name__)
+def test_arrays_of_others(t, monkeypatch):
+    """Where a tensor is expected anything else is a TypeError, as for main tensors."""
+    with pytest.raises(TypeError):
+        P._tensor("t", t, (2, 4), F32, 0)
+    with pytest.raises(TypeError):
+        P._pitched("t", t, (1, 2, 4), F32, 0)
+    x, w = torch.zeros((1, 2, 4)), torch.zeros((4, 4))
+    monkeypatch.setattr(P, "_main_pitched", lambda name, t: (0, -1, t.data_ptr(), 0))
+    monkeypatch.setattr(P, "_main", lambda name, t, dims: (0, t.data_ptr(), -1))
+    monkeypatch.setattr(P, "_run", lambda *a: pytest.fail("called"))
+    for other in (t, None):
+        with pytest.raises(TypeError):
+            P.pyramid_causal_conv_forward(x, other, None, x)
+        with pytest.raises(TypeError):
+            P.pyramid_causal_conv_backward(x, other, None, x, x, w, None, ws=x)
+        with pytest.raises(TypeError):
+            P.pyramid_selective_scan_forward(x, x, other, x, x, x, ws=x)
+    with pytest.raises(TypeError):
+        P.pyramid_causal_conv_forward(x, w, t, x)
+    with pytest.raises(TypeError):
+        P.pyramid_selective_scan_forward(x, t, w, x, x, x, ws=x)
+    p = [torch.zeros(4), torch.zeros(4)]
+    opt = P.AdamW(p)
+    for grads in ([t, t], [torch.ones(4), t]):
+        with pytest.raises(TypeError):
+            opt.step(grads)
+    with pytest.raises(TypeError):
+        P.pyramid_adamw_step(p, [None, None], [t, t], p, 1e-3, 1)
+    with pytest.raises(TypeError):
+        P.AdamW(p, copies=[t, None])
