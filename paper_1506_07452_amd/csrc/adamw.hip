@@ -241,9 +241,10 @@ __device__ inline void adamw_tile(const AdamArgs &a, const AdamSeg &s, long long
             m[u][j] = blend(a.b1, m[u][j], k1, gd);
             v[u][j] = blend(a.b2, v[u][j], k2, gd * gd);
             // off by 8 steps of fp32 at most; the root's instruction takes subnormal numbers for 0, which only an
-            // eps of their roots' size would show (ROOT)
+            // eps of their roots' size would show (ROOT: there a whole root, and a quotient, as 1 / eps need not be a number)
             const float root = ROOT ? sqrtf(v[u][j] * now.c2) : __builtin_amdgcn_sqrtf(v[u][j] * now.c2);
-            const float step = m[u][j] * now.c1 * __builtin_amdgcn_rcpf(root + a.eps);
+            const float step = ROOT ? m[u][j] * now.c1 / (root + a.eps)
+                                    : m[u][j] * now.c1 * __builtin_amdgcn_rcpf(root + a.eps);
             q[j] = fmaf(-lr, fmaf(s.decay, p[u][j], step), p[u][j]);
         }
         store_out<STREAM>(s.theta + at, have, q);

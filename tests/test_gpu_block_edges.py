@@ -43,6 +43,28 @@ def test_update_of_tensors_with_other_memory(bits):
     assert all(torch.equal(a, b) for a, b in before)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [2.0 ** -149, 2.0 ** -130, 2.0 ** -126, 2.0 ** -100, 2.0 ** -50])
+def test_update_with_a_tiny_eps(eps, bits):
+    """An eps (fp32 numbers here, subnormal ones among them) whose reciprocal is no number: elements without a gradient so far
+    only decay, others move by their quotient; gradients whose squares are 0 have eps alone below them."""
+    say("adamw eps", eps, bits)
+    n = 700
+    p, g = rand(1, (n,), F32), rand(2, (n,), F32, 0.1)
+    g[::3] = 0.0
+    g[1::7] = 2.0 ** -80                # of the square an fp32 number holds nothing; over eps it is 2^69 at most
+    p0 = p.to(DEV)
+    opt = P.AdamW([p0], lr=1e-3, betas=(0.9, 0.99), eps=eps, weight_decay=0.1, bits=bits, seed=5)
+    m, v = torch.zeros(n), torch.zeros(n)
+    for t in (1, 2):
+        new, bound, m, v = R.adamw(p, g, m, v, t, 1e-3, (0.9, 0.99), eps, 0.1)
+        opt.step([g.to(DEV)])
+        near("p", p0.cpu(), new, bound + 2.0 ** -23 * 1e-3 * 4)
+        p = p0.cpu()
+        if bits == 8:
+            m, v = (x.cpu() for x in opt.moments()[0])
+
+
 # ------------------------------------------------- more work than a launch takes
 
 @pytest.mark.parametrize("N,G", [(1024, 4096), (1025, 4096), (513, 4100)])
