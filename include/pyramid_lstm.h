@@ -546,7 +546,8 @@ int pyramid_causal_conv_backward(int64_t B, int64_t T, int64_t I, int32_t K, int
  *   p_s[i] = sum_k C_s[k] h_s[i][k] + D[i] u_s[i],
  *   y_s = p_s, or p_s z_s sigmoid(z_s) with z.
  *   u, delta, z : [B][T][I] in `dtype` with pitches (z may be NULL).
- *   A           : fp32 [I][S];  D, delta_bias: NULL (zeros), or fp32 [I].
+ *   A           : fp32 [I][S] (-infinity: the state before is forgotten);  D, delta_bias: NULL
+ *                 (zeros), or fp32 [I].
  *   Bm, Cm      : [B][T][S] in `dtype` with pitches: the same for all channels.
  *   h0, hT      : NULL, or fp32 [B][I][S]: the state before (NULL: zeros) and after; hT may
  *                 be h0 itself, so single steps (T = 1) update a state in place.

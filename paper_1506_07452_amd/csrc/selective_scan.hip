@@ -109,6 +109,15 @@ template <> struct Few<uint16_t, 2> {
     }
 };
 
+// A log2(e), of which a step's exponent is a multiple; within 2^100.  A of minus infinity (a state that forgets at once) times the 0 of
+// a step that a sequence does not have is to be 0; so large a number forgets in all steps of over 2^-92, and leaves what a
+// gradient times it is a number.
+__device__ inline float exponent_of(float A)
+{
+    const float v = A * kLog2e, most = 1.2676506e30f;
+    return v < -most ? -most : v > most ? most : v;         // a NaN stays one
+}
+
 // log(1 + exp(v)).  With e = exp(-|v|) and w = 1 + e rounded, log(1 + e) is log(w) and to first order what w has
 // lost, e - (w - 1), over w: left out, as what is lost is below 2^-24 and w is 1 where log(w) is small.
 __device__ inline float softplus_of(float v)
@@ -404,7 +413,7 @@ k_sel_fwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
         const float *from = a.chunks > 1 ? start + chunk * a.B * a.I * a.S : h0;
         load_states<SR>(from + at, from ? have : 0, h[c]);
 #pragma unroll
-        for (int j = 0; j < SR; ++j) A2[c][j] *= kLog2e;
+        for (int j = 0; j < SR; ++j) A2[c][j] = exponent_of(A2[c][j]);
         bias[c] = dbias && c < l.have ? dbias[l.i + c] : 0.0f;
         Dv[c] = D && c < l.have ? D[l.i + c] : 0.0f;
     }
@@ -533,7 +542,7 @@ k_sel_fold(SelArgs a, const T *u, const T *delta, const float *A, const T *rows,
         load_states<SR>(A + (l.i + c) * a.S + row * SR, states_have<SR>(a, row, c < l.have), A2[c]);
 #pragma unroll
         for (int j = 0; j < SR; ++j) {
-            A2[c][j] *= kLog2e;
+            A2[c][j] = exponent_of(A2[c][j]);
             h[c][j] = 0.0f;
         }
         bias[c] = dbias && c < l.have ? dbias[l.i + c] : 0.0f;
@@ -619,7 +628,7 @@ k_sel_chain(long long cols, long long I, int S, int chunks, const float *A, cons
 {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, col = at / S, states = cols * S;
     if (at >= states) return;
-    const float A2 = A[col % I * S + (at - col * S)] * kLog2e;
+    const float A2 = exponent_of(A[col % I * S + (at - col * S)]);
     float h = from ? from[at] : 0.0f;
     constexpr int U = 16;
     for (int n = 0; n < chunks; n += U) {
@@ -674,7 +683,7 @@ k_sel_step(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, c
     if (live) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            h[j] = fmaf(__builtin_amdgcn_exp2f(d * (Av[j] * kLog2e)), h[j], d * uv * Bv[j]);
+            h[j] = fmaf(__builtin_amdgcn_exp2f(d * exponent_of(Av[j])), h[j], d * uv * Bv[j]);
             s = j < have ? fmaf(Cv[j], h[j], s) : s;
         }
     }
@@ -731,7 +740,7 @@ k_sel_bwd(SelArgs a, const T *u, const T *delta, const float *A, const T *Bm, co
     load_states<SR>(A + ic * a.S + row * SR, have, A2);
 #pragma unroll
     for (int j = 0; j < SR; ++j) {
-        A2[j] *= kLog2e;
+        A2[j] = exponent_of(A2[j]);
         dA[j] = 0.0f;
         dAs[j] = 0.0;
     }

@@ -10,8 +10,8 @@ from paper_1506_07452_amd import network as net
 from tests import block_ref as R
 from tests.gpu_util import DEV, say
 from tests.seq_ref import rounded
-from tests.test_gpu_block import gn_case
-from tests.test_gpu_sequence import BF16, F32, near, rand
+from tests.test_gpu_block import gn_case, poisoned
+from tests.test_gpu_sequence import BF16, DTYPES, F32, near, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -173,3 +173,42 @@ def test_sweep_without_biases(left_out):
     assert torch.equal(y, got_y) and set(got) == set(want)
     for k, g in got.items():
         assert g is None if k in left_out else torch.equal(g, want[k]), k
+
+
+# ------------------------------------------------------- numbers at the ends of fp32
+
+@DTYPES
+@pytest.mark.parametrize("B,T,I,S,lengths", [(4, 1, 7, 16, None), (5, 70, 18, 5, [0, 1, 33, 64, 70]), (3, 40, 17, 16, [40, 7, 0]),
+                                             (2, 520, 16, 16, [520, 3]), (3, 90, 9, 40, [0, 90, 50]), (1, 1100, 33, 16, [500])])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_scan_forgets(B, T, I, S, lengths, reverse, dtype):
+    """States with A of minus infinity forget at once what was before a step, and keep what they have where a sequence has no
+    steps; outputs and gradients as with an A of -1e25, whose decays are 0 and 1 as well."""
+    say("select forgets", B, T, I, S, reverse, dtype)
+    u, delta, z, dy = (poisoned(rand(k, (B, T, I), dtype), lengths) for k in range(4))
+    Bm, Cm = (poisoned(rand(4 + k, (B, T, S), dtype), lengths) for k in range(2))
+    h0, dhT, D, bias = rand(6, (B, I, S), F32), rand(7, (B, I, S), F32), rand(8, (I,), F32), rand(9, (I,), F32, 0.5, -2.0)
+    A = -torch.exp(rand(10, (I, S), F32, 0.7))
+    at_once = rand(11, (I, S), F32) > 0.5
+    on = [None if t is None else t.to(DEV) for t in (u, delta, z, dy, Bm, Cm, h0, dhT, D, bias)]
+    ud, dd, zd, dyd, Bd, Cd, h0d, dhTd, Dd, bd = on
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+
+    def run(most):
+        Ad = A.masked_fill(at_once, most).to(DEV)
+        how = dict(D=Dd, z=zd, delta_bias=bd, softplus=True, reverse=reverse, lengths=ln)
+        saved = torch.empty(P.pyramid_selective_scan_saved_size(B, T, I, S), dtype=torch.uint8, device=DEV)
+        y, y2, hT, hT2 = torch.empty_like(ud), torch.empty_like(ud), torch.empty_like(h0d), torch.empty_like(h0d)
+        P.pyramid_selective_scan_forward(ud, dd, Ad, Bd, Cd, y, h0=h0d, hT=hT, **how)
+        P.pyramid_selective_scan_forward(ud, dd, Ad, Bd, Cd, y2, h0=h0d, hT=hT2, saved=saved, **how)
+        g = dict(du=torch.empty_like(ud), ddelta=torch.empty_like(ud), dA=torch.empty_like(Ad), dB=torch.empty_like(Bd), dC=torch.empty_like(Bd),
+                 dD=torch.empty_like(Dd), dz=torch.empty_like(ud), ddelta_bias=torch.empty_like(Dd), dh0=torch.empty_like(h0d))
+        P.pyramid_selective_scan_backward(ud, dd, Ad, Bd, Cd, saved, dyd, dhT=dhTd, **g, **how)
+        return dict(g, y=y, y2=y2, hT=hT, hT2=hT2)
+    got, want = run(float("-inf")), run(-1e25)
+    ref = R.Select(u, delta, A.masked_fill(at_once, -1e25), Bm, Cm, D, z, bias, True, reverse, lengths, h0)
+    near("y", want["y"].cpu(), ref.y, rounded(ref.y, ref.ey, dtype))
+    near("hT", want["hT"].cpu(), ref.hT, ref.ehT)
+    for k, t in got.items():
+        assert t.isfinite().all() and torch.equal(t, want[k]), k
+    assert not got["dA"][at_once.to(DEV)].any()
