@@ -2,6 +2,7 @@
 launch takes, arguments that are left out, numbers at the ends of fp32, and sums that are held in 64 bits."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
@@ -212,3 +213,82 @@ def test_scan_forgets(B, T, I, S, lengths, reverse, dtype):
     for k, t in got.items():
         assert t.isfinite().all() and torch.equal(t, want[k]), k
     assert not got["dA"][at_once.to(DEV)].any()
+
+
+# --------------------------------------------------------- sums in 64 bits
+#
+# Sums of N equal terms 1 + k 2^-23, whose last bits a running fp32 sum drops term by term once it is long
+# enough, always in the same direction.  A kernel's bound counts the additions that it makes in fp32 before it goes on in 64
+# bits, and the last rounding; one that added up a lane's terms in fp32 would be past it (`lost`).
+
+def lost(c, n):
+    """What a running fp32 sum of n terms c is off by, relative to it."""
+    s = np.cumsum(np.full(n, c, np.float32), dtype=np.float32)[-1]
+    return abs(float(s) / (n * c) - 1)
+
+
+def equal_terms(name, got, c, n, additions, in_a_lane):
+    """`got`: sums of n terms c with `additions` roundings to fp32, the last one among them, of each."""
+    assert lost(c, in_a_lane) > 1.5 * additions * R.U, "these terms show nothing"
+    want = torch.full_like(got, 1.0, dtype=torch.float64, device="cpu") * (n * c)
+    near(name, got.cpu(), want, want * additions * R.U)
+
+
+def test_group_norm_sums_in_64_bits():
+    """Two rows in fp32, then 64 bits; a thread has 88 rows."""
+    V, C, c = 1 << 24, 4, 1 + 15 * 2.0 ** -23
+    say("group norm sums")
+    x = torch.ones((1, V, C), device=DEV)
+    x[:, ::2] = -1.0                        # mean 0, deviation 1
+    one, zero = torch.ones(C, device=DEV), torch.zeros(C, device=DEV)
+    y, stats, dg, db = torch.empty_like(x), torch.empty((1, 2, 2), device=DEV), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+    P.pyramid_group_norm_forward(x, one, zero, y, 2, stats=stats, eps=1e-30)
+    assert torch.equal(y, x) and torch.equal(stats.cpu(), torch.tensor([[[0.0, 1.0]] * 2]))
+    P.pyramid_group_norm_backward(x, one, zero, stats, torch.full_like(x, c), y, dg, db, 2)
+    equal_terms("dbeta", db, c, V, 2, 88)
+    assert not dg.any()
+    P.pyramid_group_norm_backward(x, one, zero, stats, x * c, y, dg, db, 2)
+    equal_terms("dgamma", dg, c, V, 2, 88)
+    assert not db.any()
+
+
+def test_scan_sums_in_64_bits():
+    """16 steps of dA and 4 of dD and ddelta_bias in fp32 and a wave's share, then 64 bits; a wave has 1024 steps, a lane 256 of
+    them."""
+    T, I, S, c = 2048, 32768, 2, 1 + 63 * 2.0 ** -23
+    say("scan sums")
+
+    def full(v, *shape):
+        return torch.full(shape, v, device=DEV)
+
+    def run(u, B, dhT):
+        """The gradients where all decays are 1, nothing is read out and the state before is 1."""
+        one, A, D, Bm, Cm = full(1.0, 1, T, I), full(0.0, I, S), full(0.0, I), full(B, 1, T, S), full(0.0, 1, T, S)
+        u, h0, dhT, y = full(u, 1, T, I), full(1.0, 1, I, S), full(dhT, 1, I, S), torch.empty((1, T, I), device=DEV)
+        saved = torch.empty(P.pyramid_selective_scan_saved_size(1, T, I, S), dtype=torch.uint8, device=DEV)
+        P.pyramid_selective_scan_forward(u, one, A, Bm, Cm, y, D=D, h0=h0, saved=saved)
+        du, ddelta, dB, dC = torch.empty_like(u), torch.empty_like(u), torch.empty_like(Bm), torch.empty_like(Cm)
+        dA, dD, db = torch.empty_like(A), torch.empty_like(D), torch.empty_like(D)
+        P.pyramid_selective_scan_backward(u, one, A, Bm, Cm, saved, full(c, 1, T, I), du, ddelta, dA, dB, dC, D=D, dD=dD, ddelta_bias=db,
+                                          dhT=dhT)
+        return dA, dD, db
+    # G = c and h = 1: dA sums c d; dp u = c
+    dA, dD, _ = run(1.0, 0.0, c)
+    equal_terms("dA", dA, c, T, 18, 1024)
+    equal_terms("dD", dD, c, T, 6, 256)
+    # u q with q = G summed over two states of 1/2
+    _, _, db = run(c, 1.0, 0.5)
+    equal_terms("ddelta_bias", db, c, T, 6, 256)
+
+
+def test_conv_sums_in_64_bits():
+    """Two runs of 32 steps a lane and 256 lanes of a workgroup in fp32, then 64 bits, however long a sequence is: with 512
+    workgroups a lane of these would have 64 runs."""
+    T, K, c = 1 << 28, 4, 1 + 511 * 2.0 ** -23
+    say("convolution sums")
+    x, dy = torch.ones((1, T, 1), device=DEV), torch.full((1, T, 1), c, device=DEV)
+    dx, dw, db = torch.empty_like(x), torch.empty((1, K), device=DEV), torch.empty(1, device=DEV)
+    P.pyramid_causal_conv_backward(x, torch.ones((1, K), device=DEV), torch.zeros(1, device=DEV), dy, dx, dw, db)
+    for k in range(K):
+        equal_terms("dw", dw[:, k], c, T - (K - 1) + k, 64 + 256 + 2, 2048)
+    equal_terms("db", db, c, T, 64 + 256 + 2, 2048)
