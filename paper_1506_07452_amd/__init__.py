@@ -1097,8 +1097,8 @@ def _adamw_run(segs, bits, grad_dtype, dev, stream, lr, betas, eps, step, seed, 
 def pyramid_adamw_step(params, grads, m, v, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
                        mscale=None, vscale=None, copies=None, seed=0, clock=None, grad_scale=None,
                        stream=None):
-    """AdamW update number `step` (from 1) over lists of device tensors, in place: params fp32, grads
-    fp32 or bf16 (None: that tensor is left alone), m and v fp32, or uint8 codes with their
+    """AdamW update number `step` (from 1, the same for all tensors) over lists of device tensors, in
+    place: params fp32, grads fp32 or bf16 (None: that tensor is left alone), m and v fp32, or uint8 codes with their
     scales mscale and vscale (fp32, one per 256 elements, pyramid_adamw_scales).  copies: bf16
     tensors that take the updated parameters.  weight_decay: a number, or one per tensor.  lr: a
     number, or fp32 [1] on the device; grad_scale: None, or such a factor of the gradients.  clock:
@@ -1131,6 +1131,8 @@ class AdamW:
     copies: bf16 tensors (or None each) that take the updated parameters.
     weight_decay: a number or one per tensor.  capturable=True keeps the number of updates on
     the device, so that a step captured in a graph goes on counting when it is replayed.
+    The count is one for all parameters: a first gradient after many updates without one moves its
+    parameter by (1 - beta1) / sqrt(1 - beta2) times lr, as its moments are corrected for that many.
     An update works on the memory that params and copies have when it is called (a captured one on
     that of its capture).  The moments' memory, m and v (with 8 bits their codes, and the scales mscale and
     vscale), is the optimiser's from first to last: to go on from others, give them as `state`."""

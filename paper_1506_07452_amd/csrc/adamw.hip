@@ -14,7 +14,8 @@
 // m and v are made in 64 bits (as fast as 32 here), each product and the sum rounded, and then
 // rounded to fp32; ratios are 64-bit quotients: codes are a well-defined function of the inputs.
 // Bound by bytes: 66 million bf16 gradients with 8-bit moments and bf16 copies, 16 bytes an element, 203 us (5.2 TB/s; with one
-// block a wave 241), their moments as fp32 numbers, 10 bytes, 109 us (6.1 TB/s).
+// block a wave 241), their moments as fp32 numbers, 10 bytes, 109 us (6.1 TB/s); 69 million fp32 gradients with 32-bit moments, 28 bytes,
+// 355 us (5.5 TB/s).
 #include <math.h>
 
 #include "sequence.h"

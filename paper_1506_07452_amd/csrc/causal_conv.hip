@@ -7,7 +7,9 @@
 //   dw[k] = sum_s da_s x_{s - (K - 1) + k},  dbias = sum_s da_s
 // A lane has 4 channels and walks a run of positions with the last K inputs in registers,
 // so x is read once (and K - 1 rows more a run); everything is bound by bytes.  2 x 8192 x 2048 bf16, 4 taps: forward
-// 28 to 34 us (134 MB, 4 to 4.8 TB/s), backward 55 (201 MB, 3.7 TB/s: two dozen instructions an element beside them).
+// 28 to 34 us (134 MB, 4 to 4.8 TB/s), backward 55 (201 MB, 3.7 TB/s).  The backward waits: its two dozen instructions an element are
+// 16 to 20 us, but all lanes run at once, one run each, and a run of 32 positions loads some 15 times one after another (the rows
+// before it, single positions at either end, turns of four), nothing ahead of its turn.
 #include <algorithm>
 
 #include "sequence.h"

@@ -26,13 +26,15 @@ namespace plstm {
 namespace {
 
 constexpr int kSelMaxS = 64;
-constexpr int kSelKeep = 16;            // positions between the states that a training forward keeps
+// Positions between the states that a training forward keeps: those that a backward wave has in LDS at a time.  Kept states are S / 4 bytes
+// an element, written and read: 16 states 4, as much as two bf16 inputs; 64 states 16, more than all of them.
+constexpr int kSelKeep = 16;
 constexpr int kSelStage = 8;            // positions that a forward wave stages at a time
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 inline int sel_sr(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
-// Channels of a lane in the forward and the folds: two share the rows of B and C that a lane reads (2 x 4096 x 2048 515 us, with one
-// 550; 1 x 16384 x 1024 150, 163; sequences too short to fill the card lose by it, 1 x 1024 x 512 90, 78).
+// Channels of a lane in the forward and the folds: two share the rows of B and C that a lane reads (forward and backward, 2 x 4096 x
+// 2048 501 us, with one 507; 1 x 16384 x 1024 145, 148; sequences too short to fill the card lose by it, 1 x 1024 x 512 67, 64).
 __host__ __device__ constexpr int sel_cl(int SR) { return SR <= 4 ? 2 : 1; }
 
 struct SelArgs {
@@ -1044,7 +1046,8 @@ int check_sel(int64_t B, int64_t T, int64_t I, int32_t S, int32_t dtype)
 
 // Waves that fill the card, and the fewest positions of a chunk.  bf16, forward (and backward): 1 x 16384 x 1024 144 us with 4096 waves, 150
 // with 2048, 185 with 1024; 2 x 4096 x 2048 499, 515, 593.  1 x 1024 x 512 in chunks of
-// 32 positions 66 us, of 64 90, of 128 147, of 16 65.
+// 32 positions 66 us, of 64 90, of 128 147, of 16 65: a chain of 32 chunks.  The chain takes chunks one after another, 14 us for 128 of
+// them, and the rule does not weigh that: sequences of few channels have up to 4096.
 constexpr long long kSelFill = 4096, kSelChunk = 32;
 
 struct SelPlan {
